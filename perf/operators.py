@@ -205,7 +205,7 @@ def _model(case):
         dtype = "f32" if case["kv"] == "f32" else "bf16"
         shape = ModelShape("heads-%d-%d-%d" % key[:3], 1, 64, key[0], key[1], key[2], 64, 64, True, False, dtype, 1.0e4,
                            1.0e-6, kv_dtype=case["kv"] if case["kv"] in ("int8", "fp8") else "")
-        _models[key] = L.Model(shape, synth.make_weights(shape, device=DEV), max_rows=1, max_positions=64, tiles=False)
+        _models[key] = L.Model(shape, synth.make_weights(shape, device=DEV), max_rows=1, max_positions=65536, tiles=False)
     return _models[key]
 
 
