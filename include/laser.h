@@ -14,6 +14,8 @@
  *   laser_step_mixed         decode for a batch plus probe chunks for a subset, one forward
  *   laser_kv_fork, laser_forward, laser_confidence
  *                            the pieces of a probe that rides along with later decode steps
+ *   laser_kv_write, laser_kv_read, laser_attend
+ *                            a caller's own rows of K, V and queries on the paged cache
  *   laser_exit_decision      the host-side ATP decision (Eq. 5 threshold, Algorithm 1)
  *   laser_budget             the budget pre-allocation of Eq. 6-8
  *   laser_atp_match          device-side ATP detection (token-set membership)
@@ -57,7 +59,7 @@ typedef enum {
   LASER_ERR_STATE = -5          /* call out of order (e.g. before finalize, destroyed handle) */
 } laser_status;
 
-typedef enum { LASER_DTYPE_F32 = 0, LASER_DTYPE_BF16 = 1, LASER_DTYPE_FP8_E4M3 = 2 } laser_dtype;
+typedef enum { LASER_DTYPE_F32 = 0, LASER_DTYPE_BF16 = 1, LASER_DTYPE_FP8_E4M3 = 2, LASER_DTYPE_INT8 = 3 } laser_dtype;
 
 /* Message of the last failing call on this thread ("" if none).  Owned by the library. */
 const char* laser_last_error(void);
@@ -246,7 +248,11 @@ typedef struct {
   int max_positions;
   /* KV-cache element type: 0 (or dtype) = the weights' type, or LASER_DTYPE_FP8_E4M3 (bf16
    * models only): the OCP FP8 E4M3 format (bias 7, largest finite 448, NaN 0x7f/0xff), each
-   * new key and value rounded to nearest even and saturated at +-448, decoded exactly. */
+   * new key and value rounded to nearest even and saturated at +-448, decoded exactly; or
+   * LASER_DTYPE_INT8 (bf16 models only): the integers q = rint(127 x / amax) (ties to even) and
+   * one fp32 scale s = amax / 127 per (layer, position, kv head) for K and one for V, amax the
+   * largest magnitude of the head's vector; the cache stands for q s.  A vector with a NaN or an
+   * infinity reads back as NaN. */
   int kv_dtype;
 } laser_model_desc;
 
@@ -304,7 +310,8 @@ laser_status laser_model_set_tiles(laser_model* m, void* d_buf, size_t bytes, vo
  * n_layers x num_pages x n_kv_heads blocks; block (layer, page, kv_head) holds 16
  * positions x head_dim values in the order the attention kernel's matrix-core
  * operands read them: K element (t, d) at ((d/32*4 + (d%32)/8)*16 + t)*8 + d%8, V element
- * (t, d) at ((d/16*4 + t/4)*16 + d%16)*4 + t%4 (t = position within the page).  The
+ * (t, d) at ((d/16*4 + t/4)*16 + d%16)*4 + t%4 (t = position within the page).  Behind the
+ * blocks of an INT8 pool are its scales, fp32 [n_layers][num_pages][n_kv_heads][16].  The
  * block table is int32 [max_seqs][max_pages_per_seq].  Page size is 16. */
 typedef struct laser_kv laser_kv;
 
@@ -315,7 +322,7 @@ laser_status laser_kv_create(const laser_model* m, int num_pages, int max_seqs, 
  * undefined until imported).  OUT_OF_PAGES / INVALID_ARG leave the cache unchanged. */
 laser_status laser_kv_add_seq(laser_kv* kv, int seq_id, int length);
 /* Writes positions 0..length-1 of seq_id from d_k, d_v laid out [n_layers][length]
- * [n_kv_heads][head_dim] (KV-cache element type; keys already rotated).  length must equal the
+ * [n_kv_heads][head_dim] (KV-cache element type, bf16 for an INT8 cache; keys already rotated).  length must equal the
  * sequence's length. */
 laser_status laser_kv_import(laser_kv* kv, int seq_id, const void* d_k, const void* d_v, int length, void* stream);
 /* Inverse of import: gathers all positions of seq_id into [n_layers][len][hkv][hd]. */
@@ -329,6 +336,74 @@ laser_status laser_kv_fork(laser_kv* kv, int src_seq, int dst_seq, void* stream)
 laser_status laser_kv_seq_len(const laser_kv* kv, int seq_id, int* len_out);
 laser_status laser_kv_page_table(const laser_kv* kv, int seq_id, int32_t* out, int cap, int* n_out);
 laser_status laser_kv_destroy(laser_kv* kv);
+
+/* ========================================================================== */
+/* A caller's own rows on the paged cache                                      */
+/* ========================================================================== */
+/* For K, V and queries that come from elsewhere than this library's forward: another engine's
+ * prefill, layers of the caller's own, a draft model.  One layer per call.  Rows are [rows][heads]
+ * vectors of head_dim contiguous elements (fp32 or bf16) at any non-negative strides, counted in
+ * elements; rows that are written must not overlap.  Calls on one cache are ordered by the caller
+ * like every other call on it; they may be captured into a HIP graph once the block table is on the
+ * device (a call of laser_kv_write with n_runs = 0 sends it; with rows unsent a call under capture
+ * fails with STATE), and a replay repeats the captured positions and pages.  The KV pools have to be
+ * 16-byte aligned (UNSUPPORTED). */
+typedef struct {
+  void* ptr; /* device; read only where the function reads the rows */
+  int32_t dtype; /* LASER_DTYPE_F32 or LASER_DTYPE_BF16 */
+  int32_t rows;
+  int64_t row_stride, head_stride;
+} laser_rows;
+
+/* Rows row0 .. row0+n-1 of the arrays are positions pos .. pos+n-1 of sequence seq. */
+typedef struct {
+  int32_t seq, pos, n, row0;
+} laser_kv_run;
+
+/* Grows seq_id by n_tokens positions (contents undefined until written), or cuts it to `length`:
+ * the page pool's rules (laser_pages_append, laser_pages_truncate).  Host only. */
+laser_status laser_kv_append(laser_kv* kv, int seq_id, int n_tokens);
+laser_status laser_kv_truncate(laser_kv* kv, int seq_id, int length);
+
+/* Stores rows of k and v (n_kv_heads heads; keys already rotated) in layer `layer` at the runs'
+ * positions, converted to the cache's element type: fp32 as it is, bf16 rounded to nearest even, E4M3
+ * rounded to nearest even and saturated at +-448, INT8 quantised as laser_model_desc says.  Positions
+ * lie below the sequence's length; no position twice, none on a page that a fork shares
+ * (INVALID_ARG).  Other positions keep what they hold.  n_runs = 0 only sends the block table (k and v
+ * may then be NULL). */
+laser_status laser_kv_write(laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k,
+                            const laser_rows* v, void* stream);
+/* Reads the runs' positions into rows of k and v: the values that the cache stands for (INT8: q s, one
+ * fp32 product), rounded once to the rows' type.  No row twice (INVALID_ARG); other rows keep what they
+ * hold. */
+laser_status laser_kv_read(const laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k,
+                           const laser_rows* v, void* stream);
+
+/* Query rows row0 .. row0+n-1, row i at position pos + i, over the keys kv_begin .. kv_end-1 of sequence
+ * seq (kv_end = -1: the sequence's length). */
+typedef struct {
+  int32_t seq, n, row0, pos, kv_begin, kv_end;
+} laser_attend_span;
+
+/* Attention of the spans' rows over their sequences' cached positions in layer `layer`.  Query head h
+ * uses kv head h / (n_q_heads / n_kv_heads).  Row i of a span sees position t of [kv_begin, kv_end)
+ * if t <= pos + i (causal != 0) and t > pos + i - window (window > 0), and gets
+ *   o = sum_t softmax_t(scale q.k_t) v_t   in o,    log sum_t exp(scale q.k_t)   in d_lse
+ * (d_lse: [rows][n_q_heads] fp32, or NULL), so that outputs over parts of the keys can be combined.  A row
+ * that sees nothing (or only scores of -infinity) gets o = 0 and lse = -infinity.  A position that a
+ * row does not see does not touch it, whatever it holds.  Rows outside the spans keep what they hold.
+ * q and o have the same element type; o may be q itself.  With bf16 rows the softmax weights are
+ * rounded to bf16 before they meet V; with fp32 rows nothing is rounded below fp32.  Sums, maxima and the
+ * log-sum-exp are fp32 in both.  Results do not depend on what else runs, but a row's last bits may
+ * change with the other spans of the call (they decide how keys are split over workgroups).
+ * The workspace (laser_attend_workspace bytes, 16-byte aligned; NULL if 0) holds the partial results of
+ * spans whose keys are split; calls that may run at the same time, captured ones included, need
+ * workspaces of their own.  A sequence may be in several spans; a row may not (INVALID_ARG). */
+laser_status laser_attend_workspace(const laser_kv* kv, int n_spans, const laser_attend_span* spans, int dtype, int causal,
+                                    int window, size_t* bytes);
+laser_status laser_attend(laser_kv* kv, int layer, int n_spans, const laser_attend_span* spans, float scale, int causal,
+                          int window, const laser_rows* q, const laser_rows* o, float* d_lse, void* d_workspace,
+                          size_t bytes, void* stream);
 
 /* ========================================================================== */
 /* Hot path                                                                    */

@@ -25,7 +25,7 @@ PROBES = os.path.join(LIBDIR, "design_probes")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
-HIP_SOURCES = ["gemm.hip", "gemm_frag.hip", "attn.hip", "misc.hip", "runtime.cpp", "pages.cpp"]
+HIP_SOURCES = ["gemm.hip", "gemm_frag.hip", "attn.hip", "attend.hip", "kvops.hip", "misc.hip", "runtime.cpp", "pages.cpp"]
 C_SOURCES = ["controller.c", "sim.c"]
 HIP_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result",
@@ -37,7 +37,7 @@ HIP_FLAGS = [
 # beside 40 matrix-core instructions).  Other files' kernels measured no gain or a loss (3-tile
 # K-split kernel: a 37-row prefill 0.986 -> 1.032 ms).
 MFMA_VGPR = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-EXTRA_FLAGS = {"gemm_frag.hip": MFMA_VGPR, "attn.hip": MFMA_VGPR}
+EXTRA_FLAGS = {"gemm_frag.hip": MFMA_VGPR, "attn.hip": MFMA_VGPR, "attend.hip": MFMA_VGPR}
 C_FLAGS = ["-O2", "-fPIC", "-std=c99", "-Wall", "-ffp-contract=off", f"-I{INCLUDE}", f"-I{CSRC}"]
 
 

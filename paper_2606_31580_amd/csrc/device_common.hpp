@@ -32,6 +32,11 @@ struct fp8_t {
   uint8_t bits;
 };
 
+// 8-bit integers that stand for multiples of their row's scale (INT8 KV caches).
+struct i8_t {
+  int8_t bits;
+};
+
 // fp32 -> E4M3 bits: round to nearest even on the E4M3 grid (spacing 2^(e-3) in binade
 // [2^e, 2^(e+1)) for e >= -6, 2^-9 below), magnitudes that round past 448 saturate to 448,
 // NaN stays NaN.
@@ -56,6 +61,14 @@ __device__ __forceinline__ void fp8x4_to_bf16x4(uint32_t w, uint32_t& lo, uint32
   const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
   lo = __builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), 0x07060302u);
   hi = __builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), 0x07060302u);
+}
+
+// Four signed bytes of w as bf16 bit pairs (exact: 7 bits), in the same order.
+__device__ __forceinline__ void i8x4_to_bf16x4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const float a = (float)(int)(int8_t)w, b = (float)(int)(int8_t)(w >> 8);
+  const float c = (float)(int)(int8_t)(w >> 16), d = (float)((int)w >> 24);
+  lo = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+  hi = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x07060302u);
 }
 
 __device__ __forceinline__ float bf2f(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }

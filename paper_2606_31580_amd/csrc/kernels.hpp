@@ -294,10 +294,68 @@ void fetch_embed_params(FetchEmbedArgs& f, void* (&p)[12]);
 hipError_t launch_kv_copy(int kv_es, int to_pool, void* kpool, void* vpool, const int* bt, int max_pps,
                           int num_pages, int n_layers, int hkv, int hd, int seq, int len, void* k_lin,
                           void* v_lin, hipStream_t s);
+
+// Rows of K and V between a caller's arrays and the paged cache (laser_kv_write, laser_kv_read).
+constexpr int kKvRuns = 64;  // runs of one launch
+struct KvRun {
+  int seq, pos, n, row0;  // rows row0 .. row0+n-1 are positions pos .. pos+n-1 of seq
+  unsigned first;         // its first workgroup (set by the launch)
+};
+struct KvRowsArgs {
+  void* kpool;
+  void* vpool;
+  size_t scales;  // INT8: byte offset of the scales in a pool, [layers][pages][kv heads][16] fp32
+  const int* bt;
+  int max_pps, num_pages, layer, hkv;
+  void* k;  // rows; written by the read
+  void* v;
+  int64_t k_row, k_head, k_layer, v_row, v_head, v_layer;  // element strides
+  int n_runs;
+  KvRun runs[kKvRuns];
+};
+// kv_type: 0 fp32, 1 bf16, 2 E4M3, 3 INT8 (the cache); io: 0 fp32, 1 bf16 (the rows).
+hipError_t launch_kv_rows(int kv_type, int io, int hd, KvRowsArgs& a, int n_layers, bool write, hipStream_t s);
+
+// Attention of a caller's query rows over the paged cache (laser_attend).
+constexpr int kAttendSpans = 64;       // spans of one launch
+constexpr int kAttendMaxSplits = 128;  // workgroups over a span's keys, at most
+constexpr int kAttendRowCols = 16;     // columns of a query tile, row kernel (x 1 or 2)
+constexpr int kAttendTileCols = 256;   // columns of a query tile, tile kernel
+struct AttendSpan {
+  int seq, row0, n, pos, kb, ke;  // rows row0 .. row0+n-1 at positions pos ..; keys kb .. ke-1
+  int nsplit;                     // workgroups over the keys of a tile (1: the output directly)
+  unsigned part0;                 // first partial: of (row r, head h, split s) part0 + (r hq + h) nsplit + s
+  unsigned first;                 // first work item of (tile, split) pairs in the launch
+};
+struct AttendArgs {
+  const void* q;
+  void* o;
+  float* lse;  // [rows][hq] or null
+  const void* kpool;
+  const void* vpool;
+  size_t scales;
+  const int* bt;
+  int max_pps, num_pages, layer, hq, hkv, G;
+  float scale_log2;
+  int causal, window;
+  int64_t q_row, q_head, o_row, o_head;
+  int q_vec, o_vec;  // 16-byte pieces of rows are aligned
+  float* part;       // partial outputs [partial][hd]
+  float* ml;         // their (m, l)
+  int n_spans;
+  unsigned n_items;
+  AttendSpan sp[kAttendSpans];
+};
+// kind: 0, 1: the row kernel with 16, 32 columns; 2: the tile kernel.  io: 0 fp32, 1 bf16.
+hipError_t launch_attend(int kind, int kv_type, int io, int hd, const AttendArgs& a, hipStream_t s);
+// Combines the partials of a launch's spans with several splits.
+hipError_t launch_attend_merge(int io, int hd, const AttendArgs& a, hipStream_t s);
+
 hipError_t launch_confidence(const float* p, int T, int n, float* conf, hipStream_t s);
 hipError_t launch_fill_u32(unsigned* p, int n, unsigned v, hipStream_t s);
 hipError_t launch_atp_match(const int* tokens, int n, const unsigned* bitmap, int vocab, int* flags, hipStream_t s);
-hipError_t launch_page_copy(int kv_es, void* kpool, void* vpool, int num_pages, int n_layers, int hkv, int hd, int src,
-                            int dst, hipStream_t s);
+// scales: byte offset of an INT8 pool's scales, which go with the page (0: none).
+hipError_t launch_page_copy(int kv_es, void* kpool, void* vpool, int num_pages, int n_layers, int hkv, int hd, size_t scales,
+                            int src, int dst, hipStream_t s);
 
 }  // namespace laser

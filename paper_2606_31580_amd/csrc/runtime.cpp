@@ -15,6 +15,7 @@
 #include <unordered_set>
 #include <vector>
 
+#include "attend_plan.hpp"
 #include "attn_runs.hpp"
 #include "kernels.hpp"
 #include "laser.h"
@@ -168,6 +169,7 @@ struct laser_model {
   int es = 4;     // bytes per stored weight element
   int kv_es = 4;  // bytes per KV-cache element
   int kv_fp8 = 0; // KV cache in E4M3
+  int kv_i8 = 0;  // KV cache in 8-bit integers with a scale per position and head
   const void* embed = nullptr;
   const void* lm_head = nullptr;
   const void* final_norm = nullptr;
@@ -529,10 +531,10 @@ static laser_status check_desc(const laser_model_desc* d) {
   if (d->d_ffn % 8) return laser_fail(LASER_ERR_UNSUPPORTED, "d_ffn must be a multiple of 8");
   if ((d->n_q_heads * d->head_dim) % 64) return laser_fail(LASER_ERR_UNSUPPORTED, "n_q_heads*head_dim % 64 != 0");
   if (d->dtype != LASER_DTYPE_F32 && d->dtype != LASER_DTYPE_BF16) return laser_fail(LASER_ERR_INVALID_ARG, "bad dtype");
-  if (d->kv_dtype != 0 && d->kv_dtype != d->dtype && d->kv_dtype != LASER_DTYPE_FP8_E4M3)
+  if (d->kv_dtype != 0 && d->kv_dtype != d->dtype && d->kv_dtype != LASER_DTYPE_FP8_E4M3 && d->kv_dtype != LASER_DTYPE_INT8)
     return laser_fail(LASER_ERR_INVALID_ARG, "bad kv_dtype");
-  if (d->kv_dtype == LASER_DTYPE_FP8_E4M3 && d->dtype != LASER_DTYPE_BF16)
-    return laser_fail(LASER_ERR_UNSUPPORTED, "an fp8 KV cache needs bf16 weights");
+  if ((d->kv_dtype == LASER_DTYPE_FP8_E4M3 || d->kv_dtype == LASER_DTYPE_INT8) && d->dtype != LASER_DTYPE_BF16)
+    return laser_fail(LASER_ERR_UNSUPPORTED, "an 8-bit KV cache needs bf16 weights");
   if (d->max_positions < 16 || d->max_positions > 65536) return laser_fail(LASER_ERR_UNSUPPORTED, "max_positions out of range");
   if (!(d->rope_theta > 1.0f) || !(d->rms_eps > 0.0f)) return laser_fail(LASER_ERR_INVALID_ARG, "bad rope_theta or rms_eps");
   return LASER_OK;
@@ -578,7 +580,8 @@ extern "C" laser_status laser_model_create(const laser_model_desc* desc, laser_m
   m->desc = *desc;
   m->es = desc->dtype == LASER_DTYPE_BF16 ? 2 : 4;
   m->kv_fp8 = desc->kv_dtype == LASER_DTYPE_FP8_E4M3;
-  m->kv_es = m->kv_fp8 ? 1 : m->es;
+  m->kv_i8 = desc->kv_dtype == LASER_DTYPE_INT8;
+  m->kv_es = m->kv_fp8 || m->kv_i8 ? 1 : m->es;
   m->layers.assign(desc->n_layers, LayerW{});
   (void)hipGetDevice(&m->device);
   {
@@ -839,11 +842,18 @@ extern "C" laser_status laser_model_destroy(laser_model* m) {
 
 // ----------------------------------------------------------------------------- KV cache
 
+// Blocks of a pool, and where an INT8 pool's scales start: behind all blocks.
+static size_t kv_slots(const laser_model* m, int num_pages) {
+  return (size_t)m->desc.n_layers * num_pages * m->desc.n_kv_heads;
+}
+static size_t kv_scales_offset(const laser_model* m, int num_pages) {
+  return kv_slots(m, num_pages) * kPage * m->desc.head_dim * m->kv_es;
+}
+
 extern "C" laser_status laser_kv_pool_bytes(const laser_model* m, int num_pages, size_t* bytes_per_pool) {
   if (!handle_live(m)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed model");
   if (!bytes_per_pool || num_pages < 1) return laser_fail(LASER_ERR_INVALID_ARG, "bad argument");
-  const laser_model_desc& d = m->desc;
-  *bytes_per_pool = (size_t)d.n_layers * num_pages * d.n_kv_heads * kPage * d.head_dim * m->kv_es;
+  *bytes_per_pool = kv_scales_offset(m, num_pages) + (m->kv_i8 ? kv_slots(m, num_pages) * kPage * sizeof(float) : 0);
   return LASER_OK;
 }
 
@@ -1681,6 +1691,7 @@ static laser_status check_ready(laser_model* m, laser_kv* kv) {
   if (!m->finalized) return laser_fail(LASER_ERR_STATE, "model not finalized");
   if (!kv_of(kv)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed kv");
   if (kv->m != m) return laser_fail(LASER_ERR_INVALID_ARG, "kv cache belongs to another model");
+  if (m->kv_i8) return laser_fail(LASER_ERR_UNSUPPORTED, "forwards over an INT8 cache");
   return LASER_OK;
 }
 
@@ -1709,6 +1720,42 @@ static void push_updates(Plan& p, const std::vector<PageUpdate>& u) {
 
 }  // namespace
 
+static int kv_type_of(const laser_model* m) { return m->kv_i8 ? 3 : m->kv_fp8 ? 2 : m->es == 2 ? 1 : 0; }
+
+static KvRowsArgs kv_rows_args(const laser_kv* kv, int layer) {
+  KvRowsArgs a{};
+  a.kpool = kv->kpool;
+  a.vpool = kv->vpool;
+  a.scales = kv_scales_offset(kv->m, kv->pool.num_pages());
+  a.bt = kv->bt;
+  a.max_pps = kv->pool.max_pages_per_seq();
+  a.num_pages = kv->pool.num_pages();
+  a.layer = layer;
+  a.hkv = kv->m->desc.n_kv_heads;
+  return a;
+}
+
+// All positions of a sequence between an INT8 cache and dense bf16 arrays [n_layers][len][hkv][hd].
+static laser_status kv_dense(laser_kv* kv, int seq, void* d_k, void* d_v, bool write, hipStream_t s) {
+  const laser_model* m = kv->m;
+  const laser_model_desc& d = m->desc;
+  const int len = kv->pool.len(seq);
+  if (len == 0) return LASER_OK;
+  if (!aligned16(kv->kpool) || !aligned16(kv->vpool))
+    return laser_fail(LASER_ERR_UNSUPPORTED, "the KV pools are not 16-byte aligned");
+  if ((uintptr_t)d_k % 2 || (uintptr_t)d_v % 2) return laser_fail(LASER_ERR_INVALID_ARG, "elements are not aligned");
+  KvRowsArgs a = kv_rows_args(kv, 0);
+  a.k = d_k;
+  a.v = d_v;
+  a.k_head = a.v_head = d.head_dim;
+  a.k_row = a.v_row = (int64_t)d.n_kv_heads * d.head_dim;
+  a.k_layer = a.v_layer = a.k_row * len;
+  a.n_runs = 1;
+  a.runs[0] = KvRun{seq, 0, len, 0, 0};
+  HIP_TRY(launch_kv_rows(kv_type_of(m), 1, d.head_dim, a, d.n_layers, write, s));
+  return LASER_OK;
+}
+
 extern "C" laser_status laser_kv_import(laser_kv* kv, int seq_id, const void* d_k, const void* d_v, int length, void* stream) {
   if (!kv_of(kv)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed kv");
   laser_model* m = const_cast<laser_model*>(kv->m);
@@ -1720,6 +1767,7 @@ extern "C" laser_status laser_kv_import(laser_kv* kv, int seq_id, const void* d_
   laser_status st = flush_pending(kv, m, s);
   if (st != LASER_OK) return st;
   const laser_model_desc& d = m->desc;
+  if (m->kv_i8) return kv_dense(kv, seq_id, const_cast<void*>(d_k), const_cast<void*>(d_v), true, s);
   HIP_TRY(launch_kv_copy(m->kv_es, 1, kv->kpool, kv->vpool, kv->bt, kv->pool.max_pages_per_seq(),
                          kv->pool.num_pages(), d.n_layers, d.n_kv_heads, d.head_dim, seq_id, length,
                          const_cast<void*>(d_k), const_cast<void*>(d_v), s));
@@ -1737,6 +1785,7 @@ extern "C" laser_status laser_kv_export(const laser_kv* kvc, int seq_id, void* d
   laser_status st = flush_pending(kv, m, s);
   if (st != LASER_OK) return st;
   const laser_model_desc& d = m->desc;
+  if (m->kv_i8) return kv_dense(kv, seq_id, d_k, d_v, false, s);
   HIP_TRY(launch_kv_copy(m->kv_es, 0, kv->kpool, kv->vpool, kv->bt, kv->pool.max_pages_per_seq(),
                          kv->pool.num_pages(), d.n_layers, d.n_kv_heads, d.head_dim, seq_id, kv->pool.len(seq_id), d_k, d_v, s));
   return LASER_OK;
@@ -2059,7 +2108,7 @@ extern "C" laser_status laser_kv_fork(laser_kv* kv, int src_seq, int dst_seq, vo
     TimingScope scope(m);
     const hipError_t e = timed(m, LASER_K_OTHER, s, [&] {
       return launch_page_copy(m->kv_es, kv->kpool, kv->vpool, kv->pool.num_pages(), d.n_layers,
-                              d.n_kv_heads, d.head_dim, c.src, c.dst, s);
+                              d.n_kv_heads, d.head_dim, m->kv_i8 ? kv_scales_offset(m, kv->pool.num_pages()) : 0, c.src, c.dst, s);
     });
     if (e != hipSuccess) return laser_fail(LASER_ERR_HIP, "page copy: %s", hipGetErrorString(e));
   }
@@ -2133,6 +2182,344 @@ extern "C" laser_status laser_confidence(laser_model* m, const float* d_p, int T
   const hipError_t e = timed(m, LASER_K_OTHER, s, [&] { return launch_confidence(d_p, T, n, d_conf, s); });
   if (e != hipSuccess) return laser_fail(LASER_ERR_HIP, "confidence: %s", hipGetErrorString(e));
   return LASER_OK;
+}
+
+// ------------------------------------------------------- operators on a caller's rows
+
+extern "C" laser_status laser_kv_append(laser_kv* kv, int seq_id, int n_tokens) {
+  if (!kv_of(kv)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed kv");
+  if (kv->pool.live(seq_id) && n_tokens > kv->m->desc.max_positions - kv->pool.len(seq_id))
+    return laser_fail(LASER_ERR_INVALID_ARG, "seq %d would exceed max_positions", seq_id);
+  return (laser_status)kv->pool.append(seq_id, n_tokens, &kv->pending);
+}
+
+extern "C" laser_status laser_kv_truncate(laser_kv* kv, int seq_id, int length) {
+  if (!kv_of(kv)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed kv");
+  const laser_status st = (laser_status)kv->pool.truncate(seq_id, length);
+  // table rows past the length that have not been sent are void (see laser_kv_free_seq)
+  if (st == LASER_OK && !kv->pending.empty())
+    kv->pending.erase(std::remove_if(kv->pending.begin(), kv->pending.end(),
+                                     [&](const PageUpdate& u) { return u.seq == seq_id && u.idx >= kv->pool.pages_for(length); }),
+                      kv->pending.end());
+  return st;
+}
+
+namespace {
+
+// The model's device, for the time of a call.
+struct DeviceScope {
+  int prev = -1;
+  hipError_t err = hipSuccess;
+  explicit DeviceScope(int dev) {
+    err = hipGetDevice(&prev);
+    if (err == hipSuccess && prev != dev)
+      err = hipSetDevice(dev);
+    else
+      prev = -1;
+  }
+  ~DeviceScope() {
+    if (prev >= 0) (void)hipSetDevice(prev);
+  }
+};
+
+// What the calls on a caller's rows ask first: a live cache of a live model, a layer of it, pools that
+// the kernels can read in 16-byte pieces.
+laser_status check_rows_call(const laser_kv* kvc, int layer) {
+  const laser_kv* kv = kv_of(kvc);
+  if (!kv) return laser_fail(LASER_ERR_STATE, "invalid or destroyed kv");
+  if (!handle_live(kv->m)) return laser_fail(LASER_ERR_STATE, "the cache's model is destroyed");
+  if (layer < 0 || layer >= kv->m->desc.n_layers)
+    return laser_fail(LASER_ERR_INVALID_ARG, "layer %d outside [0, %d)", layer, kv->m->desc.n_layers);
+  if (!aligned16(kv->kpool) || !aligned16(kv->vpool))
+    return laser_fail(LASER_ERR_UNSUPPORTED, "the KV pools are not 16-byte aligned");
+  return LASER_OK;
+}
+
+laser_status check_rows(const laser_rows* r, const char* what, int heads, int hd, bool written) {
+  if (!r || (!r->ptr && r->rows > 0)) return laser_fail(LASER_ERR_INVALID_ARG, "%s: NULL", what);
+  if (r->dtype != LASER_DTYPE_F32 && r->dtype != LASER_DTYPE_BF16)
+    return laser_fail(LASER_ERR_UNSUPPORTED, "%s: rows are fp32 or bf16", what);
+  if (r->rows < 0 || r->rows > (1 << 30)) return laser_fail(LASER_ERR_INVALID_ARG, "%s: bad number of rows", what);
+  constexpr int64_t kFar = (int64_t)1 << 40;
+  if (r->row_stride < 0 || r->head_stride < 0 || r->row_stride > kFar || r->head_stride > kFar)
+    return laser_fail(LASER_ERR_INVALID_ARG, "%s: bad stride", what);
+  if ((uintptr_t)r->ptr % (r->dtype == LASER_DTYPE_F32 ? 4 : 2))
+    return laser_fail(LASER_ERR_INVALID_ARG, "%s: elements are not aligned", what);
+  if (written) {  // no element twice: rows within heads, or heads within rows, or one of either
+    const int64_t h = r->head_stride, w = r->row_stride;
+    const bool heads_in = (heads == 1 || h >= hd) && (r->rows <= 1 || w >= (heads - 1) * h + hd);
+    const bool rows_in = (r->rows <= 1 || w >= hd) && (heads == 1 || h >= (int64_t)(r->rows - 1) * w + hd);
+    if (!heads_in && !rows_in) return laser_fail(LASER_ERR_INVALID_ARG, "%s: written rows overlap", what);
+  }
+  return LASER_OK;
+}
+
+// [lo, hi) intervals of one id: does any pair overlap?
+struct Interval {
+  int64_t id, lo, hi;
+};
+bool overlaps(std::vector<Interval>& v) {
+  std::sort(v.begin(), v.end(), [](const Interval& a, const Interval& b) { return a.id != b.id ? a.id < b.id : a.lo < b.lo; });
+  for (size_t i = 1; i < v.size(); ++i)
+    if (v[i].id == v[i - 1].id && v[i].lo < v[i - 1].hi) return true;
+  return false;
+}
+
+// Block-table rows on the device before the kernels that read them.  A capture would replay the upload
+// with whatever the staging slot holds then.
+laser_status flush_for_rows(laser_kv* kv, hipStream_t s) {
+  if (kv->pending.empty()) return LASER_OK;
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  HIP_TRY(hipStreamIsCapturing(s, &cs));
+  if (cs != hipStreamCaptureStatusNone)
+    return laser_fail(LASER_ERR_STATE, "block-table rows are not on the device yet: call laser_kv_write with no runs before the capture");
+  return flush_pending(kv, const_cast<laser_model*>(kv->m), s);
+}
+
+laser_status kv_rows(laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k, const laser_rows* v,
+                     bool write, hipStream_t s) {
+  laser_status st = check_rows_call(kv, layer);
+  if (st != LASER_OK) return st;
+  laser_model* m = const_cast<laser_model*>(kv->m);
+  const laser_model_desc& d = m->desc;
+  if (n_runs < 0 || (n_runs > 0 && !runs)) return laser_fail(LASER_ERR_INVALID_ARG, "bad runs");
+  if (n_runs > 0) {
+    st = check_rows(k, "k", d.n_kv_heads, d.head_dim, !write);
+    if (st == LASER_OK) st = check_rows(v, "v", d.n_kv_heads, d.head_dim, !write);
+    if (st != LASER_OK) return st;
+    if (k->dtype != v->dtype) return laser_fail(LASER_ERR_UNSUPPORTED, "k and v are of different types");
+  }
+  std::vector<Interval> iv;
+  for (int i = 0; i < n_runs; ++i) {
+    const laser_kv_run& r = runs[i];
+    if (!kv->pool.live(r.seq)) return laser_fail(LASER_ERR_INVALID_ARG, "run %d: seq_id %d not present", i, r.seq);
+    const int len = kv->pool.len(r.seq);
+    if (r.n < 0 || r.pos < 0 || r.n > len - r.pos)
+      return laser_fail(LASER_ERR_INVALID_ARG, "run %d: positions outside the sequence's %d", i, len);
+    if (r.row0 < 0 || (int64_t)r.row0 + r.n > std::min(k->rows, v->rows))
+      return laser_fail(LASER_ERR_INVALID_ARG, "run %d: rows outside the arrays", i);
+    if (r.n == 0) continue;
+    if (write) {
+      const std::vector<int>& t = kv->pool.table(r.seq);
+      for (int p = r.pos / kPage; p <= (r.pos + r.n - 1) / kPage; ++p)
+        if (kv->pool.refs(t[p]) > 1)
+          return laser_fail(LASER_ERR_INVALID_ARG, "run %d: position %d is on a page that a fork shares", i, std::max(r.pos, p * kPage));
+      iv.push_back(Interval{r.seq, r.pos, (int64_t)r.pos + r.n});
+    } else {
+      iv.push_back(Interval{0, r.row0, (int64_t)r.row0 + r.n});
+    }
+  }
+  if (overlaps(iv)) return laser_fail(LASER_ERR_INVALID_ARG, write ? "two runs write the same position" : "two runs read into the same row");
+  if (!m->finalized) return laser_fail(LASER_ERR_STATE, "model not finalized");
+  DeviceScope dev(m->device);
+  HIP_TRY(dev.err);
+  st = flush_for_rows(kv, s);
+  if (st != LASER_OK) return st;
+  if (iv.empty()) return LASER_OK;
+  KvRowsArgs a = kv_rows_args(kv, layer);
+  a.k = k->ptr;
+  a.v = v->ptr;
+  a.k_row = k->row_stride;
+  a.k_head = k->head_stride;
+  a.v_row = v->row_stride;
+  a.v_head = v->head_stride;
+  TimingScope scope(m);
+  for (int i = 0; i < n_runs;) {
+    a.n_runs = 0;
+    for (; i < n_runs && a.n_runs < kKvRuns; ++i)
+      if (runs[i].n > 0) a.runs[a.n_runs++] = KvRun{runs[i].seq, runs[i].pos, runs[i].n, runs[i].row0, 0};
+    if (a.n_runs == 0) break;
+    HIP_TRY(timed(m, LASER_K_OTHER, s, [&] {
+      return launch_kv_rows(kv_type_of(m), k->dtype == LASER_DTYPE_BF16, d.head_dim, a, 1, write, s);
+    }));
+  }
+  return LASER_OK;
+}
+
+// The spans of a laser_attend call with their keys resolved, the planner's choice for each, and the
+// partials that all of them need.
+struct AttendJob {
+  std::vector<AttendSpan> sp;
+  std::vector<AttendSize> size;
+  uint64_t parts = 0;
+};
+
+laser_status plan_attend_call(const laser_kv* kv, int n_spans, const laser_attend_span* spans, int io, int causal, int window,
+                              AttendJob& job) {
+  const laser_model* m = kv->m;
+  const laser_model_desc& d = m->desc;
+  if (n_spans < 0 || (n_spans > 0 && !spans)) return laser_fail(LASER_ERR_INVALID_ARG, "bad spans");
+  if (window < 0) return laser_fail(LASER_ERR_INVALID_ARG, "window is negative");
+  if (io != LASER_DTYPE_F32 && io != LASER_DTYPE_BF16) return laser_fail(LASER_ERR_UNSUPPORTED, "rows are fp32 or bf16");
+  for (int i = 0; i < n_spans; ++i) {
+    const laser_attend_span& x = spans[i];
+    if (!kv->pool.live(x.seq)) return laser_fail(LASER_ERR_INVALID_ARG, "span %d: seq_id %d not present", i, x.seq);
+    const int len = kv->pool.len(x.seq), end = x.kv_end == -1 ? len : x.kv_end;
+    if (x.n < 0 || x.row0 < 0 || x.n > (1 << 28) || x.row0 > (1 << 30))
+      return laser_fail(LASER_ERR_INVALID_ARG, "span %d: bad rows", i);
+    if (x.pos < 0 || x.pos > (1 << 30)) return laser_fail(LASER_ERR_INVALID_ARG, "span %d: bad position", i);
+    if (x.kv_begin < 0 || x.kv_begin > end || end > len)
+      return laser_fail(LASER_ERR_INVALID_ARG, "span %d: keys outside the sequence's %d positions", i, len);
+    if (x.n == 0) continue;
+    AttendSpan a{};
+    a.seq = x.seq;
+    a.row0 = x.row0;
+    a.n = x.n;
+    a.pos = x.pos;
+    a.kb = x.kv_begin;
+    a.ke = end;
+    const int64_t lo = window > 0 ? std::max<int64_t>(a.kb, (int64_t)a.pos - window + 1) : a.kb;
+    const int64_t hi = causal ? std::min<int64_t>(a.ke, (int64_t)a.pos + a.n) : a.ke;
+    AttendSize z{};
+    z.n = a.n;
+    z.pages = hi > lo ? (int)((hi + kPage - 1) / kPage - lo / kPage) : 0;
+    job.sp.push_back(a);
+    job.size.push_back(z);
+  }
+  const int G = d.n_q_heads / d.n_kv_heads;
+  plan_attend(job.size.data(), (int)job.size.size(), G, d.n_kv_heads, m->cus, io == LASER_DTYPE_BF16 && m->kv_es <= 2);
+  for (size_t i = 0; i < job.sp.size(); ++i) {
+    job.sp[i].nsplit = job.size[i].nsplit;
+    if (job.size[i].nsplit > 1) {
+      job.sp[i].part0 = (unsigned)job.parts;
+      job.parts += (uint64_t)job.sp[i].n * d.n_q_heads * job.size[i].nsplit;
+    }
+  }
+  if (job.parts >> 32) return laser_fail(LASER_ERR_UNSUPPORTED, "too many rows and splits in one call");
+  return LASER_OK;
+}
+
+size_t attend_bytes(const laser_kv* kv, uint64_t parts) {
+  return parts == 0 ? 0 : align256((size_t)parts * kv->m->desc.head_dim * 4) + (size_t)parts * 8;
+}
+
+}  // namespace
+
+extern "C" laser_status laser_kv_write(laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k,
+                                       const laser_rows* v, void* stream) {
+  try {
+    return kv_rows(kv, layer, n_runs, runs, k, v, true, (hipStream_t)stream);
+  } catch (const std::bad_alloc&) {
+    return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
+  }
+}
+
+extern "C" laser_status laser_kv_read(const laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k,
+                                      const laser_rows* v, void* stream) {
+  try {
+    return kv_rows(const_cast<laser_kv*>(kv), layer, n_runs, runs, k, v, false, (hipStream_t)stream);
+  } catch (const std::bad_alloc&) {
+    return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
+  }
+}
+
+extern "C" laser_status laser_attend_workspace(const laser_kv* kv, int n_spans, const laser_attend_span* spans, int dtype,
+                                               int causal, int window, size_t* bytes) {
+  laser_status st = check_rows_call(kv, 0);
+  if (st != LASER_OK) return st;
+  if (!bytes) return laser_fail(LASER_ERR_INVALID_ARG, "bytes is NULL");
+  try {
+    AttendJob job;
+    st = plan_attend_call(kv, n_spans, spans, dtype, causal, window, job);
+    if (st == LASER_OK) *bytes = attend_bytes(kv, job.parts);
+    return st;
+  } catch (const std::bad_alloc&) {
+    return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
+  }
+}
+
+static laser_status attend(laser_kv* kv, int layer, int n_spans, const laser_attend_span* spans, float scale, int causal,
+                           int window, const laser_rows* q, const laser_rows* o, float* d_lse, void* d_workspace, size_t bytes,
+                           hipStream_t s) {
+  laser_status st = check_rows_call(kv, layer);
+  if (st != LASER_OK) return st;
+  laser_model* m = const_cast<laser_model*>(kv->m);
+  const laser_model_desc& d = m->desc;
+  if (!std::isfinite(scale)) return laser_fail(LASER_ERR_INVALID_ARG, "scale is not finite");
+  st = check_rows(q, "q", d.n_q_heads, d.head_dim, false);
+  if (st == LASER_OK) st = check_rows(o, "o", d.n_q_heads, d.head_dim, true);
+  if (st != LASER_OK) return st;
+  if (q->dtype != o->dtype) return laser_fail(LASER_ERR_UNSUPPORTED, "q and o are of different types");
+  if ((uintptr_t)d_lse % 4) return laser_fail(LASER_ERR_INVALID_ARG, "lse is not aligned");
+  AttendJob job;
+  st = plan_attend_call(kv, n_spans, spans, q->dtype, causal, window, job);
+  if (st != LASER_OK) return st;
+  std::vector<Interval> iv;
+  for (const AttendSpan& x : job.sp) {
+    if ((int64_t)x.row0 + x.n > std::min(q->rows, o->rows))
+      return laser_fail(LASER_ERR_INVALID_ARG, "rows %d to %lld are outside the arrays", x.row0, (long long)x.row0 + x.n - 1);
+    iv.push_back(Interval{0, x.row0, (int64_t)x.row0 + x.n});
+  }
+  if (overlaps(iv)) return laser_fail(LASER_ERR_INVALID_ARG, "two spans hold the same row");
+  const size_t need = attend_bytes(kv, job.parts);
+  if (need > 0 && (!d_workspace || bytes < need || !aligned16(d_workspace)))
+    return laser_fail(LASER_ERR_INVALID_ARG, "a 16-byte aligned workspace of %zu bytes needed", need);
+  if (!m->finalized) return laser_fail(LASER_ERR_STATE, "model not finalized");
+  DeviceScope dev(m->device);
+  HIP_TRY(dev.err);
+  st = flush_for_rows(kv, s);
+  if (st != LASER_OK) return st;
+  AttendArgs a{};
+  a.q = q->ptr;
+  a.o = o->ptr;
+  a.lse = d_lse;
+  a.kpool = kv->kpool;
+  a.vpool = kv->vpool;
+  a.scales = kv_scales_offset(m, kv->pool.num_pages());
+  a.bt = kv->bt;
+  a.max_pps = kv->pool.max_pages_per_seq();
+  a.num_pages = kv->pool.num_pages();
+  a.layer = layer;
+  a.hq = d.n_q_heads;
+  a.hkv = d.n_kv_heads;
+  a.G = d.n_q_heads / d.n_kv_heads;
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.causal = causal != 0;
+  a.window = window;
+  a.q_row = q->row_stride;
+  a.q_head = q->head_stride;
+  a.o_row = o->row_stride;
+  a.o_head = o->head_stride;
+  const int es = q->dtype == LASER_DTYPE_BF16 ? 2 : 4;
+  a.q_vec = aligned16(q->ptr) && q->row_stride * es % 16 == 0 && q->head_stride * es % 16 == 0;
+  a.o_vec = aligned16(o->ptr) && o->row_stride * es % 16 == 0 && o->head_stride * es % 16 == 0;
+  a.part = (float*)d_workspace;
+  a.ml = (float*)((char*)d_workspace + align256((size_t)job.parts * d.head_dim * 4));
+  const int io = q->dtype == LASER_DTYPE_BF16;
+  TimingScope scope(m);
+  // each kernel over the spans that it takes, then the join of those with several splits
+  for (int kind = 0; kind <= kAttendKinds; ++kind) {
+    const bool merge = kind == kAttendKinds;
+    for (size_t i = 0; i < job.sp.size();) {
+      a.n_spans = 0;
+      uint64_t items = 0;
+      for (; i < job.sp.size() && a.n_spans < kAttendSpans; ++i) {
+        if (merge ? job.sp[i].nsplit == 1 : job.size[i].kind != kind) continue;
+        const uint64_t mine = merge ? (uint64_t)job.sp[i].n * d.n_q_heads : (uint64_t)job.size[i].tiles * job.sp[i].nsplit;
+        if (a.n_spans > 0 && (items + mine) * (merge ? 1 : d.n_kv_heads) >> 31) break;
+        a.sp[a.n_spans] = job.sp[i];
+        a.sp[a.n_spans++].first = (unsigned)items;
+        items += mine;
+      }
+      if (a.n_spans == 0) break;
+      if (items * (merge ? 1 : d.n_kv_heads) >> 31) return laser_fail(LASER_ERR_UNSUPPORTED, "too many rows in a span");
+      a.n_items = (unsigned)items;
+      HIP_TRY(timed(m, LASER_K_ATTN, s, [&] {
+        return merge ? launch_attend_merge(io, d.head_dim, a, s) : launch_attend(kind, kv_type_of(m), io, d.head_dim, a, s);
+      }));
+    }
+  }
+  return LASER_OK;
+}
+
+extern "C" laser_status laser_attend(laser_kv* kv, int layer, int n_spans, const laser_attend_span* spans, float scale,
+                                     int causal, int window, const laser_rows* q, const laser_rows* o, float* d_lse,
+                                     void* d_workspace, size_t bytes, void* stream) {
+  try {
+    return attend(kv, layer, n_spans, spans, scale, causal, window, q, o, d_lse, d_workspace, bytes, (hipStream_t)stream);
+  } catch (const std::bad_alloc&) {
+    return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
+  }
 }
 
 // ----------------------------------------------------------------------------- ATP cues

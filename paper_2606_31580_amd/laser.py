@@ -14,7 +14,7 @@ from typing import Dict, Optional, Sequence
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "liblaser.so")
 
 OK, ERR_INVALID_ARG, ERR_OUT_OF_PAGES, ERR_HIP, ERR_UNSUPPORTED, ERR_STATE = 0, -1, -2, -3, -4, -5
-DTYPE_F32, DTYPE_BF16, DTYPE_FP8_E4M3 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_FP8_E4M3, DTYPE_INT8 = 0, 1, 2, 3
 CONTINUE, EARLY_EXIT, BUDGET_EXHAUSTED = 0, 1, 2
 K_EMBED, K_QKV, K_ATTN, K_OPROJ, K_GATEUP, K_DOWN, K_LMHEAD, K_OTHER = range(8)
 KERNEL_CLASSES = {"embed": 0, "qkv": 1, "attn": 2, "oproj": 3, "gateup": 4, "down": 5, "lmhead": 6, "other": 7}
@@ -104,6 +104,12 @@ _SIGS = {
     "laser_kv_seq_len": (_I, [_P, _I, C.POINTER(_I)]),
     "laser_kv_page_table": (_I, [_P, _I, _I32P, _I, C.POINTER(_I)]),
     "laser_kv_destroy": (_I, [_P]),
+    "laser_kv_append": (_I, [_P, _I, _I]),
+    "laser_kv_truncate": (_I, [_P, _I, _I]),
+    "laser_kv_write": (_I, [_P, _I, _I, _P, _P, _P, _P]),
+    "laser_kv_read": (_I, [_P, _I, _I, _P, _P, _P, _P]),
+    "laser_attend_workspace": (_I, [_P, _I, _P, _I, _I, _I, C.POINTER(C.c_size_t)]),
+    "laser_attend": (_I, [_P, _I, _I, _P, C.c_float, _I, _I, _P, _P, _P, _P, C.c_size_t, _P]),
     "laser_prefill": (_I, [_P, _P, _I, _P, _I, _P, _P]),
     "laser_decode_step": (_I, [_P, _P, _I, _I32P, _P, _P, _P, _P, _P]),
     "laser_decode_step_static": (_I, [_P, _P, _I, _I32P, _P, _P, _P, _P, _P]),
@@ -253,7 +259,7 @@ def desc_from_shape(shape, max_positions: int = 16640) -> laser_model_desc:
         shape.n_layers, shape.d_model, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.d_ffn, shape.vocab,
         int(shape.tied_embeddings), int(shape.qkv_bias), DTYPE_BF16 if shape.dtype == "bf16" else DTYPE_F32,
         float(shape.rope_theta), float(shape.rms_eps), int(max_positions),
-        DTYPE_FP8_E4M3 if getattr(shape, "kv_dtype", "") == "fp8" else 0)
+        {"fp8": DTYPE_FP8_E4M3, "int8": DTYPE_INT8}.get(getattr(shape, "kv_dtype", ""), 0))
 
 
 def _stream_ptr(stream) -> Optional[int]:
@@ -371,6 +377,13 @@ class KVCache:
     def free_seq(self, seq: int):
         _call("laser_kv_free_seq", self.h, seq)
 
+    def append(self, seq: int, n: int = 1):
+        """n more positions, to be filled by laser_kv_write."""
+        _call("laser_kv_append", self.h, seq, n)
+
+    def truncate(self, seq: int, length: int):
+        _call("laser_kv_truncate", self.h, seq, length)
+
     def fork(self, src: int, dst: int, stream=None):
         """dst (a free slot) starts as a copy of src that shares src's full pages."""
         _call("laser_kv_fork", self.h, src, dst, _stream_ptr(stream))
@@ -447,6 +460,118 @@ def laser_step_mixed(model: Model, kv: KVCache, seq_ids: Sequence[int], d_tokens
     _call("laser_step_mixed", model.h, kv.h, len(seq_ids), _i32arr(seq_ids), d_tokens.data_ptr(), d_next.data_ptr(),
           d_max_prob.data_ptr(), n, _i32arr(probe_idx) if n else None, _ptr(d_suffix) if n else None,
           d_suffix.numel() if n else 0, T, _ptr(d_conf) if n else None, _ptr(d_argmax) if n else None, _stream_ptr(stream))
+
+
+# --------------------------------------------------------------------------- a caller's own rows
+
+class laser_rows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int32), ("row_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
+
+
+class laser_kv_run(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("seq", "pos", "n", "row0")]
+
+
+class laser_attend_span(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("seq", "n", "row0", "pos", "kv_begin", "kv_end")]
+
+
+def kv_run(seq: int, pos: int, n: int, row0: int = 0) -> laser_kv_run:
+    """Rows row0 .. row0+n-1 are positions pos .. pos+n-1 of seq."""
+    return laser_kv_run(seq, pos, n, row0)
+
+
+def attend_span(seq: int, n: int, pos: int, row0: int = 0, kv_begin: int = 0, kv_end: int = -1) -> laser_attend_span:
+    """Query rows row0 .. row0+n-1 at positions pos .. over the keys kv_begin .. kv_end-1 of seq (-1: all)."""
+    return laser_attend_span(seq, n, row0, pos, kv_begin, kv_end)
+
+
+def _rows(t, what: str, kv: KVCache, heads: int) -> laser_rows:
+    """A [rows, heads, head_dim] tensor (fp32 or bf16, contiguous in its last dimension) as the library takes it."""
+    dtype = _ROW_DTYPES.get(str(t.dtype))
+    hd = kv.model.shape.head_dim
+    if dtype is None:
+        raise TypeError(f"{what}: rows are float32 or bfloat16, not {t.dtype}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != hd:
+        raise ValueError(f"{what}: expected [rows, {heads}, {hd}], got {tuple(t.shape)}")
+    if t.device != kv.k_pool.device:
+        raise ValueError(f"{what}: on {t.device}, the cache on {kv.k_pool.device}")
+    if t.stride(2) != 1:
+        raise ValueError(f"{what}: the last dimension is not contiguous")
+    return laser_rows(t.data_ptr(), dtype, t.shape[0], t.stride(0), t.stride(1))
+
+
+_ROW_DTYPES = {"torch.float32": DTYPE_F32, "torch.bfloat16": DTYPE_BF16}
+
+
+def _stream_of(kv: KVCache, stream) -> int:
+    """The given stream, or the current one of the cache's device."""
+    if stream is None:
+        import torch
+        stream = torch.cuda.current_stream(kv.k_pool.device)
+    return stream.cuda_stream
+
+
+def _kv_rows(fn, kv, layer, runs, k, v, stream):
+    heads = kv.model.shape.n_kv_heads
+    n = len(runs)
+    arr = (laser_kv_run * n)(*runs) if n else None
+    rk = C.byref(_rows(k, "k", kv, heads)) if n else None
+    rv = C.byref(_rows(v, "v", kv, heads)) if n else None
+    _call(fn, kv.h, layer, n, arr, rk, rv, _stream_of(kv, stream))
+
+
+def laser_kv_write(kv: KVCache, layer: int, runs: Sequence[laser_kv_run], k=None, v=None, stream=None) -> None:
+    """Rows of k and v ([rows, kv heads, head_dim]) into the cache, in its element type; no runs: only the block table goes up."""
+    _kv_rows("laser_kv_write", kv, layer, runs, k, v, stream)
+
+
+def laser_kv_read(kv: KVCache, layer: int, runs: Sequence[laser_kv_run], k, v, stream=None) -> None:
+    """The runs' positions as the values the cache stands for, into rows of k and v."""
+    _kv_rows("laser_kv_read", kv, layer, runs, k, v, stream)
+
+
+def laser_attend_workspace(kv: KVCache, spans: Sequence[laser_attend_span], dtype: int = DTYPE_BF16, causal: bool = True,
+                           window: int = 0) -> int:
+    """Bytes of workspace that laser_attend needs for these spans."""
+    arr = (laser_attend_span * len(spans))(*spans)
+    nb = C.c_size_t()
+    _call("laser_attend_workspace", kv.h, len(spans), arr, dtype, int(causal), window, C.byref(nb))
+    return nb.value
+
+
+def laser_attend(kv: KVCache, layer: int, spans: Sequence[laser_attend_span], q, o, lse=None, scale: Optional[float] = None,
+                 causal: bool = True, window: int = 0, workspace=None, stream=None) -> None:
+    """Attention of the spans' rows of q ([rows, query heads, head_dim]) over their cached positions, into o
+    (of q's shape and type) and lse ([rows, query heads] float32).  scale: 1/sqrt(head_dim) unless given.
+    workspace: a uint8 tensor of laser_attend_workspace bytes; without one the call takes its own from the
+    allocator, for the stream it runs on."""
+    import torch
+
+    shape = kv.model.shape
+    rq, ro = _rows(q, "q", kv, shape.n_q_heads), _rows(o, "o", kv, shape.n_q_heads)
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.dim() != 2 or lse.shape[1] != shape.n_q_heads or lse.shape[0] < q.shape[0]:
+            raise ValueError(f"lse: expected float32 [{q.shape[0]}, {shape.n_q_heads}], got {lse.dtype} {tuple(lse.shape)}")
+        if not lse.is_contiguous() or lse.device != q.device:
+            raise ValueError("lse: not contiguous, or on another device")
+    n = len(spans)
+    arr = (laser_attend_span * n)(*spans)
+    if workspace is None:
+        nb = C.c_size_t()
+        _call("laser_attend_workspace", kv.h, n, arr, rq.dtype, int(causal), window, C.byref(nb))
+        if nb.value:
+            if stream is None:
+                workspace = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+            else:
+                with torch.cuda.stream(stream):
+                    workspace = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+    elif workspace.device != q.device or not workspace.is_contiguous():
+        raise ValueError("workspace: not contiguous, or on another device")
+    _call("laser_attend", kv.h, layer, n, arr, shape.head_dim ** -0.5 if scale is None else scale, int(causal), window,
+          C.byref(rq), C.byref(ro), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+          _stream_of(kv, stream))
 
 
 # --------------------------------------------------------------------------- serving simulation
