@@ -84,8 +84,9 @@ __device__ __forceinline__ void st_out4(const AttendArgs& a, int row, int head, 
 }
 
 // Eight dims of a query row as one operand of each part.
+// (flip: sign bits to invert in every element, for the kernels that want a positive scale)
 template <class IT, int PARTS>
-__device__ __forceinline__ void ld_query8(const AttendArgs& a, int64_t e, bf16x8* out) {
+__device__ __forceinline__ void ld_query8(const AttendArgs& a, int64_t e, bf16x8* out, uint32_t flip = 0) {
   if constexpr (std::is_same_v<IT, bf16_t>) {
     const uint16_t* p = (const uint16_t*)a.q + e;
     u32x4 w;
@@ -95,6 +96,8 @@ __device__ __forceinline__ void ld_query8(const AttendArgs& a, int64_t e, bf16x8
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i] | ((uint32_t)p[2 * i + 1] << 16);
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] ^= flip | (flip >> 16);
     out[0] = __builtin_bit_cast(bf16x8, w);
   } else {
     const float* p = (const float*)a.q + e;
@@ -112,7 +115,7 @@ __device__ __forceinline__ void ld_query8(const AttendArgs& a, int64_t e, bf16x8
       uint32_t s[3];
       split3(x[i >> 1][2 * (i & 1)], x[i >> 1][2 * (i & 1) + 1], s);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) w[k][i] = s[k];
+      for (int k = 0; k < 3; ++k) w[k][i] = s[k] ^ (flip | (flip >> 16));
     }
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) out[k] = __builtin_bit_cast(bf16x8, w[k]);
@@ -477,6 +480,377 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
   }
 }
 
+// ---------------------------------------------------------------------------------- many columns
+// Chunks of many rows: the matrix cores' work.  A workgroup of 8 waves takes a tile of 256 columns, 32 to a
+// wave, over a share of the tile's pages, 4 pages (64 positions) at a time: the waves fetch them together
+// (half of them K, half V; the next 4 pages' words are in flight while these are computed), convert them
+// to bf16 once for all 256 columns and leave them in one of two LDS buffers in operand order; one
+// barrier per 4 pages.  v_mfma_f32_32x32x16_bf16: a wave's S^T is 2 x (32 positions x 32 columns), and a page's
+// 16 positions are one contraction step of the second product.
+// Bound by matrix and vector instructions together, which a SIMD overlaps only in part (32 rows x 64
+// positions: 32 matrix instructions of 32 cycles, some 270 vector ones).  4,096 rows of 32 heads behind
+// 12,288 positions, INT8: 1.00-1.03 ms, 930-960 TFLOP/s, where a large bf16 matrix product reaches 1,200-1,370;
+// 1.73 ms with the row kernel.  What it took: accumulators that no rare branch copies (1.28 -> 1.07 ms),
+// operands read six products ahead (4%), integer V scales inside the exponent (3%).
+// fp32 rows: 3 parts of each query and weight, the same 32 columns.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <class KT, class IT, int HD>
+__global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
+  constexpr int PARTS = std::is_same_v<IT, float> ? 3 : 1;
+  constexpr bool I8 = std::is_same_v<KT, i8_t>;
+  constexpr int ES = (int)sizeof(KT), NK = HD / 16, ND = HD / 32, SP = 4;  // SP: pages of a step
+  constexpr int PB = 32 * HD;             // bytes of a page's K or V in LDS (bf16)
+  constexpr int NL = 16 * HD * ES / 1024; // 16-byte loads per lane for a page's K or V
+  static_assert(ES <= 2, "fp32 pools: the row kernel");
+  constexpr int KB = PB + 128;            // (of a K page: two pages are read at once, from different banks)
+  __shared__ __align__(16) char s_k[2][SP * KB], s_v[2][SP * PB];
+  __shared__ __align__(16) float s_ks[2][16 * SP], s_vs[2][16 * SP], s_lv[2][16 * SP];
+  __shared__ __align__(16) int s_odd[2][SP];
+
+  const unsigned item = blockIdx.x / (unsigned)a.hkv;
+  const int kvh = (int)(blockIdx.x - item * a.hkv);
+  const AttendSpan sp = a.sp[__builtin_amdgcn_readfirstlane(find_span(a, item))];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+  const int lc = l & 31, h = l >> 5;
+  const int ncol = sp.n * a.G, tiles = (ncol + kAttendTileCols - 1) / kAttendTileCols;
+  const int local = (int)(item - sp.first), split = local % sp.nsplit;
+  const int tile = tiles - 1 - local / sp.nsplit;  // (the last tile has the most keys: first)
+  const int col0 = tile * kAttendTileCols;
+  auto first_key = [&](int row) { return a.window > 0 ? max(sp.kb, sp.pos + row - a.window + 1) : sp.kb; };
+  auto end_key = [&](int row) { return a.causal ? min(sp.ke, sp.pos + row + 1) : sp.ke; };
+  const int klo = first_key(col0 / a.G), khi = end_key((min(col0 + kAttendTileCols, ncol) - 1) / a.G);
+  const int pg0 = klo >> 4, pg1 = khi > klo ? (khi + 15) >> 4 : pg0;
+  const int share = ((pg1 - pg0 + sp.nsplit - 1) / sp.nsplit + SP - 1) / SP * SP;
+  const int s0 = pg0 + split * share, s1 = min(s0 + share, pg1);
+  const int* bt = a.bt + (size_t)sp.seq * a.max_pps;
+
+  // this wave's columns
+  const int wc0 = col0 + 32 * w, wcz = min(wc0 + 32, ncol) - 1;
+  const int row_a = min(wc0, ncol - 1) / a.G, row_z = max(wcz, 0) / a.G;
+  const int flo = first_key(row_z), fhi = min(end_key(row_a), 16 * s1);  // keys that all of them see
+  const int c = min(wc0 + lc, ncol - 1), row = c / a.G, head = kvh * a.G + c - row * a.G;
+  const int clo = first_key(row), chi = min(end_key(row), 16 * s1);
+  bf16x8 q[NK][PARTS];
+  {
+    const int64_t e = (sp.row0 + row) * a.q_row + head * a.q_head + 8 * h;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) ld_query8<IT, PARTS>(a, e + 16 * k, q[k], a.scale_log2 < 0.f ? 0x80000000u : 0u);
+  }
+  float m = -INFINITY, ls = 0.f;
+  f32x16 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+  // the scale, positive (the queries carry its sign; a score of -infinity stays one)
+  const float sc = fmaxf(fabsf(a.scale_log2), 1e-37f);
+
+  // staging: waves 0-3 K, 4-7 V of page w % 4 of the step
+  const bool st_v = w >= SP;
+  const int st_p = w & (SP - 1);
+  u32x4 raw[NL];
+  float raw_s = 0.f;
+  auto fetch = [&](int pg) {
+    const int pid = ld_const<int>(bt + min(pg + st_p, s1 - 1));  // (past the share: its last page again, unseen)
+    const size_t slot = ((size_t)a.layer * a.num_pages + pid) * a.hkv + kvh;
+    const char* pool = (const char*)(st_v ? a.vpool : a.kpool);
+    const char* b = pool + slot * (16 * HD * ES) + 16 * l;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) raw[i] = ld_global<u32x4>(b + 1024 * i);
+    if constexpr (I8) raw_s = ld_global<float>(pool + a.scales + slot * 64 + 4 * (l & 15));
+  };
+  auto convert = [&](uint32_t x, uint32_t& lo, uint32_t& hi) {
+    if constexpr (I8)
+      i8x4_to_bf16x4(x, lo, hi);
+    else
+      fp8x4_to_bf16x4(x, lo, hi);
+  };
+  // What V holds past the last key is taken as zero.  A page with an odd value is flagged; unless it is
+  // asked for as it is, its V is zero too, and its step is left for the end.  Odd are infinities and NaN,
+  // and V scales s of an integer page outside 2^-40 .. 2^40: there the weights p s are computed as
+  // exp2(score + log2 s), and the sum of the p as that of the p s times 1 / s, which saves an operation per
+  // weight but would lose some p below 2^-46 of the largest if the scales lay further apart.  (All zeros:
+  // any scale will do.)
+  auto stage = [&](int buf, int pg, bool as_is) {
+    if (!st_v) {  // as in the page: chunk (8 dims, position) at 16 bytes each
+      char* d = s_k[buf] + st_p * KB;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        if constexpr (ES == 2) {
+          *(u32x4*)(d + (64 * i + l) * 16) = raw[i];
+        } else {
+          uint32_t t[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) convert(raw[i][e], t[2 * e], t[2 * e + 1]);
+          *(u32x4*)(d + (64 * i + l) * 32) = u32x4{t[0], t[1], t[2], t[3]};
+          *(u32x4*)(d + (64 * i + l) * 32 + 16) = u32x4{t[4], t[5], t[6], t[7]};
+        }
+      }
+      if (I8 && l < 16) s_ks[buf][16 * st_p + l] = raw_s * sc;
+    } else {  // positions 4 x .. 4 x + 3 of a dim go to half x / 2 of its 16 bytes in plane x % 2
+      char* d = s_v[buf] + st_p * PB;
+      const int left = sp.ke - 16 * (pg + st_p);  // keys of the page
+      if (__builtin_expect(left < 16, 0)) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const int n = min(max(left - 4 * ((64 * i + l) / (ES == 2 ? 8 : 4) % 4), 0), 4);  // keys of the 4
+          const uint64_t keep = n == 4 ? ~0ull : (1ull << (8 * ES * n)) - 1;
+          raw[i] &= ES == 2 ? u32x4{(uint32_t)keep, (uint32_t)(keep >> 32), (uint32_t)keep, (uint32_t)(keep >> 32)}
+                            : u32x4{(uint32_t)keep, (uint32_t)keep, (uint32_t)keep, (uint32_t)keep};
+        }
+        if ((l & 15) >= left) raw_s = 0.f;
+      }
+      bool odd = I8 && raw_s != 0.f && !(raw_s >= 0x1p-40f && raw_s <= 0x1p40f);
+      if constexpr (!I8)
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (ES == 2) {
+              odd |= odd_bf16(raw[i][e]);
+            } else {  // E4M3: a NaN is all ones below the sign
+              const uint32_t x = raw[i][e] & 0x7f7f7f7fu;
+              odd |= ((x + 0x01010101u) & 0x80808080u) != 0;
+            }
+          }
+      const bool any = __ballot(odd) != 0;
+      if (l == 0) s_odd[buf][st_p] = any;
+      if (__builtin_expect(any && !as_is, 0)) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) raw[i] = u32x4{0, 0, 0, 0};
+        raw_s = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int k = 64 * i + l;
+        if constexpr (ES == 2) {
+          const int d0 = k / 32 * 16 + 2 * (k % 8), x = k / 8 % 4;
+          char* b = d + ((x & 1) * HD + d0) * 16 + (x >> 1) * 8;
+          *(u32x2*)b = u32x2{raw[i][0], raw[i][1]};
+          *(u32x2*)(b + 16) = u32x2{raw[i][2], raw[i][3]};
+        } else {
+          const int d0 = k / 16 * 16 + 4 * (k % 4), x = k / 4 % 4;
+          char* b = d + ((x & 1) * HD + d0) * 16 + (x >> 1) * 8;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t lo, hi;
+            convert(raw[i][e], lo, hi);
+            *(u32x2*)(b + 16 * e) = u32x2{lo, hi};
+          }
+        }
+      }
+      if (I8 && l < 16) {
+        const float s = raw_s == 0.f ? 0x1p-40f : raw_s;
+        s_lv[buf][16 * st_p + l] = __builtin_amdgcn_logf(s);
+        s_vs[buf][16 * st_p + l] = as_is ? raw_s : 1.f / s;
+      }
+    }
+  };
+  auto is_odd = [&](int buf) {  // (every wave sees the same)
+    const u32x4 f = *(const u32x4*)s_odd[buf];
+    return __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]) != 0;
+  };
+  // Scores of a step (64 positions from 16 pg): lane (column lc, half h), element i of s[x] is position
+  // 32 x + 8 (i / 4) + 4 h + i % 4.  Integer pages: in exp2 units, plus log2 of the position's V scale (as it
+  // is: without); otherwise before the scale.
+  f32x16 s[2];
+  auto scores = [&](int buf, bool as_is) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+      const char* b = s_k[buf] + (2 * x + (lc >> 4)) * KB + (lc & 15) * 16 + h * 256;
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        const bf16x8 kk = *(const bf16x8*)(b + 512 * k);
+#pragma unroll
+        for (int z = PARTS - 1; z >= 0; --z) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, q[k][z], s[x], 0, 0, 0);
+      }
+    }
+    if constexpr (I8)
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const f32x4 ks = *(const f32x4*)(s_ks[buf] + 32 * x + 8 * b + 4 * h);
+          const f32x4 lv = as_is ? f32x4{0.f, 0.f, 0.f, 0.f} : *(const f32x4*)(s_lv[buf] + 32 * x + 8 * b + 4 * h);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[x][4 * b + i] = fmaf(s[x][4 * b + i], ks[i], lv[i]);
+        }
+  };
+  // -infinity for positions outside lo .. hi-1
+  auto hide = [&](int pg, int lo, int hi) {
+    lo -= 16 * pg + 4 * h;
+    hi -= 16 * pg + 4 * h;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int t = 32 * x + 8 * (i >> 2) + (i & 3);
+        if (t < lo || t >= hi) s[x][i] = -INFINITY;
+      }
+  };
+  auto raise_max = [&]() {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
+    mx = max_x32(mx) * (I8 ? 1.f : sc);
+    const bool grow = mx > m + kSlack;
+    if (__builtin_expect(__ballot(grow) != 0, 0)) {
+      const float mn = grow ? mx : m;
+      const float alpha = grow ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
+      ls *= alpha;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= alpha;
+      m = mn;
+    }
+  };
+  u32x4 pw[2][PARTS];
+  auto weights = [&](int buf, int y, bool as_is) {  // of page y of the step: elements 8 (y % 2) .. of s[y / 2]
+    const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      float pv[4];
+      f32x4 vs = {1.f, 1.f, 1.f, 1.f};
+      if constexpr (I8) vs = *(const f32x4*)(s_vs[buf] + 16 * y + 8 * b + 4 * h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = s[y >> 1][8 * (y & 1) + 4 * b + i];
+        const float e = __builtin_amdgcn_exp2f(I8 ? x - mu : fmaf(x, sc, -mu));
+        ls = I8 && !as_is ? fmaf(e, vs[i], ls) : ls + e;
+        pv[i] = I8 && as_is ? e * vs[i] : e;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if constexpr (PARTS == 1) {
+          pw[y & 1][0][2 * b + i] = pk_bf16(pv[2 * i], pv[2 * i + 1]);
+        } else {
+          uint32_t s3[3];
+          split3(pv[2 * i], pv[2 * i + 1], s3);
+#pragma unroll
+          for (int z = 0; z < PARTS; ++z) pw[y & 1][z][2 * b + i] = s3[z];
+        }
+      }
+    }
+  };
+  auto product = [&](u32x4 v, int y, f32x16 acc) {
+#pragma unroll
+    for (int z = PARTS - 1; z >= 0; --z)
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pw[y & 1][z]), acc, 0, 0, 0);
+    return acc;
+  };
+  // What is rare (positions that not every column sees, a maximum that moves) stands in branches of its own
+  // that change the registers in place, and odd steps come after all others: so the loop keeps its
+  // accumulators where they are.
+  auto step = [&](int buf, int pg, bool odd) {
+    scores(buf, false);
+    if constexpr (PARTS == 1) {  // operands ahead of their products
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * NK; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+    if (__builtin_expect(odd || 16 * pg < flo || 16 * (pg + SP) > fhi, 0)) hide(pg, clo, odd ? 0 : chi);
+    raise_max();
+    const char* vb = s_v[buf] + (h * HD + lc) * 16;
+    weights(buf, 0, false);
+#pragma unroll
+    for (int y = 0; y < SP; ++y) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] = product(*(const u32x4*)(vb + y * PB + d * 512), y, o[d]);
+      if (y + 1 < SP) weights(buf, y + 1, false);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // A step with odd values, row by row as in the row kernel: V of the positions that the row does not see is
+  // zero (an integer page: their weights), and the row's columns take the result.
+  auto odd_step = [&](int buf, int pg) {
+    scores(buf, true);
+    hide(pg, clo, chi);
+    raise_max();
+    const char* vb = s_v[buf] + (h * HD + lc) * 16;
+#pragma unroll
+    for (int y = 0; y < SP; ++y) {
+      weights(buf, y, true);
+#pragma unroll 1
+      for (int r = row_a; r <= row_z; ++r) {
+        const int begin = first_key(r), end = min(end_key(r), 16 * s1);
+        u32x4 keep;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = 16 * (pg + y) + 8 * (j >> 2) + 4 * h + (j & 3);
+          const uint32_t k16 = t >= begin && t < end ? 0xffffu : 0u;
+          keep[j >> 1] = (j & 1) ? keep[j >> 1] | (k16 << 16) : k16;
+        }
+        if constexpr (I8)  // (a lane's own column decides; the others' results are not taken)
+#pragma unroll
+          for (int z = 0; z < PARTS; ++z)
+            if (row == r) pw[y & 1][z] &= keep;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const u32x4 v = *(const u32x4*)(vb + y * PB + d * 512);
+          const f32x16 t = product(I8 ? v : v & keep, y, o[d]);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] = row == r ? t[i] : o[d][i];
+        }
+      }
+    }
+  };
+  if (s0 < s1) {  // (workgroup-uniform)
+    fetch(s0);
+    stage(0, s0, false);
+    __syncthreads();
+    int buf = 0;
+    bool left = false;
+    for (int pg = s0; pg < s1; pg += SP, buf ^= 1) {
+      const bool more = pg + SP < s1, odd = is_odd(buf);
+      left |= odd;
+      if (more) fetch(pg + SP);
+      step(buf, pg, odd);
+      if (more) stage(buf ^ 1, pg + SP, false);
+      __syncthreads();
+    }
+    if (__builtin_expect(left, 0)) {
+#pragma unroll 1
+      for (int pg = s0; pg < s1; pg += SP) {
+        fetch(pg);
+        stage(0, pg, true);
+        __syncthreads();
+        if (is_odd(0)) odd_step(0, pg);
+        __syncthreads();
+      }
+    }
+  }
+  if (wc0 + lc >= ncol) return;
+  ls = sum_x32(ls);
+  if (sp.nsplit == 1) {
+    const float inv = ls == 0.f ? 0.f : 1.f / ls;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        st_out4<IT>(a, sp.row0 + row, head, 32 * d + 8 * b + 4 * h,
+                    f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * inv);
+    if (h == 0 && a.lse != nullptr)
+      a.lse[(size_t)(sp.row0 + row) * a.hq + head] = ls == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(ls)) * kLn2;
+  } else {
+    const size_t part = sp.part0 + ((size_t)row * a.hq + head) * sp.nsplit + split;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *(f32x4*)(a.part + part * HD + 32 * d + 8 * b + 4 * h) =
+            f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+    if (h == 0) *(float2*)(a.ml + part * 2) = make_float2(m, ls);
+  }
+}
+
 // ---------------------------------------------------------------------------------- the splits joined
 // o = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  A workgroup per (row, head): HD / 4 lanes read a
 // split's O with 16-byte loads, so that the workgroup's 4 waves take 8 (16 at head dim 64) splits at once,
@@ -552,6 +926,10 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
 template <class KT, class IT, int HD>
 static hipError_t launch_kind(int kind, const AttendArgs& a, hipStream_t s) {
   const dim3 grid(a.n_items * (unsigned)a.hkv), block(256);
+  if (kind == 2) {
+    if constexpr (sizeof(KT) <= 2) return launch_k(k_attend_tile<KT, IT, HD>, grid, dim3(512), s, a);
+    return hipErrorInvalidValue;
+  }
   if (kind == 0) return launch_k(k_attend_rows<KT, IT, HD, 1>, grid, block, s, a);
   return launch_k(k_attend_rows<KT, IT, HD, 2>, grid, block, s, a);
 }

@@ -7,12 +7,13 @@
 
 namespace laser {
 
-constexpr int kAttendKinds = 2;  // row kernel with 16 columns, with 32
+constexpr int kAttendKinds = 3;  // row kernel with 16 columns, with 32; tile kernel
+constexpr int kAttendFewCols = 64;
 
 // A span as the planner sees it, and what it decides.
 struct AttendSize {
   int n, pages;  // query rows; pages that any of them sees
-  int kind;      // AttendArgs' kernel
+  int kind;      // the kernel
   int tiles;     // query tiles
   int nsplit;    // workgroups over a tile's pages
 };
@@ -20,23 +21,32 @@ struct AttendSize {
 inline int attend_ceil(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Columns (rows x query heads of a kv head) of a tile of each kernel.
-inline int attend_cols(int kind) { return kind == 0 ? 16 : 32; }
+inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256; }
 
-// wide: 16-bit rows and at most 16-bit K and V, for which the 32-column row kernel fits its registers.
-// Splits: enough workgroups of 4 waves that every CU has two of them, a wave with at least 2 pages (they
-// are computed in pairs); a span of up to 32 pages stays whole, since joining splits is a launch of
-// its own.
-inline void plan_attend(AttendSize* s, int n, int group, int kv_heads, int cus, bool wide) {
-  int64_t work = 0;
+// es: bytes of a cached element; io16: 16-bit rows.  fp32 pools have only the row kernel with 16 columns,
+// and fp32 rows not the one with 32 (three parts of everything would not fit the registers).
+// Splits.  Row kernels: enough workgroups of 4 waves that every CU has two of them, a wave with at least 2
+// pages (they are computed in pairs); a span of up to 32 pages stays whole, since joining splits is a
+// launch of its own.  Tile kernel: one workgroup per CU, each with at least 16 pages.
+inline void plan_attend(AttendSize* s, int n, int group, int kv_heads, int cus, int es, bool io16) {
+  int64_t work = 0, wgs = 0;
   for (int i = 0; i < n; ++i) {
     const int64_t cols = (int64_t)s[i].n * group;
-    s[i].kind = cols <= 16 || !wide ? 0 : 1;
+    s[i].kind = es == 4 || cols <= 16 ? 0 : cols > kAttendFewCols ? 2 : io16 ? 1 : 0;
     s[i].tiles = attend_ceil(cols, attend_cols(s[i].kind));
-    work += (int64_t)s[i].pages * s[i].tiles * kv_heads;
+    if (s[i].kind == 2)
+      wgs += (int64_t)s[i].tiles * kv_heads;
+    else
+      work += (int64_t)s[i].pages * s[i].tiles * kv_heads;
   }
   const int run = std::max(2, attend_ceil(work, (int64_t)cus * 8));  // pages per wave
-  for (int i = 0; i < n; ++i)
-    s[i].nsplit = s[i].pages <= 32 ? 1 : std::min(128, attend_ceil(s[i].pages, 4 * run));
+  const int tile_splits = wgs > 0 ? std::max(1, attend_ceil(cus, wgs)) : 1;
+  for (int i = 0; i < n; ++i) {
+    if (s[i].kind == 2)
+      s[i].nsplit = std::max(1, std::min({128, tile_splits, s[i].pages / 16}));
+    else
+      s[i].nsplit = s[i].pages <= 32 ? 1 : std::min(128, attend_ceil(s[i].pages, 4 * run));
+  }
 }
 
 }  // namespace laser

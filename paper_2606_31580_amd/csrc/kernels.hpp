@@ -319,8 +319,7 @@ hipError_t launch_kv_rows(int kv_type, int io, int hd, KvRowsArgs& a, int n_laye
 // Attention of a caller's query rows over the paged cache (laser_attend).
 constexpr int kAttendSpans = 64;       // spans of one launch
 constexpr int kAttendMaxSplits = 128;  // workgroups over a span's keys, at most
-constexpr int kAttendRowCols = 16;     // columns of a query tile, row kernel (x 1 or 2)
-constexpr int kAttendTileCols = 256;   // columns of a query tile, tile kernel
+constexpr int kAttendTileCols = 256;  // columns of a tile of the tile kernel
 struct AttendSpan {
   int seq, row0, n, pos, kb, ke;  // rows row0 .. row0+n-1 at positions pos ..; keys kb .. ke-1
   int nsplit;                     // workgroups over the keys of a tile (1: the output directly)

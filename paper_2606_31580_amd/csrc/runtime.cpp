@@ -2377,7 +2377,7 @@ laser_status plan_attend_call(const laser_kv* kv, int n_spans, const laser_atten
     job.size.push_back(z);
   }
   const int G = d.n_q_heads / d.n_kv_heads;
-  plan_attend(job.size.data(), (int)job.size.size(), G, d.n_kv_heads, m->cus, io == LASER_DTYPE_BF16 && m->kv_es <= 2);
+  plan_attend(job.size.data(), (int)job.size.size(), G, d.n_kv_heads, m->cus, m->kv_es, io == LASER_DTYPE_BF16);
   for (size_t i = 0; i < job.sp.size(); ++i) {
     job.sp[i].nsplit = job.size[i].nsplit;
     if (job.size[i].nsplit > 1) {

@@ -38,7 +38,7 @@ def tolerance(io, ref, v, q, k, scale):
     their terms, 2^-24 hd scale max|q| max|k| sqrt(hd)-ish; four times the root-sum is taken, which moves every
     weight by that factor.  Sums over up to some thousand keys add 2^-24 sqrt(keys), inside the constant."""
     top = np.nanmax(np.abs(v)) if v.size else 1.0
-    terms = scale * np.abs(q).max() * np.abs(k).max() * math.sqrt(q.shape[-1]) if k.size else 0.0
+    terms = abs(scale) * np.abs(q).max() * np.abs(k).max() * math.sqrt(q.shape[-1]) if k.size else 0.0
     tol = (4 * 2.0 ** -24 * terms + 64 * 2.0 ** -24) * top
     if io == "bf16":
         tol += 2.0 ** -9 * top + 2.0 ** -8 * np.abs(ref)
@@ -297,3 +297,40 @@ def test_long_context():
     held = fill(kv, "int8", [n], hkv, hd, 26)
     q = queries(np.random.default_rng(27), 9, hq, hd, "f32")
     check(kv, "int8", "f32", held, [L.attend_span(0, 1, n - 1), L.attend_span(0, 8, n - 8, row0=1)], q)
+
+
+@pytest.mark.parametrize("kind,io", [("int8", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 0.9])
+def test_scales(kind, io, scale):
+    """A negative scale turns the order of the scores, a zero one weighs every seen key alike."""
+    hq, hkv, hd = 4, 2, 64
+    kv = cache(kind, hq, hkv, hd, pages=40, seqs=1, per_seq=40)
+    held = fill(kv, kind, [333], hkv, hd, 28)
+    q = queries(np.random.default_rng(29), 60, hq, hd, io)
+    check(kv, kind, io, held, [L.attend_span(0, 2, 331), L.attend_span(0, 50, 283, row0=5)], q, scale=scale)
+
+
+@pytest.mark.parametrize("n", [2, 70])
+def test_int8_scales_far_apart(n):
+    """Value rows of 2^-60 to 2^60, rows of zeros, beside ordinary ones: each weight counts once in the sum and once,
+    times its row's scale, in the output."""
+    hq, hkv, hd, length = 4, 2, 64, 300
+    kv = cache("int8", hq, hkv, hd, pages=40, seqs=1, per_seq=40)
+    rng = np.random.default_rng(30)
+    kv.add_seq(0, length)
+    k, v = (rng.standard_normal((length, hkv, hd)).astype(np.float32) for _ in range(2))
+    v[10] *= 2.0 ** 60
+    v[50:70] = 0.0
+    v[100:120] *= 2.0 ** -60
+    v[200] *= 2.0 ** -30
+    v[230] *= 2.0 ** 38
+    k, v = (torch.from_numpy(x).to(torch.bfloat16).cuda() for x in (k, v))
+    L.laser_kv_write(kv, 1, [L.kv_run(0, 0, length)], k, v)
+    held = [(kept("int8", f64(k)), kept("int8", f64(v)))]
+    q = queries(rng, n, hq, hd, "bf16")
+    # over all keys the largest row decides; over the keys behind it and in front of the next large one, the others do
+    check(kv, "int8", "bf16", held, [L.attend_span(0, n, length - n)], q)
+    check(kv, "int8", "bf16", [(held[0][0], np.where(np.arange(length)[:, None, None] < 230, held[0][1], 0))],
+          [L.attend_span(0, n, length - n, kv_begin=11, kv_end=229)], q)
+    o, _ = check(kv, "int8", "bf16", held, [L.attend_span(0, n, length - n, kv_begin=100, kv_end=120)], q)
+    assert float(o.float().abs().max()) > 2.0 ** -64  # (the small rows by themselves are not lost)
