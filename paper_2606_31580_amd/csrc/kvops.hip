@@ -52,6 +52,14 @@ struct RowScale {
   }
 };
 
+// Four values as E4M3 (to nearest even, saturated at +-448; NaN stays NaN).
+__device__ __forceinline__ uint32_t pk_fp8x4(const float* x) {
+  float c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c[i] = x[i] != x[i] ? x[i] : fminf(fmaxf(x[i], -448.f), 448.f);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false), true);
+}
+
 __device__ __forceinline__ uint16_t f2bf_any(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 
 // 8 elements of one position in the cache's type.
@@ -72,13 +80,14 @@ __device__ __forceinline__ Piece<KT> pack(const float* x, const RowScale* rs) {
   } else {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint32_t w = 0;
+      if constexpr (std::is_same_v<KT, fp8_t>) {
+        p.w[h] = pk_fp8x4(x + 4 * h);
+      } else {
+        uint32_t w = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t b = std::is_same_v<KT, fp8_t> ? f2fp8(x[4 * h + e]) : ((uint32_t)rs->quant(x[4 * h + e]) & 0xffu);
-        w |= b << (8 * e);
+        for (int e = 0; e < 4; ++e) w |= ((uint32_t)rs->quant(x[4 * h + e]) & 0xffu) << (8 * e);
+        p.w[h] = w;
       }
-      p.w[h] = w;
     }
   }
   return p;
@@ -176,7 +185,8 @@ __device__ __forceinline__ void st_row8(void* base, int64_t e, const float* x) {
 
 }  // namespace
 
-// grid (workgroups of all runs, layers, K and V), 256 threads: thread -> (4 positions, kv head, 8 dims).
+// grid (workgroups of all runs, layers, K and V), 256 threads: thread -> (page, kv head, 4 positions, 8 dims), so
+// that a wave writes whole page blocks.
 template <class KT, class IT, int LD8, bool WRITE, bool VEC>
 __global__ __launch_bounds__(256) void k_kv_rows(KvRowsArgs a) {
   constexpr int HD = 8 << LD8;
@@ -187,9 +197,9 @@ __global__ __launch_bounds__(256) void k_kv_rows(KvRowsArgs a) {
   const KvRun run = a.runs[ri];
   const unsigned idx = (blockIdx.x - run.first) * 256 + threadIdx.x;
   const int d8 = idx & ((1 << LD8) - 1);
-  const unsigned r = idx >> LD8, g = r / (unsigned)a.hkv;
+  const unsigned r = idx >> (LD8 + 2), g = r / (unsigned)a.hkv;
   const int kvh = (int)(r - g * a.hkv);
-  const int pos4 = (run.pos >> 2) + (int)g;                       // group of 4 positions
+  const int pos4 = 4 * ((run.pos >> 4) + (int)g) + ((idx >> LD8) & 3);  // group of 4 positions
   const int lo = max(run.pos - 4 * pos4, 0), hi = min(run.pos + run.n - 4 * pos4, 4);  // the run's part of it
   if (hi <= lo) return;  // (whole rows of lanes leave together)
   const bool is_v = blockIdx.z;
@@ -221,18 +231,25 @@ __global__ __launch_bounds__(256) void k_kv_rows(KvRowsArgs a) {
         p[j] = pack<KT>(x[j], nullptr);
       }
     }
-    if (!is_v) {
+    if (hi - lo == 4) {  // 32 elements: 8 e + j of a K block (dim j, position e), 4 e + j of a V block (position j, dim e)
+      uint32_t t[4 * Piece<KT>::W] = {};
+      if (!is_v) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < Piece<KT>::W; ++e) t[j * Piece<KT>::W + e] = p[j].w[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) put_e<KT>(t, 4 * e + j, get_e<KT>(p[j].w, e));
+      }
+#pragma unroll
+      for (int q = 0; q < Piece<KT>::W; ++q) *(u32x4*)(blk + 16 * q) = u32x4{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
+    } else if (!is_v) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (j >= lo && j < hi) st_words<KT>(blk + j * 8 * sizeof(KT), p[j].w);
-    } else if (hi - lo == 4) {  // element 4 e + j of the block's 32 is (position j, dim e)
-      uint32_t t[4 * Piece<KT>::W] = {};
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) put_e<KT>(t, 4 * e + j, get_e<KT>(p[j].w, e));
-#pragma unroll
-      for (int q = 0; q < 4; ++q) st_words<KT>(blk + q * 8 * sizeof(KT), t + q * Piece<KT>::W);
     } else {  // (the group's other positions keep what they hold)
       using E = std::conditional_t<sizeof(KT) == 1, uint8_t, std::conditional_t<sizeof(KT) == 2, uint16_t, uint32_t>>;
 #pragma unroll
@@ -244,7 +261,11 @@ __global__ __launch_bounds__(256) void k_kv_rows(KvRowsArgs a) {
   } else {
     uint32_t w[4 * Piece<KT>::W];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) ld_words<KT>(blk + q * 8 * sizeof(KT), w + q * Piece<KT>::W);
+    for (int q = 0; q < Piece<KT>::W; ++q) {
+      const u32x4 x = ld_global<u32x4>(blk + 16 * q);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[4 * q + i] = x[i];
+    }
     f32x4 s4 = {1.f, 1.f, 1.f, 1.f};
     if constexpr (std::is_same_v<KT, i8_t>) s4 = ld_global<f32x4>(sc);
 #pragma unroll
@@ -279,9 +300,9 @@ hipError_t launch_kv_rows(int kv_type, int io, int hd, KvRowsArgs& a, int n_laye
   for (int i = 0; i < a.n_runs; ++i) {
     KvRun& r = a.runs[i];
     if (r.n < 1) return hipErrorInvalidValue;
-    const unsigned groups = (unsigned)((r.pos + r.n + 3) / 4 - r.pos / 4);
+    const unsigned pages = (unsigned)((r.pos + r.n + kPage - 1) / kPage - r.pos / kPage);
     r.first = wgs;
-    wgs += (unsigned)(((uint64_t)groups * a.hkv * (hd / 8) + 255) / 256);
+    wgs += (unsigned)(((uint64_t)pages * a.hkv * (hd / 2) + 255) / 256);
   }
   const int es = io == 1 ? 2 : 4;
   auto on16 = [&](int64_t e) { return e * es % 16 == 0; };
