@@ -252,7 +252,7 @@ typedef struct {
    * LASER_DTYPE_INT8 (bf16 models only): the integers q = rint(127 x / amax) (ties to even) and
    * one fp32 scale s = amax / 127 per (layer, position, kv head) for K and one for V, amax the
    * largest magnitude of the head's vector; the cache stands for q s.  A vector with a NaN or an
-   * infinity reads back as NaN. */
+   * infinity reads back as NaN.  The pools of an INT8 cache are 16-byte aligned (UNSUPPORTED). */
   int kv_dtype;
 } laser_model_desc;
 
@@ -432,7 +432,7 @@ laser_status laser_decode_step(laser_model* m, laser_kv* kv, int batch, const in
  * statistics, K-share partials) lives in a static device array of 32 MiB per GPU, held from
  * the library's first use on that GPU until the process ends, instead of in the model's
  * workspace (but for the K-share partials of batches of 17 rows and more whose projections run
- * on fragments: those stay in the workspace).  The kernels are launched one by one (no graph is captured or instantiated), the
+ * on fragments, and the rows' K and V on their way into an INT8 cache: those stay in the workspace).  The kernels are launched one by one (no graph is captured or instantiated), the
  * host plan is built in a buffer the model allocated at finalize, and the arrival counters
  * are cleared by a kernel at every call (the array keeps the previous call's contents).
  * Calls that overlap on one GPU (any model, any stream) race on the array: order them.

@@ -50,6 +50,18 @@ def round_fp8_e4m3(x) -> np.ndarray:
     return np.clip(r, -E4M3_MAX, E4M3_MAX)
 
 
+def round_int8_rows(x) -> np.ndarray:
+    """The values that 8-bit integers with one scale per row stand for: a row is the last axis, its
+    scale the largest magnitude / 127, each element the nearest multiple of it, ties to even.
+
+    Returns float64 values.
+    """
+    x = np.asarray(x, dtype=np.float64)
+    top = np.max(np.abs(x), axis=-1, keepdims=True)
+    safe = np.where(top > 0, top, 1.0)
+    return np.where(top > 0, np.rint(127.0 * x / safe) * (top / 127.0), 0.0)
+
+
 def fp8_e4m3_bits_to_float(bits) -> np.ndarray:
     """Decode E4M3 bit patterns (uint8) to their values."""
     b = np.asarray(bits, dtype=np.uint8).astype(np.int64)

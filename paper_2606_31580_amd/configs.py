@@ -29,7 +29,7 @@ class ModelShape:
     dtype: str  # "bf16" or "f32": weight storage type (and the KV cache's unless kv_dtype is set)
     rope_theta: float
     rms_eps: float
-    kv_dtype: str = ""  # "" = dtype, or "fp8" (OCP E4M3 KV cache, bf16 models)
+    kv_dtype: str = ""  # "" = dtype, "fp8" (OCP E4M3 KV cache) or "int8" (scales per position and head): bf16 models
 
     @property
     def kv_storage(self) -> str:
@@ -50,8 +50,9 @@ class ModelShape:
         return es * (self.n_layers * per_layer + self.vocab * d + d)
 
     def kv_bytes_per_token(self) -> int:
-        es = {"fp8": 1, "bf16": 2}.get(self.kv_storage, 4)
-        return self.n_layers * 2 * self.n_kv_heads * self.head_dim * es
+        es = {"fp8": 1, "int8": 1, "bf16": 2}.get(self.kv_storage, 4)
+        scale = 4 if self.kv_storage == "int8" else 0
+        return self.n_layers * 2 * self.n_kv_heads * (self.head_dim * es + scale)
 
 
 @dataclass(frozen=True)
@@ -79,7 +80,13 @@ QWEN_1P5B_FP8KV = replace(QWEN_1P5B, name="qwen2-1.5B-shape-fp8kv", kv_dtype="fp
 QWEN_7B_FP8KV = replace(QWEN_7B, name="qwen2-7B-shape-fp8kv", kv_dtype="fp8")
 LLAMA_8B_FP8KV = replace(LLAMA_8B, name="llama-8B-shape-fp8kv", kv_dtype="fp8")
 
-SHAPES = {s.name: s for s in (TINY, QWEN_1P5B, QWEN_7B, LLAMA_8B, QWEN_1P5B_FP8KV, QWEN_7B_FP8KV, LLAMA_8B_FP8KV)}
+# and with an 8-bit integer KV cache
+QWEN_1P5B_INT8KV = replace(QWEN_1P5B, name="qwen2-1.5B-shape-int8kv", kv_dtype="int8")
+QWEN_7B_INT8KV = replace(QWEN_7B, name="qwen2-7B-shape-int8kv", kv_dtype="int8")
+LLAMA_8B_INT8KV = replace(LLAMA_8B, name="llama-8B-shape-int8kv", kv_dtype="int8")
+
+SHAPES = {s.name: s for s in (TINY, QWEN_1P5B, QWEN_7B, LLAMA_8B, QWEN_1P5B_FP8KV, QWEN_7B_FP8KV, LLAMA_8B_FP8KV,
+                             QWEN_1P5B_INT8KV, QWEN_7B_INT8KV, LLAMA_8B_INT8KV)}
 
 WORKLOADS = {
     w.name: w

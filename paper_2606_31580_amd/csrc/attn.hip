@@ -48,7 +48,9 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
   static_assert(RING || NT == 1, "two tiles: long runs");
   constexpr int OS = HD + 4;   // merge-slot row stride (floats; padded so that 16 rows fall in different bank groups)
   constexpr int PB = 16 * HD * (int)sizeof(KT);  // bytes of a page's K (or V) block
-  constexpr int RBYTES = 4 * PB;                 // a wave's two pages, K and V of each
+  constexpr bool I8 = std::is_same_v<KT, i8_t>;  // 8-bit integers, a scale per position
+  constexpr int SB = I8 ? 256 : 0;               // the two pages' scales: K (64 bytes) and V of each
+  constexpr int RBYTES = 4 * PB + SB;            // a wave's two pages, K and V of each
   constexpr int QS = HD + 8;                     // query row stride (bf16 elements; padded likewise), short runs
   constexpr int QB = RING ? NC * HD * 4 : 4 * NC * QS;  // the tile's queries: fp32, or bf16 hi rows, then lo rows
   constexpr int MB = NT * 3 * 16 * OS * 4;       // merge slots of waves 1-3 (after the pages)
@@ -150,12 +152,17 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
       copy_to_lds16<true>((const char*)a.kpool + blk + u * 1024, ring0 + slot * 2 * PB + u * 1024);
       copy_to_lds16<true>((const char*)a.vpool + blk + u * 1024, ring0 + slot * 2 * PB + PB + u * 1024);
     }
+    if constexpr (I8) {  // lanes 0-3 the page's K scales, 4-7 its V scales
+      const size_t sc = a.scales + ((layer_base + pid) * a.hkv + kvh) * 64 + 16 * (l & 3);
+      if (l < 8) copy_to_lds16<true>((const char*)(l < 4 ? a.kpool : a.vpool) + sc, ring0 + 4 * PB + slot * 128);
+    }
   };
   constexpr int KW = sizeof(KT) == 4 ? 2 : 1;  // 16-byte K reads per k-step (fp8: one 8-byte read)
   using KRaw = std::conditional_t<sizeof(KT) == 1, u32x2, u32x4>;
   using VRaw = std::conditional_t<sizeof(KT) == 1, uint32_t, std::conditional_t<sizeof(KT) == 2, u32x2, u32x4>>;
   KRaw kraw[2][NS][KW];
   VRaw vraw[2][ND];
+  f32x4 kscale[2], vscale[2];  // (I8) of positions 4 lg ..
   auto read_page = [&](auto bufc) {  // this lane's words of the page in a ring slot
     constexpr int buf = decltype(bufc)::value;
     const char* kb = ring + buf * 2 * PB;
@@ -166,6 +173,10 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
       for (int q = 0; q < KW; ++q) kraw[buf][s][q] = *(const KRaw*)(kb + (s * 512 + 8 * l) * sizeof(KT) + 16 * q);
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) vraw[buf][dt] = *(const VRaw*)(vb + (dt * 256 + 4 * l) * sizeof(KT));
+    if constexpr (I8) {
+      kscale[buf] = *(const f32x4*)(ring + 4 * PB + buf * 128 + 16 * lg);
+      vscale[buf] = *(const f32x4*)(ring + 4 * PB + buf * 128 + 64 + 16 * lg);
+    }
   };
   auto load_page = [&](int pid, auto bufc) {  // the same words straight from memory
     constexpr int buf = decltype(bufc)::value;
@@ -180,6 +191,11 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
       vraw[buf][dt] = __builtin_nontemporal_load((global_ptr<VRaw>)(vb + (dt * 256 + 4 * l) * sizeof(KT)));
+    if constexpr (I8) {
+      const size_t sc = a.scales + ((layer_base + pid) * a.hkv + kvh) * 64 + 16 * lg;
+      kscale[buf] = ld_global<f32x4>((const char*)a.kpool + sc);
+      vscale[buf] = ld_global<f32x4>((const char*)a.vpool + sc);
+    }
   };
   // MFMA operands of one page.  K: lane l holds K[t = l%16][d = 32s + 8(l/16) + j];
   // V^T: V[t = 4(l/16) + j][d = 16dt + l%16].  Slots past the group's last position hold no
@@ -191,18 +207,24 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
   };
   auto unpack = [&](int pg, auto cbc, PageOps& P) {
     constexpr int cb = decltype(cbc)::value;
-    if constexpr (sizeof(KT) == 1) {  // E4M3 -> bf16 is exact: no lo part
+    if constexpr (sizeof(KT) == 1) {  // E4M3 and integers -> bf16 is exact: no lo part
+      auto to_bf16 = [](uint32_t w, uint32_t& lo, uint32_t& hi) {
+        if constexpr (I8)
+          i8x4_to_bf16x4(w, lo, hi);
+        else
+          fp8x4_to_bf16x4(w, lo, hi);
+      };
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         uint32_t w0, w1, w2, w3;
-        fp8x4_to_bf16x4(kraw[cb][s][0][0], w0, w1);
-        fp8x4_to_bf16x4(kraw[cb][s][0][1], w2, w3);
+        to_bf16(kraw[cb][s][0][0], w0, w1);
+        to_bf16(kraw[cb][s][0][1], w2, w3);
         P.khi[s] = __builtin_bit_cast(bf16x8, u32x4{w0, w1, w2, w3});
       }
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) {
         uint32_t w0, w1;
-        fp8x4_to_bf16x4(vraw[cb][dt], w0, w1);
+        to_bf16(vraw[cb][dt], w0, w1);
         P.vhi[dt] = __builtin_bit_cast(s16x4, u32x2{w0, w1});
       }
     } else if constexpr (sizeof(KT) == 2) {
@@ -242,7 +264,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
         P.vlo[dt] = l4;
       }
     }
-    if (pg * 16 + 15 > wi.maxpos) {
+    if (!I8 && pg * 16 + 15 > wi.maxpos) {  // (integers are finite, and their scales are only applied where seen)
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
@@ -357,8 +379,9 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int ta = pgA * 16 + 4 * lg + i, tb = pgB * 16 + 4 * lg + i;
-        sv[i] = (ta <= cpos[u]) ? sa[i] * a.scale_log2 : -INFINITY;
-        sv[4 + i] = (hasB && tb <= cpos[u]) ? sb[i] * a.scale_log2 : -INFINITY;
+        const float ka = I8 ? kscale[ca][i] * a.scale_log2 : a.scale_log2, kb = I8 ? kscale[cbB][i] * a.scale_log2 : a.scale_log2;
+        sv[i] = (ta <= cpos[u]) ? sa[i] * ka : -INFINITY;
+        sv[4 + i] = (hasB && tb <= cpos[u]) ? sb[i] * kb : -INFINITY;
         mloc = fmaxf(mloc, fmaxf(sv[i], sv[4 + i]));
       }
       mloc = max_x16(mloc);
@@ -372,6 +395,8 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
       for (int i = 0; i < 8; ++i) {
         pv[i] = (sv[i] == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(sv[i] - m_new);
         ls += pv[i];
+        if constexpr (I8)
+          if (sv[i] != -INFINITY) pv[i] *= i < 4 ? vscale[ca][i & 3] : vscale[cbB][i & 3];
       }
       ls = sum_x16(ls);
       ls = sum_x32(ls);
@@ -666,7 +691,10 @@ static hipError_t launch_hd(const AttnArgs& a, dim3 grid, hipStream_t s) {
 }
 
 hipError_t launch_attn(int dtype, int hd, const AttnArgs& a, dim3 grid, hipStream_t s) {
-  if (dtype == 2) {
+  if (dtype == 3) {
+    if (hd == 128) return launch_hd<i8_t, 128>(a, grid, s);
+    if (hd == 64) return launch_hd<i8_t, 64>(a, grid, s);
+  } else if (dtype == 2) {
     if (hd == 128) return launch_hd<fp8_t, 128>(a, grid, s);
     if (hd == 64) return launch_hd<fp8_t, 64>(a, grid, s);
   } else if (dtype == 1) {

@@ -176,6 +176,10 @@ __device__ __forceinline__ void epi_apply(const GemmArgs& a, int g, const EpiIte
       float* qo = a.q_out + ((size_t)it.m * a.hq + q.hh) * a.hd;
       qo[dlo] = ylo;
       qo[dhi] = yhi;
+    } else if (a.kv_rows != nullptr) {
+      float* r = a.kv_rows + ((size_t)(2 * it.m + (q.isk ? 0 : 1)) * a.hkv + q.hh) * a.hd;
+      r[dlo] = ylo;
+      r[dhi] = yhi;
     } else {
       const int t = it.pos & 15;
       const size_t blk = (((size_t)a.layer * a.num_pages + it.page) * a.hkv + q.hh) * (size_t)(16 * a.hd);
@@ -1305,6 +1309,10 @@ __global__ __launch_bounds__(256) void k_qkv_slices_epi(GemmArgs a, const float*
       float* qo = a.q_out + ((size_t)m * a.hq + q.hh) * a.hd;
       qo[dlo] = ylo;
       qo[dhi] = yhi;
+    } else if (a.kv_rows != nullptr) {
+      float* r = a.kv_rows + ((size_t)(2 * m + (q.isk ? 0 : 1)) * a.hkv + q.hh) * a.hd;
+      r[dlo] = ylo;
+      r[dhi] = yhi;
     } else {
       const int t = rd.pos & 15;
       const size_t blk = (((size_t)a.layer * a.num_pages + page) * a.hkv + q.hh) * (size_t)(16 * a.hd);

@@ -138,6 +138,7 @@ struct GemmArgs {
   const int* bt;
   int max_pps, num_pages, layer;
   int kv_fp8;  // K/V stored as E4M3 (else in the weight type)
+  float* kv_rows;  // INT8 cache: K and V of the rows go here, [M][K, V][hkv][hd], for launch_kv_quant
   // EPI_RESID
   float* h;  // [M][N]
   // MFMA path, EPI_RESID only: K split across `ksplit` workgroups per row group (1: none).
@@ -178,6 +179,7 @@ struct AttnArgs {
   int ring;       // workspace and pools are 16-byte aligned: long runs through the LDS rings
   int tiles;      // query tiles per item (1; 2 where a group has more than 16 columns)
   char* ofrag;  // the output as fragments for the O-projection (null: fp32 rows in o)
+  size_t scales;  // INT8 pools: byte offset of the scales
   uint32_t part_bytes, ml_bytes;
   unsigned* cnt;  // fused groups' arrival counters [hkv][kMaxGroups] x kAttnCntStride; zero between kernels
 };
@@ -261,7 +263,7 @@ hipError_t launch_resid_norm(float* h, const float* kpart, int ksplit, int M, in
 // Writes the tile-order copy of one projection's weights (the MFMA path's 16-row groups of
 // `a`, as weight_row maps them) to dst: a.n_groups groups x ceil(K/32) steps.
 hipError_t launch_tile_weights(int dtype, int epi, const GemmArgs& a, char* dst, hipStream_t s);
-// dtype: the KV element type, 0 fp32, 1 bf16, 2 fp8 (E4M3).
+// dtype: the KV element type, 0 fp32, 1 bf16, 2 fp8 (E4M3), 3 INT8.
 hipError_t launch_attn(int dtype, int hd, const AttnArgs& a, dim3 grid, hipStream_t s);
 hipError_t launch_attn_merge(const AttnArgs& a, int M, int hd, int nslots, hipStream_t s);  // nslots >= every group's nwg
 hipError_t launch_lm_reduce(const Plan* plan, const LmPart* part, int n_groups, int n_out, hipStream_t s);
@@ -315,6 +317,10 @@ struct KvRowsArgs {
 };
 // kv_type: 0 fp32, 1 bf16, 2 E4M3, 3 INT8 (the cache); io: 0 fp32, 1 bf16 (the rows).
 hipError_t launch_kv_rows(int kv_type, int io, int hd, KvRowsArgs& a, int n_layers, bool write, hipStream_t s);
+
+// A forward's new rows (GemmArgs::kv_rows) into an INT8 cache at their positions.
+hipError_t launch_kv_quant(const Plan* plan, int M, const float* rows, void* kpool, void* vpool, size_t scales, const int* bt,
+                           int max_pps, int num_pages, int layer, int hkv, int hd, hipStream_t s);
 
 // Attention of a caller's query rows over the paged cache (laser_attend).
 constexpr int kAttendSpans = 64;       // spans of one launch

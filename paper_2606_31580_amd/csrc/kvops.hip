@@ -284,6 +284,46 @@ __global__ __launch_bounds__(256) void k_kv_rows(KvRowsArgs a) {
   }
 }
 
+// A forward's rows: grid (rows, heads of K and of V), thread d8 of a head takes 8 dims.  Its two dependent reads
+// (page id, row) and scattered stores of a few KB are latency: 7B decode step, batch 1, see the launch.
+template <int LD8>
+__global__ __launch_bounds__(256) void k_kv_quant(const Plan* plan, const float* rows, void* kpool, void* vpool, size_t scales,
+                                                  const int* bt, int max_pps, int num_pages, int layer, int hkv) {
+  constexpr int HD = 8 << LD8;
+  const int m = blockIdx.x, idx = blockIdx.y * 256 + threadIdx.x;
+  const int d8 = idx & ((1 << LD8) - 1), kh = idx >> LD8;  // kh: K heads, then V heads
+  if (kh >= 2 * hkv) return;  // (whole rows of lanes leave together)
+  float x[8];
+  ld_row8<float, true>(rows, ((int64_t)m * 2 * hkv + kh) * HD + 8 * d8, x);
+  const RowDesc rd = row_desc(plan, m);
+  const int page = bt[(size_t)rd.seq * max_pps + (rd.pos >> 4)], t = rd.pos & 15;
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  const RowScale rs(row_umax<LD8>(top));
+  const Piece<i8_t> p = pack<i8_t>(x, &rs);
+  const bool is_v = kh >= hkv;
+  char* pool = (char*)(is_v ? vpool : kpool);
+  const size_t slot = ((size_t)layer * num_pages + page) * hkv + (is_v ? kh - hkv : kh);
+  char* blk = pool + slot * (16 * HD) + (is_v ? v_block_off(t, 8 * d8) : k_block_off(t, 8 * d8));
+  if (is_v) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) blk[4 * e] = (char)get_e<i8_t>(p.w, e);
+  } else {
+    st_words<i8_t>(blk, p.w);
+  }
+  if (d8 == 0) ((float*)(pool + scales))[slot * 16 + t] = rs.scale;
+}
+
+hipError_t launch_kv_quant(const Plan* plan, int M, const float* rows, void* kpool, void* vpool, size_t scales, const int* bt,
+                           int max_pps, int num_pages, int layer, int hkv, int hd, hipStream_t s) {
+  if (M < 1 || (hd != 64 && hd != 128)) return hipErrorInvalidValue;
+  const dim3 grid(M, (2 * hkv * (hd / 8) + 255) / 256), block(256);
+  if (hd == 128)
+    return launch_k(k_kv_quant<4>, grid, block, s, plan, rows, kpool, vpool, scales, bt, max_pps, num_pages, layer, hkv);
+  return launch_k(k_kv_quant<3>, grid, block, s, plan, rows, kpool, vpool, scales, bt, max_pps, num_pages, layer, hkv);
+}
+
 template <class KT, class IT, int LD8>
 static hipError_t launch_rows(const KvRowsArgs& a, bool write, bool vec, dim3 grid, hipStream_t s) {
   const dim3 block(256);

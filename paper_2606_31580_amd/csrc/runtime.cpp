@@ -98,6 +98,7 @@ constexpr size_t kMergeMinOBytes = (size_t)16 << 20;
 struct Layout {
   size_t xfrag, row_scale;  // the fragment path's gain times h, the rows' 1 / rms
   int frag_rows;  // rows the fragment path's buffers hold (0: it is not used)
+  size_t kv_rows;  // INT8 caches: the rows' K and V before they are quantised
   size_t rope, h, q, o, act, kpart, kcnt, mcnt, qpart, sqpart, lm_part, attn_part, attn_ml, attn_cnt, plans, probe_p, tok_buf,
       p_buf, total;
   size_t attn_part_bytes, attn_ml_bytes, attn_cnt_bytes, kcnt_bytes, mcnt_bytes;
@@ -488,6 +489,7 @@ static Layout make_layout(const laser_model_desc& d, int max_rows, bool wide = t
   L.q = take(rows * d.n_q_heads * hd * 4);
   L.o = take(rows * d.n_q_heads * hd * 4);
   L.act = take(rows * d.d_ffn * 4);
+  if (d.kv_dtype == LASER_DTYPE_INT8) L.kv_rows = take(rows * 2 * d.n_kv_heads * hd * 4);
   if (L.frag_rows) {
     L.xfrag = take(rows * d.d_model * 4);
     L.row_scale = take(rows * 4);
@@ -842,6 +844,8 @@ extern "C" laser_status laser_model_destroy(laser_model* m) {
 
 // ----------------------------------------------------------------------------- KV cache
 
+// The cache's element type as the kernels name it.
+static int kv_type_of(const laser_model* m) { return m->kv_i8 ? 3 : m->kv_fp8 ? 2 : m->es == 2 ? 1 : 0; }
 // Blocks of a pool, and where an INT8 pool's scales start: behind all blocks.
 static size_t kv_slots(const laser_model* m, int num_pages) {
   return (size_t)m->desc.n_layers * num_pages * m->desc.n_kv_heads;
@@ -865,6 +869,8 @@ extern "C" laser_status laser_kv_create(const laser_model* m, int num_pages, int
     return laser_fail(LASER_ERR_INVALID_ARG, "sizes must be positive");
   if ((long long)max_pages_per_seq * kPage > m->desc.max_positions + kPage)
     return laser_fail(LASER_ERR_INVALID_ARG, "max_pages_per_seq exceeds max_positions");
+  if (m->kv_i8 && (!aligned16(d_k_pool) || !aligned16(d_v_pool)))
+    return laser_fail(LASER_ERR_UNSUPPORTED, "the pools of an INT8 cache have to be 16-byte aligned");
   laser_kv* kv = new (std::nothrow) laser_kv(m, num_pages, max_seqs, max_pages_per_seq, d_k_pool, d_v_pool, d_block_table);
   if (!kv) return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
   handle_add(kv);
@@ -1483,6 +1489,7 @@ static laser_status launch_forward(laser_model* m, laser_kv* kv, const FwdKey& k
   base.max_pps = max_pps;
   base.num_pages = kv->pool.num_pages();
   base.kv_fp8 = m->kv_fp8;
+  base.kv_rows = m->kv_i8 ? m->wsp<float>(L.kv_rows) : nullptr;
   base.h = h;
   base.act = m->wsp<float>(L.act);
   base.F = d.d_ffn;
@@ -1577,6 +1584,7 @@ static laser_status launch_forward(laser_model* m, laser_kv* kv, const FwdKey& k
   aa.ring = attn_ring(m, kv);
   aa.tiles = key.attn_tiles;
   aa.ofrag = key.frag ? m->wsp<char>(L.o) : nullptr;
+  aa.scales = kv_scales_offset(m, kv->pool.num_pages());
   aa.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)hd));
   aa.part = sc.attn_part;
   aa.ml = sc.attn_ml;
@@ -1603,10 +1611,15 @@ static laser_status launch_forward(laser_model* m, laser_kv* kv, const FwdKey& k
     st = key.frag ? frag_gemm(LASER_K_QKV, EPI_QKV, a, sc.xfrag, d.d_model, nqkv, nqkv / 16, T ? T->qkv : nullptr, nullptr)
                   : gemm(LASER_K_QKV, EPI_QKV, a, d.d_model, nqkv, nqkv, key.M, T ? T->qkv : nullptr);
     if (st != LASER_OK) return st;
+    if (m->kv_i8)
+      HIP_TRY(timed(m, LASER_K_OTHER, s, [&] {
+        return launch_kv_quant(dp, key.M, base.kv_rows, kv->kpool, kv->vpool, aa.scales, kv->bt, max_pps, aa.num_pages, li,
+                               d.n_kv_heads, hd, s);
+      }));
 
     aa.layer = li;
     HIP_TRY(timed(m, LASER_K_ATTN, s, [&] {
-      hipError_t e = launch_attn(m->kv_fp8 ? 2 : dt, hd, aa, agrid, s);
+      hipError_t e = launch_attn(kv_type_of(m), hd, aa, agrid, s);
       if (e == hipSuccess && key.merge && !key.mo) e = launch_attn_merge(aa, key.M, hd, key.mslots, s);
       return e;
     }));
@@ -1691,7 +1704,6 @@ static laser_status check_ready(laser_model* m, laser_kv* kv) {
   if (!m->finalized) return laser_fail(LASER_ERR_STATE, "model not finalized");
   if (!kv_of(kv)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed kv");
   if (kv->m != m) return laser_fail(LASER_ERR_INVALID_ARG, "kv cache belongs to another model");
-  if (m->kv_i8) return laser_fail(LASER_ERR_UNSUPPORTED, "forwards over an INT8 cache");
   return LASER_OK;
 }
 
@@ -1720,7 +1732,6 @@ static void push_updates(Plan& p, const std::vector<PageUpdate>& u) {
 
 }  // namespace
 
-static int kv_type_of(const laser_model* m) { return m->kv_i8 ? 3 : m->kv_fp8 ? 2 : m->es == 2 ? 1 : 0; }
 
 static KvRowsArgs kv_rows_args(const laser_kv* kv, int layer) {
   KvRowsArgs a{};
@@ -1741,8 +1752,6 @@ static laser_status kv_dense(laser_kv* kv, int seq, void* d_k, void* d_v, bool w
   const laser_model_desc& d = m->desc;
   const int len = kv->pool.len(seq);
   if (len == 0) return LASER_OK;
-  if (!aligned16(kv->kpool) || !aligned16(kv->vpool))
-    return laser_fail(LASER_ERR_UNSUPPORTED, "the KV pools are not 16-byte aligned");
   if ((uintptr_t)d_k % 2 || (uintptr_t)d_v % 2) return laser_fail(LASER_ERR_INVALID_ARG, "elements are not aligned");
   KvRowsArgs a = kv_rows_args(kv, 0);
   a.k = d_k;

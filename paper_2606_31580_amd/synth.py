@@ -46,7 +46,7 @@ def _tdtype(shape: ModelShape) -> torch.dtype:
 def _kv_tdtype(shape: ModelShape) -> torch.dtype:
     if shape.kv_storage == "fp8":
         return torch.float8_e4m3fn
-    return _tdtype(shape)
+    return _tdtype(shape)  # (an int8 cache takes rows of the weights' type and quantises them)
 
 
 def tensor_specs(shape: ModelShape) -> List[tuple]:

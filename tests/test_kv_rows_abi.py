@@ -49,6 +49,12 @@ def test_int8_needs_bf16_weights():
     assert _code("laser_model_create", C.byref(desc), C.byref(m)) == L.ERR_INVALID_ARG
 
 
+def test_int8_pools_are_aligned():
+    with pytest.raises(L.LaserError, match="16-byte aligned") as e:
+        _kv(pool=PTR + 8)
+    assert e.value.code == L.ERR_UNSUPPORTED
+
+
 def test_append_and_truncate():
     _, kv = _kv(pages=6)
     L._call("laser_kv_add_seq", kv, 0, 15)
@@ -121,7 +127,7 @@ def test_rows_refusals(fn):
         refused(L.ERR_INVALID_ARG, k=_rows(64, 2, row=0))
         refused(L.ERR_STATE, k=_rows(64, 2, row=64, head=64 * 64))
     assert _write(None, ok, good, good, fn=fn) == L.ERR_STATE
-    _, odd = _kv(pool=PTR + 8)
+    _, odd = _kv("bf16", pool=PTR + 8)
     L._call("laser_kv_add_seq", odd, 0, 40)
     assert _write(odd, ok, good, good, fn=fn) == L.ERR_UNSUPPORTED
 
