@@ -22,6 +22,8 @@
 // (whatever the scale), and where the stored V itself can be infinite or NaN, pages that not every
 // column sees whole are looked through and, if one has such a value, taken row by row with the
 // unseen positions' V zeroed.
+#include <cstddef>
+
 #include "device_common.hpp"
 #include "kernels.hpp"
 
@@ -52,11 +54,21 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t* p) {
   }
 }
 
-// The span of a work item (spans are listed by their first item).
-__device__ __forceinline__ int find_span(const AttendArgs& a, unsigned item) {
+// The span of a work item (spans are listed by their first item), read from the argument segment itself: an
+// index into an argument would have the compiler copy all of it to scratch.  With one span its fields come in the
+// first round of loads.
+__device__ __forceinline__ AttendSpan item_span(int n_spans, unsigned item) {
+  using Words = const __attribute__((address_space(4))) int;
+  Words* sp = (Words*)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(AttendArgs, sp));
+  constexpr int W = sizeof(AttendSpan) / 4;
+  static_assert(sizeof(AttendSpan) == 36 && offsetof(AttendSpan, first) == 32, "read as words");
+  auto get = [](Words* p) {
+    return AttendSpan{p[0], p[1], p[2], p[3], p[4], p[5], p[6], (unsigned)p[7], (unsigned)p[8]};
+  };
+  if (n_spans == 1) return get(sp);
   const int lane = threadIdx.x & 63;
-  const unsigned first = lane < a.n_spans ? a.sp[lane].first : 0xffffffffu;
-  return __builtin_popcountll(__ballot(first <= item)) - 1;
+  const unsigned first = lane < n_spans ? (unsigned)sp[lane * W + 8] : 0xffffffffu;
+  return get(sp + W * __builtin_amdgcn_readfirstlane(__builtin_popcountll(__ballot(first <= item)) - 1));
 }
 
 // Four output dims of a row, in the rows' type.
@@ -148,7 +160,7 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
 
   const unsigned item = blockIdx.x / (unsigned)a.hkv;
   const int kvh = (int)(blockIdx.x - item * a.hkv);
-  const AttendSpan sp = a.sp[__builtin_amdgcn_readfirstlane(find_span(a, item))];
+  const AttendSpan sp = item_span(a.n_spans, item);
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
   const int lc = l & 15, lg = l >> 4;
   const int ncol = sp.n * a.G, tiles = (ncol + NC - 1) / NC;
@@ -202,10 +214,13 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
     f32x4 ks[2], vs[2];
   };
   Pair buf[2];
+  int ids = 0;  // lane i: page p0 + i of the run (then the next 64)
   auto load = [&](Pair& b, int pg) {
+    const int at = (pg - p0) & 63;
+    if (at == 0) ids = bt[min(pg + l, p1 - 1)];  // (past the run: its last page again)
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int pid = ld_const<int>(bt + min(pg + x, p1 - 1));  // (past the run: its last page again)
+      const int pid = __builtin_amdgcn_readlane(ids, at + x);
       const size_t slot = ((size_t)a.layer * a.num_pages + pid) * a.hkv + kvh;
       const char* kb = (const char*)a.kpool + slot * (16 * HD * ES);
       const char* vb = (const char*)a.vpool + slot * (16 * HD * ES);
@@ -510,7 +525,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
 
   const unsigned item = blockIdx.x / (unsigned)a.hkv;
   const int kvh = (int)(blockIdx.x - item * a.hkv);
-  const AttendSpan sp = a.sp[__builtin_amdgcn_readfirstlane(find_span(a, item))];
+  const AttendSpan sp = item_span(a.n_spans, item);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   const int lc = l & 31, h = l >> 5;
   const int ncol = sp.n * a.G, tiles = (ncol + kAttendTileCols - 1) / kAttendTileCols;
@@ -861,7 +876,7 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
   __shared__ __align__(16) float s_o[4][HD];
   __shared__ float s_m[4], s_l[4];
   const unsigned item = blockIdx.x;
-  const AttendSpan sp = a.sp[__builtin_amdgcn_readfirstlane(find_span(a, item))];
+  const AttendSpan sp = item_span(a.n_spans, item);
   const unsigned local = item - sp.first;
   const int r = (int)(local / (unsigned)a.hq), h = (int)(local - (unsigned)r * a.hq);
   const size_t part = sp.part0 + (size_t)local * sp.nsplit;

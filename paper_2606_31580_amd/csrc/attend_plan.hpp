@@ -25,9 +25,17 @@ inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256;
 
 // es: bytes of a cached element; io16: 16-bit rows.  fp32 pools have only the row kernel with 16 columns,
 // and fp32 rows not the one with 32 (three parts of everything would not fit the registers).
-// Splits.  Row kernels: enough workgroups of 4 waves that every CU has two of them, a wave with at least 2
-// pages (they are computed in pairs); a span of up to 32 pages stays whole, since joining splits is a
-// launch of its own.  Tile kernel: one workgroup per CU, each with at least 16 pages.
+//
+// Row kernels: pages per wave.  Every CU runs one workgroup of 4 waves, or two on 8-bit pools (fewer
+// registers).  Long runs stream best when two workgroups per CU share the pages; where that leaves a wave only
+// a few pages, one per CU with twice the pages has fewer splits to join and, on wider pools, no second
+// round (us, two and one per CU: 7B heads, 4 sequences of 3,000-14,000, bf16 pool, 4 pages a wave 23.9 and 19.4; 8B
+// heads, 8 sequences, 17 pages 50.5 and 60.8; INT8, 16 sequences of 100-2,000, 2 pages 13.4 and 11.5; 6 of
+// 3,000-9,000, 9 pages 20.5 and 26.6).  Runs end at 32 pages: more rounds even out ragged lengths (64 sequences of
+// 3,000-14,000: 219 us with runs of 133 pages, 192 with 33).
+// A span of up to 32 pages stays whole, since joining splits is a launch of its own, up to 64 where there
+// are spans enough to fill the CUs (64 sequences of 50-600 positions: 18.2 us split, 14.4 whole).
+// Tile kernel: one workgroup per CU, each with at least 16 pages.
 inline void plan_attend(AttendSize* s, int n, int group, int kv_heads, int cus, int es, bool io16) {
   int64_t work = 0, wgs = 0;
   for (int i = 0; i < n; ++i) {
@@ -39,13 +47,15 @@ inline void plan_attend(AttendSize* s, int n, int group, int kv_heads, int cus, 
     else
       work += (int64_t)s[i].pages * s[i].tiles * kv_heads;
   }
-  const int run = std::max(2, attend_ceil(work, (int64_t)cus * 8));  // pages per wave
+  const int two = attend_ceil(work, (int64_t)cus * 8);  // pages per wave, two workgroups per CU
+  const int run = two <= (es == 1 ? 4 : 8) ? std::max(2, attend_ceil(work, (int64_t)cus * 4)) : std::min(two, 32);
+  const int whole = two >= 4 ? 64 : 32;
   const int tile_splits = wgs > 0 ? std::max(1, attend_ceil(cus, wgs)) : 1;
   for (int i = 0; i < n; ++i) {
     if (s[i].kind == 2)
       s[i].nsplit = std::max(1, std::min({128, tile_splits, s[i].pages / 16}));
     else
-      s[i].nsplit = s[i].pages <= 32 ? 1 : std::min(128, attend_ceil(s[i].pages, 4 * run));
+      s[i].nsplit = s[i].pages <= whole ? 1 : std::min(128, attend_ceil(s[i].pages, 4 * run));
   }
 }
 
