@@ -33,22 +33,38 @@ __device__ __forceinline__ uint32_t row_umax(uint32_t v) {
 // A row's scale, and what its elements are multiplied by and divided by: rows far from 1 are moved by a
 // power of two first, so that neither 127 x nor 1 / amax leaves the normal range.
 struct RowScale {
-  float scale, pre, top, inv;
+  float scale, pre, top, inv, off0;
   __device__ __forceinline__ explicit RowScale(uint32_t amax_bits) {
     const float amax = __uint_as_float(amax_bits);
     const float c = amax > 0x1p100f ? 0x1p-32f : (amax < 0x1p-60f ? 0x1p64f : 1.f);
     scale = amax_bits >= 0x7f800000u ? amax : amax / 127.f;
     pre = 127.f * c;
     top = amax * c;
-    inv = amax_bits >= 0x7f800000u || amax == 0.f ? 0.f : __builtin_amdgcn_rcpf(top);
+    const bool small = amax < 0x1p-100f;  // (127 / amax may leave the range: divided)
+    inv = amax_bits >= 0x7f800000u || amax == 0.f ? 0.f : small ? 1.f : pre * __builtin_amdgcn_rcpf(top);
+    off0 = small ? 1.f : 0.f;
   }
-  // rint(127 x / amax).  The product with 1 / amax is off by less than 2^-14 steps; only next to half a
-  // step does that matter, and there the division decides.
-  __device__ __forceinline__ int quant(float x) const {
-    const float y = x * pre;
-    float r = y * inv, q = rintf(r);
-    if (fabsf(r - q) > 0.4999f) q = rintf(y / top);
-    return inv == 0.f ? 0 : (int)fminf(fmaxf(q, -127.f), 127.f);
+  // rint(127 x / amax) of 8 elements, packed.  The products with 127 / amax are off by less than 2^-14 steps;
+  // only next to half a step does that matter, and then the division decides.
+  __device__ __forceinline__ void quant8(const float* x, uint32_t* w) const {
+    float q[8], off = off0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float r = x[e] * inv;
+      q[e] = rintf(r);
+      off = fmaxf(off, fabsf(r - q[e]));
+    }
+    if (off > 0.4999f)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[e] = rintf(x[e] * pre / top);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t b[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b[e] = (uint32_t)(int)fminf(fmaxf(q[4 * h + e], -127.f), 127.f);
+      const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
+      w[h] = inv == 0.f ? 0u : lo | hi;
+    }
   }
 };
 
@@ -78,16 +94,11 @@ __device__ __forceinline__ Piece<KT> pack(const float* x, const RowScale* rs) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) p.w[e] = (uint32_t)f2bf_any(x[2 * e]) | ((uint32_t)f2bf_any(x[2 * e + 1]) << 16);
   } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if constexpr (std::is_same_v<KT, fp8_t>) {
-        p.w[h] = pk_fp8x4(x + 4 * h);
-      } else {
-        uint32_t w = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w |= ((uint32_t)rs->quant(x[4 * h + e]) & 0xffu) << (8 * e);
-        p.w[h] = w;
-      }
+    if constexpr (std::is_same_v<KT, fp8_t>) {
+      p.w[0] = pk_fp8x4(x);
+      p.w[1] = pk_fp8x4(x + 4);
+    } else {
+      rs->quant8(x, p.w);
     }
   }
   return p;
