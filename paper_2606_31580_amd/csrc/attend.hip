@@ -147,6 +147,10 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // one of a pair is infi
 // pages; each of its 4 waves walks a run of pages by itself, straight from memory into operands (the
 // page layout makes every load contiguous), two pages ahead of the pair that it computes; no barrier
 // until the waves' (m, l, O) are joined in LDS.
+// INT8, 8B heads, 64 sequences of 3,000-14,000 positions: 195 us, 5.9 TB/s (a copy reaches 5.07); 7B heads, one
+// sequence of 14,336: 10.2 us with the join, mostly latency: a round of loads each for the arguments, the queries
+// and the first pages, some 1 us per pair of pages, the join's launch.  Workgroups of 8 waves were slower
+// at every size measured (12.1 and 208 us there), and so was a third pair in flight.
 template <class KT, class IT, int HD, int NT>
 __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
   constexpr int PARTS = std::is_same_v<IT, float> ? 3 : 1;    // of a query or weight
@@ -214,13 +218,18 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
     f32x4 ks[2], vs[2];
   };
   Pair buf[2];
-  int ids = 0;  // lane i: page p0 + i of the run (then the next 64)
+  // The next pair's page ids, through the scalar unit.  Past the run they are its last page's again: a pair's
+  // loads are always the same number, so that the wait for one pair leaves the next one's in flight (behind
+  // a branch around them every wait is for all loads).
+  int id[2] = {0, 0};
+  auto look = [&](int pg) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) id[x] = ld_const<int>(bt + min(pg + x, p1 - 1));
+  };
   auto load = [&](Pair& b, int pg) {
-    const int at = (pg - p0) & 63;
-    if (at == 0) ids = bt[min(pg + l, p1 - 1)];  // (past the run: its last page again)
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int pid = __builtin_amdgcn_readlane(ids, at + x);
+      const int pid = __builtin_amdgcn_readfirstlane(id[x]);
       const size_t slot = ((size_t)a.layer * a.num_pages + pid) * a.hkv + kvh;
       const char* kb = (const char*)a.kpool + slot * (16 * HD * ES);
       const char* vb = (const char*)a.vpool + slot * (16 * HD * ES);
@@ -236,6 +245,7 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
         b.vs[x] = ld_global<f32x4>((const char*)a.vpool + a.scales + slot * 64 + 16 * lg);
       }
     }
+    look(pg + 2);
   };
   auto key = [&](const KRaw* raw, bf16x8* k) {
     if constexpr (ES == 1) {
@@ -442,14 +452,14 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
     }
   };
   if (p0 < p1) {
+    look(p0);
     load(buf[0], p0);
     for (int pg = p0; pg < p1; pg += 4) {
-      if (pg + 2 < p1) load(buf[1], pg + 2);
+      load(buf[1], pg + 2);
       compute(buf[0], pg);
-      if (pg + 2 < p1) {
-        if (pg + 4 < p1) load(buf[0], pg + 4);
-        compute(buf[1], pg + 2);
-      }
+      if (pg + 2 >= p1) break;
+      load(buf[0], pg + 4);
+      compute(buf[1], pg + 2);
     }
   }
 
