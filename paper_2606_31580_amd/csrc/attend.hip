@@ -948,6 +948,40 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
     a.lse[(size_t)(sp.row0 + r) * a.hq + h] = Lt == 0.f ? -INFINITY : (Mt + __builtin_amdgcn_logf(Lt)) * kLn2;
 }
 
+// The same for spans of at most kAttendFewSplits splits (chunks: many rows, few splits): HD / 4 lanes per (row, head)
+// hold all of them; bounded by the partials' bytes.
+template <class IT, int HD>
+__global__ __launch_bounds__(256) void k_attend_merge_few(AttendArgs a) {
+  constexpr int LPS = HD / 4, NG = 256 / LPS;
+  const AttendSpan sp = item_span(a.n_spans, blockIdx.x);
+  const unsigned local = (blockIdx.x - sp.first) * NG + threadIdx.x / LPS;
+  if (local >= (unsigned)sp.n * a.hq) return;
+  const int r = (int)(local / (unsigned)a.hq), h = (int)(local - (unsigned)r * a.hq), d4 = threadIdx.x % LPS;
+  const size_t part = sp.part0 + (size_t)local * sp.nsplit;
+  float mv[kAttendFewSplits], lv[kAttendFewSplits], M = -INFINITY, L = 0.f;
+  f32x4 ov[kAttendFewSplits], O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < kAttendFewSplits; ++s) {
+    const size_t at = part + min(s, sp.nsplit - 1);
+    const float2 x = *(const float2*)(a.ml + at * 2);
+    mv[s] = x.x;
+    lv[s] = x.y;
+    ov[s] = ld_global<f32x4>(a.part + at * HD + 4 * d4);
+  }
+#pragma unroll
+  for (int s = 0; s < kAttendFewSplits; ++s) M = fmaxf(M, mv[s]);  // (the last one several times: the same maximum)
+#pragma unroll
+  for (int s = 0; s < kAttendFewSplits; ++s) {
+    if (s >= sp.nsplit) break;
+    const float f = mv[s] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv[s] - M);
+    L += lv[s] * f;
+    O += ov[s] * f;
+  }
+  st_out4<IT>(a, sp.row0 + r, h, 4 * d4, O * (L == 0.f ? 0.f : 1.f / L));
+  if (d4 == 0 && a.lse != nullptr)
+    a.lse[(size_t)(sp.row0 + r) * a.hq + h] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
+}
+
 template <class KT, class IT, int HD>
 static hipError_t launch_kind(int kind, const AttendArgs& a, hipStream_t s) {
   const dim3 grid(a.n_items * (unsigned)a.hkv), block(256);
@@ -974,10 +1008,16 @@ hipError_t launch_attend(int kind, int kv_type, int io, int hd, const AttendArgs
   }
 }
 
-hipError_t launch_attend_merge(int io, int hd, const AttendArgs& a, hipStream_t s) {
+hipError_t launch_attend_merge(int io, int hd, bool few, const AttendArgs& a, hipStream_t s) {
+  if (a.n_spans < 1 || a.n_spans > kAttendSpans || a.n_items < 1 || (hd != 64 && hd != 128)) return hipErrorInvalidValue;
   const dim3 grid(a.n_items), block(256);
-  if (io == 1) return hd == 128 ? launch_k(k_attend_merge<bf16_t, 128>, grid, block, s, a) : launch_k(k_attend_merge<bf16_t, 64>, grid, block, s, a);
-  return hd == 128 ? launch_k(k_attend_merge<float, 128>, grid, block, s, a) : launch_k(k_attend_merge<float, 64>, grid, block, s, a);
+  auto go = [&](auto it) {
+    using IT = decltype(it);
+    if (few)
+      return hd == 128 ? launch_k(k_attend_merge_few<IT, 128>, grid, block, s, a) : launch_k(k_attend_merge_few<IT, 64>, grid, block, s, a);
+    return hd == 128 ? launch_k(k_attend_merge<IT, 128>, grid, block, s, a) : launch_k(k_attend_merge<IT, 64>, grid, block, s, a);
+  };
+  return io == 1 ? go(bf16_t{}) : go(float{});
 }
 
 }  // namespace laser

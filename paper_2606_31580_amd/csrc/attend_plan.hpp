@@ -12,7 +12,8 @@ constexpr int kAttendFewCols = 64;
 
 // A span as the planner sees it, and what it decides.
 struct AttendSize {
-  int n, pages;  // query rows; pages that any of them sees
+  int n, pages;    // query rows; pages that any of them sees
+  int rows_pages;  // pages that the last row sees and the first does not (causal)
   int kind;      // the kernel
   int tiles;     // query tiles
   int nsplit;    // workgroups over a tile's pages
@@ -35,28 +36,58 @@ inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256;
 // 3,000-14,000: 219 us with runs of 133 pages, 192 with 33).
 // A span of up to 32 pages stays whole, since joining splits is a launch of its own, up to 64 where there
 // are spans enough to fill the CUs (64 sequences of 50-600 positions: 18.2 us split, 14.4 whole).
-// Tile kernel: one workgroup per CU, each with at least 16 pages.
-inline void plan_attend(AttendSize* s, int n, int group, int kv_heads, int cus, int es, bool io16) {
-  int64_t work = 0, wgs = 0;
+// Tile kernel: see tile_splits.
+inline int tile_splits(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus);
+inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool io16) {
+  int64_t work = 0;
   for (int i = 0; i < n; ++i) {
-    const int64_t cols = (int64_t)s[i].n * group;
+    const int64_t cols = (int64_t)s[i].n * (q_heads / kv_heads);
     s[i].kind = es == 4 || cols <= 16 ? 0 : cols > kAttendFewCols ? 2 : io16 ? 1 : 0;
     s[i].tiles = attend_ceil(cols, attend_cols(s[i].kind));
-    if (s[i].kind == 2)
-      wgs += (int64_t)s[i].tiles * kv_heads;
-    else
-      work += (int64_t)s[i].pages * s[i].tiles * kv_heads;
+    if (s[i].kind != 2) work += (int64_t)s[i].pages * s[i].tiles * kv_heads;
   }
   const int two = attend_ceil(work, (int64_t)cus * 8);  // pages per wave, two workgroups per CU
   const int run = two <= (es == 1 ? 4 : 8) ? std::max(2, attend_ceil(work, (int64_t)cus * 4)) : std::min(two, 32);
   const int whole = two >= 4 ? 64 : 32;
-  const int tile_splits = wgs > 0 ? std::max(1, attend_ceil(cus, wgs)) : 1;
+  const int tile = tile_splits(s, n, kv_heads, q_heads, hd, cus);
   for (int i = 0; i < n; ++i) {
     if (s[i].kind == 2)
-      s[i].nsplit = std::max(1, std::min({128, tile_splits, s[i].pages / 16}));
+      s[i].nsplit = std::max(1, std::min(tile, s[i].pages / 4));
     else
       s[i].nsplit = s[i].pages <= whole ? 1 : std::min(128, attend_ceil(s[i].pages, 4 * run));
   }
+}
+
+// Splits of the tile kernel's spans (the same for all, but never less than a step of 4 pages each): the
+// number that makes the call shortest, counting 2.2 us for a step of a CU's workgroup, 2 us to start one, the
+// partials written and read at 5 TB/s and 5 us for joining them.
+inline int tile_splits(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus) {
+  int best = 1;
+  double best_us = 1e300;
+  for (int k : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+    double all = 0, longest = 0, parts = 0, wgs = 0;
+    for (int i = 0; i < n; ++i) {
+      if (s[i].kind != 2) continue;
+      const int mine = std::max(1, std::min(k, s[i].pages / 4));
+      const double us = 2 + 2.2 * attend_ceil(s[i].pages, 4 * mine);
+      const double mean = 2 + 2.2 * (s[i].pages - 0.5 * s[i].rows_pages) / (4.0 * mine);
+      const double w = (double)s[i].tiles * kv_heads * mine;
+      all += w * mean;
+      wgs += w;
+      longest = std::max(longest, us);
+      if (mine > 1) parts += (double)s[i].n * heads * mine;
+    }
+    if (wgs == 0) return 1;
+    // workgroups of like length run in whole rounds; many of them even out
+    const double rounds = wgs / cus, whole = wgs <= 3.0 * cus ? attend_ceil((int64_t)wgs, cus) : rounds;
+    const double us = std::max(all / cus * (whole / rounds > 1 && rounds > 1 ? whole / rounds : 1.0), longest) +
+                      (parts > 0 ? 5 + parts * (hd + 2) * 8 / 5e6 : 0);
+    if (us < best_us) {
+      best = k;
+      best_us = us;
+    }
+  }
+  return best;
 }
 
 }  // namespace laser

@@ -353,8 +353,10 @@ struct AttendArgs {
 };
 // kind: 0, 1: the row kernel with 16, 32 columns; 2: the tile kernel.  io: 0 fp32, 1 bf16.
 hipError_t launch_attend(int kind, int kv_type, int io, int hd, const AttendArgs& a, hipStream_t s);
-// Combines the partials of a launch's spans with several splits.
-hipError_t launch_attend_merge(int io, int hd, const AttendArgs& a, hipStream_t s);
+// Combines the partials of a launch's spans with several splits; items: (row, head) pairs, or (few: spans of at
+// most kAttendFewSplits splits) 1024 / hd of them.
+constexpr int kAttendFewSplits = 8;
+hipError_t launch_attend_merge(int io, int hd, bool few, const AttendArgs& a, hipStream_t s);
 
 hipError_t launch_confidence(const float* p, int T, int n, float* conf, hipStream_t s);
 hipError_t launch_fill_u32(unsigned* p, int n, unsigned v, hipStream_t s);

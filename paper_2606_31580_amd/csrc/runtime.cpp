@@ -2382,11 +2382,12 @@ laser_status plan_attend_call(const laser_kv* kv, int n_spans, const laser_atten
     AttendSize z{};
     z.n = a.n;
     z.pages = hi > lo ? (int)((hi + kPage - 1) / kPage - lo / kPage) : 0;
+    z.rows_pages = causal ? a.n / kPage : 0;
     job.sp.push_back(a);
     job.size.push_back(z);
   }
-  const int G = d.n_q_heads / d.n_kv_heads;
-  plan_attend(job.size.data(), (int)job.size.size(), G, d.n_kv_heads, m->cus, m->kv_es, io == LASER_DTYPE_BF16);
+  plan_attend(job.size.data(), (int)job.size.size(), d.n_q_heads, d.n_kv_heads, d.head_dim, m->cus, m->kv_es,
+              io == LASER_DTYPE_BF16);
   for (size_t i = 0; i < job.sp.size(); ++i) {
     job.sp[i].nsplit = job.size[i].nsplit;
     if (job.size[i].nsplit > 1) {
@@ -2496,25 +2497,34 @@ static laser_status attend(laser_kv* kv, int layer, int n_spans, const laser_att
   a.ml = (float*)((char*)d_workspace + align256((size_t)job.parts * d.head_dim * 4));
   const int io = q->dtype == LASER_DTYPE_BF16;
   TimingScope scope(m);
-  // each kernel over the spans that it takes, then the join of those with several splits
-  for (int kind = 0; kind <= kAttendKinds; ++kind) {
-    const bool merge = kind == kAttendKinds;
+  // Each kernel over the spans that it takes, then the joins: a workgroup per row and head, or, where many rows
+  // have few splits, several to a workgroup (a few thousand rows measured 1-2 us faster the first way, 14,336 of two
+  // splits 25 us slower).
+  uint64_t few_rows = 0;
+  for (const AttendSpan& x : job.sp)
+    if (x.nsplit > 1 && x.nsplit <= kAttendFewSplits) few_rows += (uint64_t)x.n * d.n_q_heads;
+  const int few_splits = few_rows <= 8192 ? 1 : kAttendFewSplits;
+  for (int pass = 0; pass < kAttendKinds + 2; ++pass) {
+    const bool merge = pass >= kAttendKinds, few = pass == kAttendKinds + 1;
+    const int heads = merge ? 1 : d.n_kv_heads;  // workgroups per item
     for (size_t i = 0; i < job.sp.size();) {
       a.n_spans = 0;
       uint64_t items = 0;
       for (; i < job.sp.size() && a.n_spans < kAttendSpans; ++i) {
-        if (merge ? job.sp[i].nsplit == 1 : job.size[i].kind != kind) continue;
-        const uint64_t mine = merge ? (uint64_t)job.sp[i].n * d.n_q_heads : (uint64_t)job.size[i].tiles * job.sp[i].nsplit;
-        if (a.n_spans > 0 && (items + mine) * (merge ? 1 : d.n_kv_heads) >> 31) break;
-        a.sp[a.n_spans] = job.sp[i];
+        const AttendSpan& x = job.sp[i];
+        if (merge ? x.nsplit == 1 || (x.nsplit <= few_splits) != few : job.size[i].kind != pass) continue;
+        const uint64_t rows = (uint64_t)x.n * d.n_q_heads, per = few ? 1024 / d.head_dim : 1;
+        const uint64_t mine = merge ? (rows + per - 1) / per : (uint64_t)job.size[i].tiles * x.nsplit;
+        if (a.n_spans > 0 && ((items + mine) * heads) >> 31) break;
+        a.sp[a.n_spans] = x;
         a.sp[a.n_spans++].first = (unsigned)items;
         items += mine;
       }
       if (a.n_spans == 0) break;
-      if (items * (merge ? 1 : d.n_kv_heads) >> 31) return laser_fail(LASER_ERR_UNSUPPORTED, "too many rows in a span");
+      if ((items * heads) >> 31) return laser_fail(LASER_ERR_UNSUPPORTED, "too many rows in a span");
       a.n_items = (unsigned)items;
       HIP_TRY(timed(m, LASER_K_ATTN, s, [&] {
-        return merge ? launch_attend_merge(io, d.head_dim, a, s) : launch_attend(kind, kv_type_of(m), io, d.head_dim, a, s);
+        return merge ? launch_attend_merge(io, d.head_dim, few, a, s) : launch_attend(pass, kv_type_of(m), io, d.head_dim, a, s);
       }));
     }
   }

@@ -1,0 +1,76 @@
+"""The planner of laser_attend (csrc/attend_plan.hpp), compiled with the host compiler: which kernel takes a
+span and over how many workgroups its keys are split, over sizes from one row and no key to the longest."""
+import os
+import random
+import subprocess
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2606_31580_amd", "csrc")
+MAIN = """
+#include <cstdio>
+#include <vector>
+#include "attend_plan.hpp"
+int main() {
+  int n, hq, hkv, hd, cus, es, io16;
+  while (std::scanf("%d %d %d %d %d %d %d", &n, &hq, &hkv, &hd, &cus, &es, &io16) == 7) {
+    std::vector<laser::AttendSize> s(n);
+    for (auto& x : s) std::scanf("%d %d %d", &x.n, &x.pages, &x.rows_pages);
+    laser::plan_attend(s.data(), n, hq, hkv, hd, cus, es, io16);
+    for (auto& x : s) std::printf("%d %d %d ", x.kind, x.tiles, x.nsplit);
+    std::printf("\\n");
+  }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    d = tmp_path_factory.mktemp("plan")
+    (d / "main.cpp").write_text(MAIN)
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", f"-I{CSRC}", "-o", str(d / "plan"), str(d / "main.cpp")], check=True)
+
+    def call(spans, hq=28, hkv=4, hd=128, cus=256, es=1, io16=1):
+        line = f"{len(spans)} {hq} {hkv} {hd} {cus} {es} {io16} " + " ".join(f"{n} {p} {r}" for n, p, r in spans)
+        out = [int(x) for x in subprocess.run([str(d / "plan")], input=line, capture_output=True, text=True, check=True).stdout.split()]
+        return [tuple(out[3 * i:3 * i + 3]) for i in range(len(spans))]
+
+    return call
+
+
+def span(n, end):
+    """n rows that end at position `end`, causal."""
+    return (n, -(-end // 16), min(n, end) // 16)
+
+
+def test_kernels_and_bounds(plan):
+    rng = random.Random(3)
+    for _ in range(60):
+        hq, hkv = rng.choice([(28, 4), (32, 8), (12, 2), (16, 1), (3, 3)])
+        es, io16 = rng.choice([(1, 1), (1, 0), (2, 1), (2, 0), (4, 0), (4, 1)])
+        spans = []
+        for _ in range(rng.choice([1, 1, 2, 8, 64])):
+            n = int(2 ** rng.uniform(0, 13))
+            spans.append(span(n, int(2 ** rng.uniform(0, 16)) if rng.random() < 0.95 else 0))
+        for (n, pages, _), (kind, tiles, splits) in zip(spans, plan(spans, hq, hkv, rng.choice([64, 128]), 256, es, io16)):
+            cols = n * hq // hkv
+            assert kind in ((0,) if es == 4 else (0, 1, 2)) and not (kind == 1 and not io16)
+            assert kind == 0 or cols > 16
+            assert tiles == -(-cols // {0: 16, 1: 32, 2: 256}[kind])
+            assert 1 <= splits <= 128 and splits <= max(1, pages)
+
+
+def test_one_long_request_fills_the_card(plan):
+    ((kind, _, splits),) = plan([span(1, 14336)])
+    assert kind == 0 and splits * 4 >= 128
+    ((kind, tiles, splits),) = plan([span(128, 14000)])
+    assert kind == 2 and 128 <= tiles * 4 * splits <= 512
+
+
+def test_short_keys_and_full_cards_are_not_split(plan):
+    assert plan([span(1, 500)]) == [(0, 1, 1)]
+    assert all(s == 1 for _, _, s in plan([span(1, 50 + 9 * i) for i in range(64)], 32, 8))
+    ((_, _, splits),) = plan([span(4096, 8192)], 32, 8)
+    assert splits == 1
+    ((_, _, splits),) = plan([span(512, 512)])
+    assert splits == 1
