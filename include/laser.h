@@ -374,8 +374,8 @@ laser_status laser_kv_truncate(laser_kv* kv, int seq_id, int length);
 laser_status laser_kv_write(laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k,
                             const laser_rows* v, void* stream);
 /* Reads the runs' positions into rows of k and v: the values that the cache stands for (INT8: q s, one
- * fp32 product), rounded once to the rows' type.  No row twice (INVALID_ARG); other rows keep what they
- * hold. */
+ * fp32 product), rounded once to the rows' type.  No row twice, and k and v apart (INVALID_ARG); other
+ * rows keep what they hold. */
 laser_status laser_kv_read(const laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k,
                            const laser_rows* v, void* stream);
 
@@ -392,7 +392,8 @@ typedef struct {
  * (d_lse: [rows][n_q_heads] fp32, or NULL), so that outputs over parts of the keys can be combined.  A row
  * that sees nothing (or only scores of -infinity) gets o = 0 and lse = -infinity.  A position that a
  * row does not see does not touch it, whatever it holds.  Rows outside the spans keep what they hold.
- * q and o have the same element type; o may be q itself.  With bf16 rows the softmax weights are
+ * q and o have the same element type; o may be q itself (the same pointer and strides), and overlaps it in
+ * no other way.  With bf16 rows the softmax weights are
  * rounded to bf16 before they meet V; with fp32 rows nothing is rounded below fp32.  Sums, maxima and the
  * log-sum-exp are fp32 in both.  Results do not depend on what else runs, but a row's last bits may
  * change with the other spans of the call (they decide how keys are split over workgroups).

@@ -74,7 +74,7 @@ def check(kv, kind, io, held, spans, q, scale=None, causal=True, window=0, layer
         lf = np.isfinite(rl)
         terms = abs(scale) * np.abs(q64[r]).max() * np.abs(kf).max() * math.sqrt(hd)
         # lse: the same score error, and 2^-23 of itself for the two roundings and the logarithm
-        assert np.all(np.abs(gl[r] - rl)[lf] <= (4 * 2.0 ** -24 * terms + 64 * 2.0 ** -24) + 2.0 ** -22 * np.abs(rl[lf]))
+        assert np.all(np.abs(gl[r][lf] - rl[lf]) <= (4 * 2.0 ** -24 * terms + 64 * 2.0 ** -24) + 2.0 ** -22 * np.abs(rl[lf]))
     assert np.all(go[~seen] == 5.0) and np.all(gl[~seen] == 5.0)
     return o, lse
 
@@ -334,3 +334,107 @@ def test_int8_scales_far_apart(n):
           [L.attend_span(0, n, length - n, kv_begin=11, kv_end=229)], q)
     o, _ = check(kv, "int8", "bf16", held, [L.attend_span(0, n, length - n, kv_begin=100, kv_end=120)], q)
     assert float(o.float().abs().max()) > 2.0 ** -64  # (the small rows by themselves are not lost)
+
+
+def device_reference(kv, layer, spans, q, scale, causal, window, hkv):
+    """The definition in float64 on the device, over the values that laser_kv_read gives: (o, lse) with 5.0 in other rows."""
+    rows_, hq, hd = q.shape
+    o = torch.full(q.shape, 5.0, dtype=torch.float64, device="cuda")
+    lse = torch.full((rows_, hq), 5.0, dtype=torch.float64, device="cuda")
+    top = 0.0
+    for s in spans:
+        n = kv.seq_len(s.seq)
+        end = n if s.kv_end == -1 else s.kv_end
+        k, v = (torch.zeros(n, hkv, hd, device="cuda") for _ in range(2))
+        if n:
+            L.laser_kv_read(kv, layer, [L.kv_run(s.seq, 0, n)], k, v)
+            top = max(top, float(v.abs().max()))
+        row = torch.arange(s.pos, s.pos + s.n, device="cuda")[:, None]
+        t = torch.arange(n, device="cuda")[None, :]
+        seen = (t >= s.kv_begin) & (t < end)
+        seen = seen & (t <= row) if causal else seen.expand(s.n, n)
+        if window:
+            seen = seen & (t > row - window)
+        r = slice(s.row0, s.row0 + s.n)
+        for h in range(hq):
+            x = (q[r, h].double() @ k[:, h // (hq // hkv)].double().t()) * scale
+            x = x.masked_fill(~seen, -math.inf)
+            z = torch.logsumexp(x, -1)
+            w = torch.where(torch.isinf(z)[:, None], 0.0, torch.exp(x - z[:, None]))
+            o[r, h], lse[r, h] = w @ v[:, h // (hq // hkv)].double(), z
+    return o, lse, top
+
+
+def check_device(kv, io, spans, q, causal=True, window=0, layer=1, o=None, hkv=2):
+    o = torch.full_like(q, 5.0) if o is None else o
+    lse = torch.full(q.shape[:2], 5.0, device="cuda")
+    scale = q.shape[-1] ** -0.5
+    ref, rl, top = device_reference(kv, layer, spans, q.clone(), scale, causal, window, hkv)
+    L.laser_attend(kv, layer, spans, q, o, lse=lse, causal=causal, window=window)
+    torch.cuda.synchronize()
+    # (as `tolerance` has it; scores of standard-normal rows stay below 40, their errors below 40 x 2^-22)
+    tol = 40 * 2.0 ** -22 * top + (2.0 ** -9 * top + 2.0 ** -8 * ref.abs() if io == "bf16" else 2.0 ** -20 * top)
+    assert bool(((o.double() - ref).abs() <= tol).all()), float(((o.double() - ref).abs() - tol).max())
+    assert torch.equal(torch.isinf(lse), torch.isinf(rl))
+    fin = ~torch.isinf(rl)
+    assert bool(((lse.double() - rl).abs()[fin] <= 40 * 2.0 ** -22 + 2.0 ** -22 * rl.abs()[fin]).all())
+    return o
+
+
+@pytest.mark.parametrize("kind,io", [("int8", "bf16"), ("fp8", "f32"), ("bf16", "bf16")])
+def test_many_rows_few_splits(kind, io):
+    """Some hundred rows behind a long context: tiles whose keys are split a few times, joined row by row; a long prompt
+    beside it that is not split; the same in place."""
+    hq, hkv, hd = 28, 4, 128
+    kv = cache(kind, hq, hkv, hd, pages=700, seqs=3, per_seq=400)
+    fill(kv, kind, [4200, 1500, 37], hkv, hd, 31)
+    rng = np.random.default_rng(32)
+    q = queries(rng, 400 + 700 + 30, hq, hd, io)
+    spans = [L.attend_span(0, 400, 3800), L.attend_span(1, 700, 800, row0=400), L.attend_span(2, 3, 34, row0=1101)]
+    want = check_device(kv, io, spans, q, hkv=hkv)
+    got = check_device(kv, io, spans[:1], q, hkv=hkv)
+    assert bool((got[:400].float() - want[:400].float()).abs().max() <= 2.0 ** -7 * float(want[:400].abs().max()))
+    again = q.clone()
+    L.laser_attend(kv, 1, spans, again, again)
+    for s in spans:
+        assert torch.equal(again[s.row0:s.row0 + s.n], want[s.row0:s.row0 + s.n])
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_tile_strides(io):
+    """Chunks wide enough for tiles: heads before rows, rows off 16 bytes, in and out."""
+    hq, hkv, hd, n = 6, 2, 64, 190
+    kv = cache("int8", hq, hkv, hd, pages=60, seqs=1, per_seq=60)
+    fill(kv, "int8", [800], hkv, hd, 33)
+    rng = np.random.default_rng(34)
+    base = queries(rng, n, hq, hd, io)
+    spans = [L.attend_span(0, n, 800 - n)]
+    want = check_device(kv, io, spans, base)
+    odd = torch.zeros(n, hq, hd + 1, dtype=IO[io], device="cuda")[:, :, 1:]
+    odd.copy_(base)
+    out = torch.full((hq, n, hd + 3), 5.0, dtype=IO[io], device="cuda").transpose(0, 1)[:, :, 3:]
+    assert torch.equal(check_device(kv, io, spans, odd, o=out), want)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_calls(seed):
+    """Calls of random shape: heads, types, spans of all sizes in one call, key ranges, windows, causal or not."""
+    rng = np.random.default_rng(1000 + seed)
+    hq, hkv, hd = [(4, 2, 64), (7, 1, 128), (16, 1, 64), (3, 3, 128), (12, 2, 128)][int(rng.integers(5))]
+    kind = ["int8", "int8", "fp8", "bf16", "f32"][int(rng.integers(5))]
+    io = ["bf16", "f32"][int(rng.integers(2))]
+    b = int(rng.integers(1, 9))
+    lens = [int(2 ** rng.uniform(0, 11.5)) for _ in range(b)]
+    kv = cache(kind, hq, hkv, hd, pages=sum(-(-n // 16) for n in lens) + 1, seqs=b, per_seq=200)
+    fill(kv, kind, lens, hkv, hd, 2000 + seed)
+    causal, window = bool(rng.random() < 0.8), int(rng.choice([0, 0, 1, 33, 500]))
+    spans, at = [], 1
+    for _ in range(int(rng.integers(1, 7))):
+        s = int(rng.integers(b))
+        n = int(2 ** rng.uniform(0, 8.5))
+        lo = int(rng.integers(0, lens[s] + 1)) if rng.random() < 0.3 else 0
+        hi = int(rng.integers(lo, lens[s] + 1)) if rng.random() < 0.3 else -1
+        pos = max(0, lens[s] - n) if rng.random() < 0.6 else int(rng.integers(0, lens[s] + 50))
+        spans.append(L.attend_span(s, n, pos, row0=at, kv_begin=lo, kv_end=hi))
+        at += n + int(rng.integers(0, 3))
+    check_device(kv, io, spans, queries(rng, at + 1, hq, hd, io), causal=causal, window=window, hkv=hkv)

@@ -88,11 +88,11 @@ def test_rows_refusals(fn):
     _, kv = _kv()
     L._call("laser_kv_add_seq", kv, 0, 40)
     L._call("laser_kv_add_seq", kv, 1, 20)
-    good = _rows(64, 2)
+    good, also = _rows(64, 2), _rows(64, 2, ptr=2 * PTR)
     ok = [L.kv_run(0, 3, 20, 5)]
-    assert _write(kv, ok, good, good, fn=fn) == L.ERR_STATE and "finalized" in _msg()  # the arguments are in order
+    assert _write(kv, ok, good, also, fn=fn) == L.ERR_STATE and "finalized" in _msg()  # the arguments are in order
 
-    def refused(code, runs=ok, k=good, v=good, layer=0):
+    def refused(code, runs=ok, k=good, v=also, layer=0):
         assert _write(kv, runs, k, v, layer, fn) == code, _msg()
 
     for layer in (-1, 2):
@@ -121,6 +121,7 @@ def test_rows_refusals(fn):
         refused(L.ERR_STATE, k=flat)
         refused(L.ERR_STATE, k=_rows(64, 2, row=0, head=0))
     else:
+        refused(L.ERR_INVALID_ARG, v=good)  # both into the same place
         refused(L.ERR_STATE, twice)
         refused(L.ERR_INVALID_ARG, same_row)
         refused(L.ERR_INVALID_ARG, k=flat)
@@ -170,7 +171,7 @@ def test_attend_refusals():
     S = L.attend_span
     for bad in (S(2, 1, 0), S(0, -1, 0), S(0, 1, -1), S(0, 1, 0, row0=-1), S(0, 1, 0, kv_begin=-1), S(0, 1, 0, kv_end=401),
                 S(0, 1, 0, kv_end=-2), S(0, 1, 0, kv_begin=5, kv_end=4), S(0, 10, 0, row0=55), S(0, 65, 0),
-                S(0, 1, 2 ** 31 - 1), S(0, 1, 0, row0=2 ** 31 - 1), S(0, 2 ** 31 - 1, 0)):
+                S(0, 1, 2 ** 31 - 1), S(0, 1, 0, row0=2 ** 31 - 1), S(0, 2 ** 31 - 1, 0), S(0, 2 ** 26 + 1, 0)):
         refused(L.ERR_INVALID_ARG, [bad])
     refused(L.ERR_INVALID_ARG, [S(0, 10, 0), S(0, 3, 0, row0=9)])
     refused(L.ERR_INVALID_ARG, q=_rows(64, 4, ptr=0))
