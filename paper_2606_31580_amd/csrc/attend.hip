@@ -168,7 +168,8 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
   const int lc = l & 15, lg = l >> 4;
   const int ncol = sp.n * a.G, tiles = (ncol + NC - 1) / NC;
-  const int local = (int)(item - sp.first), split = local / tiles, tile = local - split * tiles;
+  const int local = (int)(item - sp.first), split = local / tiles;
+  const int tile = tiles - 1 - (local - split * tiles);  // (the last tile has the most keys: first)
   const int col0 = tile * NC;
   const int row_a = col0 / a.G, row_b = min(col0 + NC, ncol) - 1;  // first row, last column
   const int row_z = row_b / a.G;                                   // last row

@@ -27,6 +27,12 @@ inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256;
 // es: bytes of a cached element; io16: 16-bit rows.  fp32 pools have only the row kernel with 16 columns,
 // and fp32 rows not the one with 32 (three parts of everything would not fit the registers).
 //
+// The tile kernel converts a page once for 256 columns and not for 32, but has 8 times fewer, longer workgroups: it
+// pays from some work on, counted in pages x 32-column tiles per CU (us, tiles and rows, 7B heads, INT8, bf16 rows: a
+// prompt of 512 rows, 28 per CU, 26.2 and 15.8, of 1,024, 112, 41 and 34, of 2,048, 450, 68 and 84; 512 rows
+// behind 2,000 positions, 246, 44 and 57; bf16 pools: 20 rows behind 14,000, 68, 24 and 32; fp32 rows: a prompt of
+// 1,024 70 and 49, of 2,048 137 and 139).
+//
 // Row kernels: pages per wave.  Every CU runs one workgroup of 4 waves, or two on 8-bit pools (fewer
 // registers).  Long runs stream best when two workgroups per CU share the pages; where that leaves a wave only
 // a few pages, one per CU with twice the pages has fewer splits to join and, on wider pools, no second
@@ -35,26 +41,32 @@ inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256;
 // 3,000-9,000, 9 pages 20.5 and 26.6).  Runs end at 32 pages: more rounds even out ragged lengths (64 sequences of
 // 3,000-14,000: 219 us with runs of 133 pages, 192 with 33).
 // A span of up to 32 pages stays whole, since joining splits is a launch of its own, up to 64 where there
-// are spans enough to fill the CUs (64 sequences of 50-600 positions: 18.2 us split, 14.4 whole).
+// are spans enough to fill the CUs (64 sequences of 50-600 positions: 18.2 us split, 14.4 whole) or rows enough to
+// make the join long.
 // Tile kernel: see tile_splits.
 inline int tile_splits(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus);
-inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool io16) {
-  int64_t work = 0;
+// mode: 0 the kernels as above, 1 only row kernels, 2 the tile kernel wherever it can be (laser_model_set_attend_kernel).
+inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool io16, int mode) {
+  int64_t work = 0, wide = 0;
   for (int i = 0; i < n; ++i) {
     const int64_t cols = (int64_t)s[i].n * (q_heads / kv_heads);
-    s[i].kind = es == 4 || cols <= 16 ? 0 : cols > kAttendFewCols ? 2 : io16 ? 1 : 0;
+    if (cols > kAttendFewCols) wide += (int64_t)attend_ceil(cols, 32) * kv_heads * (s[i].pages - s[i].rows_pages / 2);
+  }
+  const bool tiles = es <= 2 && mode != 1 && (mode == 2 || wide > (int64_t)cus * (io16 ? (es == 1 ? 130 : 60) : 300));
+  for (int i = 0; i < n; ++i) {
+    const int64_t cols = (int64_t)s[i].n * (q_heads / kv_heads);
+    s[i].kind = cols > kAttendFewCols && tiles ? 2 : es == 4 || cols <= 16 || !io16 ? 0 : 1;
     s[i].tiles = attend_ceil(cols, attend_cols(s[i].kind));
     if (s[i].kind != 2) work += (int64_t)s[i].pages * s[i].tiles * kv_heads;
   }
   const int two = attend_ceil(work, (int64_t)cus * 8);  // pages per wave, two workgroups per CU
   const int run = two <= (es == 1 ? 4 : 8) ? std::max(2, attend_ceil(work, (int64_t)cus * 4)) : std::min(two, 32);
-  const int whole = two >= 4 ? 64 : 32;
   const int tile = tile_splits(s, n, kv_heads, q_heads, hd, cus);
   for (int i = 0; i < n; ++i) {
     if (s[i].kind == 2)
       s[i].nsplit = std::max(1, std::min(tile, s[i].pages / 4));
     else
-      s[i].nsplit = s[i].pages <= whole ? 1 : std::min(128, attend_ceil(s[i].pages, 4 * run));
+      s[i].nsplit = s[i].pages <= (two >= 4 || (int64_t)s[i].n * q_heads > 512 ? 64 : 32) ? 1 : std::min(128, attend_ceil(s[i].pages, 4 * run));
   }
 }
 

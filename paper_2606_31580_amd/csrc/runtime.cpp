@@ -191,6 +191,7 @@ struct laser_model {
   int last_stop = -1;  // pool index bound to the most recent launch's end
   bool use_graphs = true;
   int gemm_kernel = 0;  // MFMA-path kernel choice (laser_model_set_gemm_kernel)
+  int attend_kernel = 0;  // kernels of laser_attend (laser_model_set_attend_kernel)
   // one-row attention groups merge their splits inside the attention kernel (laser_model_set_attn_merge;
   // off by default: measured slower than the merge kernel at the 7B shape, batch 1)
   int attn_fuse = 0;
@@ -2388,7 +2389,7 @@ laser_status plan_attend_call(const laser_kv* kv, int n_spans, const laser_atten
     job.size.push_back(z);
   }
   plan_attend(job.size.data(), (int)job.size.size(), d.n_q_heads, d.n_kv_heads, d.head_dim, m->cus, m->kv_es,
-              io == LASER_DTYPE_BF16);
+              io == LASER_DTYPE_BF16, m->attend_kernel);
   for (size_t i = 0; i < job.sp.size(); ++i) {
     job.sp[i].nsplit = job.size[i].nsplit;
     if (job.size[i].nsplit > 1) {
@@ -2598,6 +2599,13 @@ extern "C" laser_status laser_model_set_gemm_kernel(laser_model* m, int mode) {
   if (mode < 0 || mode > 2) return laser_fail(LASER_ERR_INVALID_ARG, "gemm kernel mode must be 0, 1 or 2");
   if (mode != m->gemm_kernel) drop_graphs(m);  // captured forwards hold the previous choice
   m->gemm_kernel = mode;
+  return LASER_OK;
+}
+
+extern "C" laser_status laser_model_set_attend_kernel(laser_model* m, int mode) {
+  if (!model_of(m)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed model");
+  if (mode < 0 || mode > 2) return laser_fail(LASER_ERR_INVALID_ARG, "attend kernel mode must be 0, 1 or 2");
+  m->attend_kernel = mode;
   return LASER_OK;
 }
 

@@ -121,6 +121,7 @@ _SIGS = {
     "laser_timing_read": (_I, [_P, _I, C.POINTER(C.c_double), C.POINTER(_I)]),
     "laser_model_set_graphs": (_I, [_P, _I]),
     "laser_model_set_gemm_kernel": (_I, [_P, _I]),
+    "laser_model_set_attend_kernel": (_I, [_P, _I]),
     "laser_model_set_attn_merge": (_I, [_P, _I, _I]),
     "laser_model_set_oproj_merge": (_I, [_P, _I]),
     "laser_model_graph_stats": (_I, [_P, C.POINTER(C.c_longlong), C.POINTER(C.c_int)]),
@@ -329,6 +330,10 @@ class Model:
     def set_gemm_kernel(self, mode: int):
         """Matrix-core projection kernel: 0 by cost (default), 1 K-split waves, 2 row waves."""
         _call("laser_model_set_gemm_kernel", self.h, int(mode))
+
+    def set_attend_kernel(self, mode: int):
+        """Kernels of laser_attend: 0 by work (default), 1 row kernels only, 2 the tile kernel above 64 columns."""
+        _call("laser_model_set_attend_kernel", self.h, int(mode))
 
     def timing_enable(self, cls: int, on: bool = True):
         _call("laser_timing_enable", self.h, cls, int(on))

@@ -12,11 +12,11 @@ MAIN = """
 #include <vector>
 #include "attend_plan.hpp"
 int main() {
-  int n, hq, hkv, hd, cus, es, io16;
-  while (std::scanf("%d %d %d %d %d %d %d", &n, &hq, &hkv, &hd, &cus, &es, &io16) == 7) {
+  int n, hq, hkv, hd, cus, es, io16, mode;
+  while (std::scanf("%d %d %d %d %d %d %d %d", &n, &hq, &hkv, &hd, &cus, &es, &io16, &mode) == 8) {
     std::vector<laser::AttendSize> s(n);
     for (auto& x : s) std::scanf("%d %d %d", &x.n, &x.pages, &x.rows_pages);
-    laser::plan_attend(s.data(), n, hq, hkv, hd, cus, es, io16);
+    laser::plan_attend(s.data(), n, hq, hkv, hd, cus, es, io16, mode);
     for (auto& x : s) std::printf("%d %d %d ", x.kind, x.tiles, x.nsplit);
     std::printf("\\n");
   }
@@ -30,8 +30,8 @@ def plan(tmp_path_factory):
     (d / "main.cpp").write_text(MAIN)
     subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", f"-I{CSRC}", "-o", str(d / "plan"), str(d / "main.cpp")], check=True)
 
-    def call(spans, hq=28, hkv=4, hd=128, cus=256, es=1, io16=1):
-        line = f"{len(spans)} {hq} {hkv} {hd} {cus} {es} {io16} " + " ".join(f"{n} {p} {r}" for n, p, r in spans)
+    def call(spans, hq=28, hkv=4, hd=128, cus=256, es=1, io16=1, mode=0):
+        line = f"{len(spans)} {hq} {hkv} {hd} {cus} {es} {io16} {mode} " + " ".join(f"{n} {p} {r}" for n, p, r in spans)
         out = [int(x) for x in subprocess.run([str(d / "plan")], input=line, capture_output=True, text=True, check=True).stdout.split()]
         return [tuple(out[3 * i:3 * i + 3]) for i in range(len(spans))]
 
@@ -48,14 +48,16 @@ def test_kernels_and_bounds(plan):
     for _ in range(60):
         hq, hkv = rng.choice([(28, 4), (32, 8), (12, 2), (16, 1), (3, 3)])
         es, io16 = rng.choice([(1, 1), (1, 0), (2, 1), (2, 0), (4, 0), (4, 1)])
+        mode = rng.choice([0, 0, 1, 2])
         spans = []
         for _ in range(rng.choice([1, 1, 2, 8, 64])):
             n = int(2 ** rng.uniform(0, 13))
             spans.append(span(n, int(2 ** rng.uniform(0, 16)) if rng.random() < 0.95 else 0))
-        for (n, pages, _), (kind, tiles, splits) in zip(spans, plan(spans, hq, hkv, rng.choice([64, 128]), 256, es, io16)):
+        for (n, pages, _), (kind, tiles, splits) in zip(spans, plan(spans, hq, hkv, rng.choice([64, 128]), 256, es, io16, mode)):
             cols = n * hq // hkv
+            assert (kind != 2 or mode != 1) and (mode != 2 or es == 4 or cols <= 64 or kind == 2)
             assert kind in ((0,) if es == 4 else (0, 1, 2)) and not (kind == 1 and not io16)
-            assert kind == 0 or cols > 16
+            assert (kind != 1 or cols > 16) and (kind != 2 or cols > 64)
             assert tiles == -(-cols // {0: 16, 1: 32, 2: 256}[kind])
             assert 1 <= splits <= 128 and splits <= max(1, pages)
 
@@ -63,7 +65,7 @@ def test_kernels_and_bounds(plan):
 def test_one_long_request_fills_the_card(plan):
     ((kind, _, splits),) = plan([span(1, 14336)])
     assert kind == 0 and splits * 4 >= 128
-    ((kind, tiles, splits),) = plan([span(128, 14000)])
+    ((kind, tiles, splits),) = plan([span(128, 14000)], mode=2)
     assert kind == 2 and 128 <= tiles * 4 * splits <= 512
 
 
@@ -72,5 +74,11 @@ def test_short_keys_and_full_cards_are_not_split(plan):
     assert all(s == 1 for _, _, s in plan([span(1, 50 + 9 * i) for i in range(64)], 32, 8))
     ((_, _, splits),) = plan([span(4096, 8192)], 32, 8)
     assert splits == 1
-    ((_, _, splits),) = plan([span(512, 512)])
-    assert splits == 1
+    for mode, kind in ((1, 1), (2, 2)):
+        assert plan([span(512, 512)], mode=mode)[0][::2] == (kind, 1)
+
+
+def test_tiles_pay_from_some_work_on(plan):
+    """Prompts of a few hundred rows through row kernels, long ones and chunks behind long contexts through tiles."""
+    for n, end, kind in ((64, 64, 1), (512, 512, 1), (2048, 2048, 2), (512, 14000, 2), (4096, 16384, 2)):
+        assert plan([span(n, end)])[0][0] == kind, (n, end)

@@ -7,11 +7,30 @@ import numpy as np
 import pytest
 import torch
 
+import test_gpu_16_kv_rows
 from paged_ref import attend, kept
 from paper_2606_31580_amd import laser as L
 from test_gpu_16_kv_rows import IO, cache, f64, rows
 
 pytestmark = pytest.mark.gpu
+ROWS, TILES = 1, 2  # laser_model_set_attend_kernel: row kernels only; the tile kernel above 64 columns
+
+
+@pytest.fixture(autouse=True)
+def kernels(request):
+    """Runs a test with the kernels that its `kernels` parameter names (by work: 0); models are shared, so it is set back."""
+    from test_gpu_16_kv_rows import _models
+    mode = request.param if hasattr(request, "param") else 0
+    test_gpu_16_kv_rows.MODE = mode
+    for m in _models.values():
+        m.set_attend_kernel(mode)
+    yield mode
+    test_gpu_16_kv_rows.MODE = 0
+    for m in _models.values():
+        m.set_attend_kernel(0)
+
+
+both = pytest.mark.parametrize("kernels", [ROWS, TILES], indirect=True, ids=["rows", "tiles"])
 
 
 def fill(kv, kind, lens, hkv, hd, seed, layer=1, spread=1.0):
@@ -91,6 +110,7 @@ def test_decode_rows(kind, io, hq, hkv, hd):
     check(kv, kind, io, held, [L.attend_span(s, 1, max(n - 1, 0), row0=s + 1) for s, n in enumerate(lens)], q)
 
 
+@both
 @pytest.mark.parametrize("hq,hkv,hd", [(4, 2, 64), (7, 1, 128), (3, 3, 128)])
 @pytest.mark.parametrize("kind,io", [("int8", "bf16"), ("int8", "f32"), ("fp8", "bf16"), ("bf16", "bf16"), ("bf16", "f32"),
                                      ("f32", "f32")])
@@ -108,6 +128,7 @@ def test_chunks(kind, io, hq, hkv, hd):
     check(kv, kind, io, held, spans, q)
 
 
+@both
 @pytest.mark.parametrize("kind,io", [("int8", "bf16"), ("bf16", "f32"), ("fp8", "bf16")])
 @pytest.mark.parametrize("causal,window", [(True, 1), (True, 16), (True, 77), (False, 0), (False, 40)])
 def test_masks_and_ranges(kind, io, causal, window):
@@ -124,6 +145,7 @@ def test_masks_and_ranges(kind, io, causal, window):
     check(kv, kind, io, held, spans, q, causal=causal, window=window)
 
 
+@both
 @pytest.mark.parametrize("kind,io", [("bf16", "bf16"), ("bf16", "f32"), ("fp8", "bf16"), ("int8", "bf16"), ("f32", "f32")])
 @pytest.mark.parametrize("n", [3, 40, 150])
 def test_odd_values_in_unseen_places(kind, io, n):
@@ -299,6 +321,7 @@ def test_long_context():
     check(kv, "int8", "f32", held, [L.attend_span(0, 1, n - 1), L.attend_span(0, 8, n - 8, row0=1)], q)
 
 
+@both
 @pytest.mark.parametrize("kind,io", [("int8", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 0.9])
 def test_scales(kind, io, scale):
@@ -310,6 +333,7 @@ def test_scales(kind, io, scale):
     check(kv, kind, io, held, [L.attend_span(0, 2, 331), L.attend_span(0, 50, 283, row0=5)], q, scale=scale)
 
 
+@both
 @pytest.mark.parametrize("n", [2, 70])
 def test_int8_scales_far_apart(n):
     """Value rows of 2^-60 to 2^60, rows of zeros, beside ordinary ones: each weight counts once in the sum and once,
@@ -381,6 +405,7 @@ def check_device(kv, io, spans, q, causal=True, window=0, layer=1, o=None, hkv=2
     return o
 
 
+@both
 @pytest.mark.parametrize("kind,io", [("int8", "bf16"), ("fp8", "f32"), ("bf16", "bf16")])
 def test_many_rows_few_splits(kind, io):
     """Some hundred rows behind a long context: tiles whose keys are split a few times, joined row by row; a long prompt
@@ -400,6 +425,7 @@ def test_many_rows_few_splits(kind, io):
         assert torch.equal(again[s.row0:s.row0 + s.n], want[s.row0:s.row0 + s.n])
 
 
+@both
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 def test_tile_strides(io):
     """Chunks wide enough for tiles: heads before rows, rows off 16 bytes, in and out."""
@@ -416,6 +442,7 @@ def test_tile_strides(io):
     assert torch.equal(check_device(kv, io, spans, odd, o=out), want)
 
 
+@both
 @pytest.mark.parametrize("seed", range(12))
 def test_random_calls(seed):
     """Calls of random shape: heads, types, spans of all sizes in one call, key ranges, windows, causal or not."""

@@ -203,3 +203,15 @@ def test_attend_workspace():
     assert _attend(kv, [S(0, 1, 999)], q, q, ws=PTR, nb=nb) == L.ERR_STATE
     assert _bytes(kv, [S(0, 1, 999)], dtype=L.DTYPE_FP8_E4M3)[0] == L.ERR_UNSUPPORTED
     assert _bytes(kv, [S(3, 1, 0)])[0] == L.ERR_INVALID_ARG
+
+
+def test_attend_kernel_modes():
+    m, kv = _kv(pages=64, per_seq=64)
+    L._call("laser_kv_add_seq", kv, 0, 1000)
+    for mode in (-1, 3):
+        assert _code("laser_model_set_attend_kernel", m, mode) == L.ERR_INVALID_ARG
+    assert _code("laser_model_set_attend_kernel", None, 0) == L.ERR_STATE
+    for mode in (0, 1, 2):
+        L._call("laser_model_set_attend_kernel", m, mode)
+        code, nb = _bytes(kv, [L.attend_span(0, 400, 600)])
+        assert code == L.OK and nb % 4 == 0
