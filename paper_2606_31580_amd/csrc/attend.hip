@@ -15,8 +15,8 @@
 // the second takes P^T as the first leaves it in its accumulators: which position stands in which slot
 // of the contraction is free, as long as V is read in the same order.
 // Types: K and V as bf16 (bf16, E4M3 and 8-bit integers are exact in it; an integer row's scale goes
-// onto the scores, and onto the weights).  bf16 queries are exact; the weights are rounded to bf16, a
-// relative 2^-9 each beside the 2^-9 of the bf16 output.  With fp32 queries and output, queries and weights
+// onto the scores, and onto the weights).  bf16 queries are exact; the weights are rounded to bf16, each off
+// by at most 2^-8 of itself, as the bf16 output is anyway.  With fp32 queries and output, queries and weights
 // (and fp32 K and V) are split into three bf16 parts, which hold all 24 bits.  m, l, O: fp32.
 // A key that a row does not see may hold anything: its score is replaced, an integer row's weight too
 // (whatever the scale), and where the stored V itself can be infinite or NaN, pages that not every
@@ -147,7 +147,7 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // one of a pair is infi
 // pages; each of its 4 waves walks a run of pages by itself, straight from memory into operands (the
 // page layout makes every load contiguous), two pages ahead of the pair that it computes; no barrier
 // until the waves' (m, l, O) are joined in LDS.
-// INT8, 8B heads, 64 sequences of 3,000-14,000 positions: 195 us, 5.9 TB/s (a copy reaches 5.07); 7B heads, one
+// INT8, 8B heads, 64 sequences of 3,000-14,000 positions: 192 us, 6.0 TB/s (a copy reaches 5.07); 7B heads, one
 // sequence of 14,336: 10.2 us with the join, mostly latency: a round of loads each for the arguments, the queries
 // and the first pages, some 1 us per pair of pages, the join's launch.  Workgroups of 8 waves were slower
 // at every size measured (12.1 and 208 us there), and so was a third pair in flight.
@@ -515,8 +515,8 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
 // 16 positions are one contraction step of the second product.
 // Bound by matrix and vector instructions together, which a SIMD overlaps only in part (32 rows x 64
 // positions: 32 matrix instructions of 32 cycles, some 270 vector ones).  4,096 rows of 32 heads behind
-// 12,288 positions, INT8: 1.00-1.03 ms, 930-960 TFLOP/s, where a large bf16 matrix product reaches 1,200-1,370;
-// 1.73 ms with the row kernel.  What it took: accumulators that no rare branch copies (1.28 -> 1.07 ms),
+// 12,288 positions, INT8: 1.00-1.14 ms from card to card, 840-960 TFLOP/s, where a large bf16 matrix product reaches
+// 1,200-1,370; 1.73 ms with the row kernel.  What it took: accumulators that no rare branch copies (1.28 -> 1.07 ms),
 // operands read six products ahead (4%), integer V scales inside the exponent (3%).
 // fp32 rows: 3 parts of each query and weight, the same 32 columns.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -990,8 +990,11 @@ static hipError_t launch_kind(int kind, const AttendArgs& a, hipStream_t s) {
     if constexpr (sizeof(KT) <= 2) return launch_k(k_attend_tile<KT, IT, HD>, grid, dim3(512), s, a);
     return hipErrorInvalidValue;
   }
-  if (kind == 0) return launch_k(k_attend_rows<KT, IT, HD, 1>, grid, block, s, a);
-  return launch_k(k_attend_rows<KT, IT, HD, 2>, grid, block, s, a);
+  if (kind == 1) {
+    if constexpr (sizeof(KT) <= 2 && sizeof(IT) == 2) return launch_k(k_attend_rows<KT, IT, HD, 2>, grid, block, s, a);
+    return hipErrorInvalidValue;
+  }
+  return launch_k(k_attend_rows<KT, IT, HD, 1>, grid, block, s, a);
 }
 
 hipError_t launch_attend(int kind, int kv_type, int io, int hd, const AttendArgs& a, hipStream_t s) {
