@@ -2258,7 +2258,7 @@ laser_status check_rows(const laser_rows* r, const char* what, int heads, int hd
   if (written) {  // no element twice: rows within heads, or heads within rows, or one of either
     const int64_t h = r->head_stride, w = r->row_stride;
     const bool heads_in = (heads == 1 || h >= hd) && (r->rows <= 1 || w >= (heads - 1) * h + hd);
-    const bool rows_in = (r->rows <= 1 || w >= hd) && (heads == 1 || h >= (int64_t)(r->rows - 1) * w + hd);
+    const bool rows_in = (r->rows <= 1 || w >= hd) && (heads == 1 || (h >= hd && (r->rows <= 1 || r->rows - 1 <= (h - hd) / w)));
     if (!heads_in && !rows_in) return laser_fail(LASER_ERR_INVALID_ARG, "%s: written rows overlap", what);
   }
   return LASER_OK;

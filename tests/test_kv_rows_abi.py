@@ -133,6 +133,19 @@ def test_rows_refusals(fn):
     assert _write(odd, ok, good, good, fn=fn) == L.ERR_UNSUPPORTED
 
 
+def test_overlap_of_far_rows():
+    """rows - 1 times a row stride of 2^40 passes 64 bits: not taken for rows that lie within heads."""
+    _, kv = _kv()
+    L._call("laser_kv_add_seq", kv, 0, 40)
+    run = [L.kv_run(0, 0, 1)]
+    also = _rows(4, 2, ptr=2 * PTR)
+    # two heads 2^39 apart, rows 2^40 apart: apart; rows 2^38 apart: row 2 of head 0 is row 0 of head 1
+    assert _write(kv, run, _rows(2 ** 30, 2, row=2 ** 40, head=2 ** 39), also, fn="laser_kv_read") == L.ERR_STATE
+    assert _write(kv, run, _rows(2 ** 25 + 1, 2, row=2 ** 39, head=2 ** 40), also, fn="laser_kv_read") == L.ERR_INVALID_ARG
+    assert _write(kv, run, _rows(3, 2, row=2 ** 38, head=2 ** 39), also, fn="laser_kv_read") == L.ERR_INVALID_ARG
+    assert _write(kv, run, _rows(2, 2, row=2 ** 38, head=2 ** 39), also, fn="laser_kv_read") == L.ERR_STATE
+
+
 def test_write_into_a_shared_page_is_refused():
     _, kv = _kv()
     L._call("laser_kv_add_seq", kv, 0, 32)
