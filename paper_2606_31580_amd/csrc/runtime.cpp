@@ -2452,6 +2452,8 @@ static laser_status attend(laser_kv* kv, int layer, int n_spans, const laser_att
   if (st == LASER_OK) st = check_rows(o, "o", d.n_q_heads, d.head_dim, true);
   if (st != LASER_OK) return st;
   if (q->dtype != o->dtype) return laser_fail(LASER_ERR_UNSUPPORTED, "q and o are of different types");
+  if (q->ptr == o->ptr && (q->row_stride != o->row_stride || q->head_stride != o->head_stride))
+    return laser_fail(LASER_ERR_INVALID_ARG, "o is q's memory with other strides");
   if ((uintptr_t)d_lse % 4) return laser_fail(LASER_ERR_INVALID_ARG, "lse is not aligned");
   AttendJob job;
   st = plan_attend_call(kv, n_spans, spans, q->dtype, causal, window, job);

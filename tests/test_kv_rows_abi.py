@@ -196,6 +196,17 @@ def test_attend_refusals():
     assert _attend(None, ok, good, good) == L.ERR_STATE
 
 
+def test_attend_in_place_wants_the_same_strides():
+    _, kv = _kv()
+    L._call("laser_kv_add_seq", kv, 0, 40)
+    span = [L.attend_span(0, 4, 10)]
+    q = _rows(64, 4)
+    assert _attend(kv, span, q, _rows(64, 4)) == L.ERR_STATE and "finalized" in _msg()
+    assert _attend(kv, span, q, _rows(64, 4, row=512)) == L.ERR_INVALID_ARG
+    assert _attend(kv, span, q, _rows(64, 4, row=64, head=64 * 64)) == L.ERR_INVALID_ARG
+    assert _attend(kv, span, q, _rows(64, 4, row=512, ptr=2 * PTR)) == L.ERR_STATE
+
+
 def test_attend_workspace():
     """Short keys need none; long ones (rows + 2) floats per row, head and split; a call without it is refused."""
     _, kv = _kv(pages=64, per_seq=64)
