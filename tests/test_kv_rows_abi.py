@@ -192,7 +192,7 @@ def test_attend_refusals():
     refused(L.ERR_INVALID_ARG, o=_rows(64, 4, row=128))
     refused(L.ERR_UNSUPPORTED, o=_rows(64, 4, dtype=L.DTYPE_F32))
     refused(L.ERR_UNSUPPORTED, q=_rows(64, 4, dtype=L.DTYPE_INT8), o=_rows(64, 4, dtype=L.DTYPE_INT8))
-    refused(L.ERR_STATE, q=_rows(64, 4, row=0, head=0))  # (queries may be broadcast)
+    refused(L.ERR_STATE, q=_rows(64, 4, row=0, head=0), o=_rows(64, 4, ptr=2 * PTR))  # (queries may be broadcast)
     assert _attend(None, ok, good, good) == L.ERR_STATE
 
 
