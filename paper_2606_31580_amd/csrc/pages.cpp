@@ -1,6 +1,7 @@
 // Paged KV bookkeeping (host) and the laser_pages_* C ABI over it.
 #include "pages.hpp"
 
+#include <algorithm>
 #include <new>
 
 #include "laser.h"
@@ -55,6 +56,12 @@ int PagePool::append(int seq, int n, std::vector<PageUpdate>* upd) {
   if (pages_for(lens_[seq] + n) > max_pages_per_seq_)
     return laser_fail(LASER_ERR_INVALID_ARG, "seq %d would exceed max_pages_per_seq", seq);
   if (need > (int)free_.size()) return laser_fail(LASER_ERR_OUT_OF_PAGES, "need %d pages, %d free", need, (int)free_.size());
+  // (room first: an allocation that fails leaves everything as it is)
+  auto room = [&](auto& v) {
+    if (v.capacity() - v.size() < (size_t)need) v.reserve(v.size() + std::max<size_t>(need, v.size()));
+  };
+  if (upd) room(*upd);
+  room(tables_[seq]);
   for (int i = 0; i < need; ++i) {
     int p = take_lowest();
     if (upd) upd->push_back({seq, (int)tables_[seq].size(), p});

@@ -2198,14 +2198,24 @@ extern "C" laser_status laser_confidence(laser_model* m, const float* d_p, int T
 
 extern "C" laser_status laser_kv_append(laser_kv* kv, int seq_id, int n_tokens) {
   if (!kv_of(kv)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed kv");
+  if (!handle_live(kv->m)) return laser_fail(LASER_ERR_STATE, "the cache's model is destroyed");
   if (kv->pool.live(seq_id) && n_tokens > kv->m->desc.max_positions - kv->pool.len(seq_id))
     return laser_fail(LASER_ERR_INVALID_ARG, "seq %d would exceed max_positions", seq_id);
-  return (laser_status)kv->pool.append(seq_id, n_tokens, &kv->pending);
+  try {
+    return (laser_status)kv->pool.append(seq_id, n_tokens, &kv->pending);
+  } catch (const std::bad_alloc&) {
+    return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
+  }
 }
 
 extern "C" laser_status laser_kv_truncate(laser_kv* kv, int seq_id, int length) {
   if (!kv_of(kv)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed kv");
-  const laser_status st = (laser_status)kv->pool.truncate(seq_id, length);
+  laser_status st;
+  try {
+    st = (laser_status)kv->pool.truncate(seq_id, length);
+  } catch (const std::bad_alloc&) {
+    return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
+  }
   // table rows past the length that have not been sent are void (see laser_kv_free_seq)
   if (st == LASER_OK && !kv->pending.empty())
     kv->pending.erase(std::remove_if(kv->pending.begin(), kv->pending.end(),

@@ -78,6 +78,14 @@ def test_append_and_truncate():
     assert _code("laser_kv_truncate", None, 0, 1) == L.ERR_STATE
 
 
+def test_append_after_the_model_is_gone():
+    m, kv = _kv()
+    L._call("laser_kv_add_seq", kv, 0, 15)
+    L._call("laser_model_destroy", m)
+    assert _code("laser_kv_append", kv, 0, 1) == L.ERR_STATE
+    L._call("laser_kv_truncate", kv, 0, 3)  # (host bookkeeping alone)
+
+
 def _write(kv, runs, k, v, layer=0, fn="laser_kv_write"):
     arr = (L.laser_kv_run * max(1, len(runs)))(*runs)
     return _code(fn, kv, layer, len(runs), arr, C.byref(k), C.byref(v), None)
