@@ -2365,6 +2365,9 @@ struct AttendJob {
   uint64_t parts = 0;
 };
 
+// Workgroups of a launch (a grid has fewer than 2^32 threads).
+uint64_t attend_max_wgs(int kind) { return ((uint64_t)1 << 32) / (kind == 2 ? 512 : 256); }
+
 laser_status plan_attend_call(const laser_kv* kv, int n_spans, const laser_attend_span* spans, int io, int causal, int window,
                               AttendJob& job) {
   const laser_model* m = kv->m;
@@ -2394,7 +2397,7 @@ laser_status plan_attend_call(const laser_kv* kv, int n_spans, const laser_atten
     AttendSize z{};
     z.n = a.n;
     z.pages = hi > lo ? (int)((hi + kPage - 1) / kPage - lo / kPage) : 0;
-    z.rows_pages = causal ? a.n / kPage : 0;
+    z.rows_pages = causal ? (int)(std::max<int64_t>(hi - std::min<int64_t>(a.ke, (int64_t)a.pos + 1), 0) / kPage) : 0;
     job.sp.push_back(a);
     job.size.push_back(z);
   }
@@ -2402,6 +2405,9 @@ laser_status plan_attend_call(const laser_kv* kv, int n_spans, const laser_atten
               io == LASER_DTYPE_BF16, m->attend_kernel);
   for (size_t i = 0; i < job.sp.size(); ++i) {
     job.sp[i].nsplit = job.size[i].nsplit;
+    const uint64_t rows = (uint64_t)job.sp[i].n * d.n_q_heads, wgs = (uint64_t)job.size[i].tiles * job.size[i].nsplit * d.n_kv_heads;
+    if (wgs >= attend_max_wgs(job.size[i].kind) || (job.size[i].nsplit > 1 && rows >= attend_max_wgs(0)))
+      return laser_fail(LASER_ERR_UNSUPPORTED, "too many rows in a span");
     if (job.size[i].nsplit > 1) {
       job.sp[i].part0 = (unsigned)job.parts;
       job.parts += (uint64_t)job.sp[i].n * d.n_q_heads * job.size[i].nsplit;
@@ -2528,13 +2534,12 @@ static laser_status attend(laser_kv* kv, int layer, int n_spans, const laser_att
         if (merge ? x.nsplit == 1 || (x.nsplit <= few_splits) != few : job.size[i].kind != pass) continue;
         const uint64_t rows = (uint64_t)x.n * d.n_q_heads, per = few ? 1024 / d.head_dim : 1;
         const uint64_t mine = merge ? (rows + per - 1) / per : (uint64_t)job.size[i].tiles * x.nsplit;
-        if (a.n_spans > 0 && ((items + mine) * heads) >> 31) break;
+        if ((items + mine) * heads >= attend_max_wgs(pass)) break;  // (one span fits: plan_attend_call)
         a.sp[a.n_spans] = x;
         a.sp[a.n_spans++].first = (unsigned)items;
         items += mine;
       }
       if (a.n_spans == 0) break;
-      if ((items * heads) >> 31) return laser_fail(LASER_ERR_UNSUPPORTED, "too many rows in a span");
       a.n_items = (unsigned)items;
       HIP_TRY(timed(m, LASER_K_ATTN, s, [&] {
         return merge ? launch_attend_merge(io, d.head_dim, few, a, s) : launch_attend(pass, kv_type_of(m), io, d.head_dim, a, s);

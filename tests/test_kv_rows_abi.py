@@ -237,6 +237,20 @@ def test_attend_workspace():
     assert _bytes(kv, [S(3, 1, 0)])[0] == L.ERR_INVALID_ARG
 
 
+def test_attend_rows_beyond_a_grid():
+    """A launch has fewer than 2^32 threads: 2^26 rows of 2 heads per kv head are 2^23 tiles of 16 columns, 2 kv heads,
+    256 threads.  Refused before anything is launched."""
+    _, kv = _kv("f32")
+    L._call("laser_kv_add_seq", kv, 0, 40)
+    most = [L.attend_span(0, 2 ** 26 - 16, 0, kv_end=8)]
+    assert _bytes(kv, most, L.DTYPE_F32)[0] == L.OK
+    q, ws = _rows(2 ** 26, 4, dtype=L.DTYPE_F32), _bytes(kv, most, L.DTYPE_F32)[1]
+    assert ws == 0 and _attend(kv, most, q, q) == L.ERR_STATE and "finalized" in _msg()
+    over = [L.attend_span(0, 2 ** 26, 0, kv_end=8)]
+    assert _bytes(kv, over, L.DTYPE_F32)[0] == L.ERR_UNSUPPORTED and "too many rows" in _msg()
+    assert _attend(kv, over, q, q) == L.ERR_UNSUPPORTED
+
+
 def test_attend_kernel_modes():
     m, kv = _kv(pages=64, per_seq=64)
     L._call("laser_kv_add_seq", kv, 0, 1000)
