@@ -43,11 +43,14 @@ inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256;
 // A span of up to 32 pages stays whole, since joining splits is a launch of its own, up to 64 where there
 // are spans enough to fill the CUs (64 sequences of 50-600 positions: 18.2 us split, 14.4 whole) or rows enough to
 // make the join long.
+// All splits together are at most 64 workgroups per CU beyond one per tile: more rounds than that even out nothing, and
+// the partials (8 or 17 KB per workgroup) stay below some 300 MB however many rows a call has (16 per CU cost 4%
+// at 128 sequences of 3,000-14,000 and 256 of 1,000-6,000 positions).
 // Tile kernel: see tile_splits.
 inline int tile_splits(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus);
 // mode: 0 the kernels as above, 1 only row kernels, 2 the tile kernel wherever it can be (laser_model_set_attend_kernel).
 inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool io16, int mode) {
-  int64_t work = 0, wide = 0;
+  int64_t work = 0, wide = 0, wgs = 0;
   for (int i = 0; i < n; ++i) {
     const int64_t cols = (int64_t)s[i].n * (q_heads / kv_heads);
     if (cols > kAttendFewCols) wide += (int64_t)attend_ceil(cols, 32) * kv_heads * (s[i].pages - s[i].rows_pages / 2);
@@ -57,16 +60,19 @@ inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd,
     const int64_t cols = (int64_t)s[i].n * (q_heads / kv_heads);
     s[i].kind = cols > kAttendFewCols && tiles ? 2 : es == 4 || cols <= 16 || !io16 ? 0 : 1;
     s[i].tiles = attend_ceil(cols, attend_cols(s[i].kind));
-    if (s[i].kind != 2) work += (int64_t)s[i].pages * s[i].tiles * kv_heads;
+    if (s[i].kind == 2) continue;
+    work += (int64_t)s[i].pages * s[i].tiles * kv_heads;
+    wgs += (int64_t)s[i].tiles * kv_heads;
   }
   const int two = attend_ceil(work, (int64_t)cus * 8);  // pages per wave, two workgroups per CU
   const int run = two <= (es == 1 ? 4 : 8) ? std::max(2, attend_ceil(work, (int64_t)cus * 4)) : std::min(two, 32);
+  const int most = std::max(1, attend_ceil(64 * (int64_t)cus, std::max<int64_t>(wgs, 1)));
   const int tile = tile_splits(s, n, kv_heads, q_heads, hd, cus);
   for (int i = 0; i < n; ++i) {
     if (s[i].kind == 2)
       s[i].nsplit = std::max(1, std::min(tile, s[i].pages / 4));
     else
-      s[i].nsplit = s[i].pages <= (two >= 4 || (int64_t)s[i].n * q_heads > 512 ? 64 : 32) ? 1 : std::min(128, attend_ceil(s[i].pages, 4 * run));
+      s[i].nsplit = s[i].pages <= (two >= 4 || (int64_t)s[i].n * q_heads > 512 ? 64 : 32) ? 1 : std::min({128, attend_ceil(s[i].pages, 4 * run), most});
   }
 }
 

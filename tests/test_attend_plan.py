@@ -78,6 +78,15 @@ def test_short_keys_and_full_cards_are_not_split(plan):
         assert plan([span(512, 512)], mode=mode)[0][::2] == (kind, 1)
 
 
+def test_partials_are_bounded(plan):
+    """However many rows a call has, its splits are at most 64 workgroups per CU beyond one per tile."""
+    for es, io16, mode in ((4, 0, 0), (1, 1, 1), (2, 0, 1), (1, 1, 0)):
+        for spans in ([(200000, 4000, 0)], [(20000, 4000, 10)] * 3, [(900, 3000, 0)] * 20, [(1, 4000, 0)] * 200, [(7, 900, 0)] * 900):
+            got = plan(spans, 28, 4, es=es, io16=io16, mode=mode)
+            tiles = sum(t * 4 for _, t, _ in got)
+            assert sum(t * 4 * s for _, t, s in got) <= tiles + 64 * 256, (es, io16, spans[0], got[0])
+
+
 def test_tiles_pay_from_some_work_on(plan):
     """Prompts of a few hundred rows through row kernels, long ones and chunks behind long contexts through tiles."""
     for n, end, kind in ((64, 64, 1), (512, 512, 1), (2048, 2048, 2), (512, 14000, 2), (4096, 16384, 2)):
