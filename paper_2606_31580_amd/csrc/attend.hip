@@ -140,6 +140,13 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // one of a pair is infi
 
 }  // namespace
 
+// A piece of a page that other workgroups read as well (SH: it stays in the caches), or none.
+template <bool SH, class T>
+__device__ __forceinline__ T ld_page(const char* p) {
+  if constexpr (SH) return *(global_ptr<T>)p;
+  return __builtin_nontemporal_load((global_ptr<T>)p);
+}
+
 // ---------------------------------------------------------------------------------- few columns
 // One token per sequence, or a few: every position's K and V comes once from memory and is used for
 // at most 32 columns, so memory bounds it (8-bit keys at 14k positions: 8.4 KB per page and kv head
@@ -151,7 +158,12 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // one of a pair is infi
 // sequence of 14,336: 10.2 us with the join, mostly latency: a round of loads each for the arguments, the queries
 // and the first pages, some 1 us per pair of pages, the join's launch.  Workgroups of 8 waves were slower
 // at every size measured (12.1 and 208 us there), and so was a third pair in flight.
-template <class KT, class IT, int HD, int NT>
+// SH: a span of the launch has several tiles.  They read the same pages, so these stay in the caches (without SH every
+// load is non-temporal: 33 sequences of 3,000-14,000 positions, 16 rows, two tiles, 219 us; 195 so; 1,000 rows of an fp32
+// pool behind 8,000 positions 125 and 92 us), and the tiles of a page share an XCD (8 rows of the 7B heads behind
+// 14,001, bf16 pool, 18.7 and 15.8 us).  Where each page is read once, cached loads cost 7%: 32 sequences, 5 rows, 94
+// us against 87.
+template <class KT, class IT, int HD, int NT, bool SH>
 __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
   constexpr int PARTS = std::is_same_v<IT, float> ? 3 : 1;    // of a query or weight
   constexpr int KP = std::is_same_v<KT, float> ? 3 : 1;       // of a key or value
@@ -163,13 +175,19 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
   __shared__ float s_m[4 * NC], s_l[4 * NC];
 
   const unsigned item = blockIdx.x / (unsigned)a.hkv;
-  const int kvh = (int)(blockIdx.x - item * a.hkv);
   const AttendSpan sp = item_span(a.n_spans, item);
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
   const int lc = l & 15, lg = l >> 4;
-  const int ncol = sp.n * a.G, tiles = (ncol + NC - 1) / NC;
-  const int local = (int)(item - sp.first), split = local / tiles;
-  const int tile = tiles - 1 - (local - split * tiles);  // (the last tile has the most keys: first)
+  const int ncol = sp.n * a.G;
+  int split = (int)(item - sp.first), kvh = (int)(blockIdx.x - item * a.hkv), tile = 0;
+  if constexpr (SH) {  // the tiles that read the same pages are 8 workgroups apart, on one XCD and its L2
+    const int tiles = (ncol + NC - 1) / NC, block = split * a.hkv + kvh, group = block / (8 * tiles);
+    const int rest = block - group * 8 * tiles, across = min(8, sp.nsplit * a.hkv - 8 * group), nth = rest / across;
+    const int pair = 8 * group + rest - nth * across;
+    split = pair / a.hkv;
+    kvh = pair - split * a.hkv;
+    tile = tiles - 1 - nth;  // (the last tile has the most keys: first)
+  }
   const int col0 = tile * NC;
   const int row_a = col0 / a.G, row_b = min(col0 + NC, ncol) - 1;  // first row, last column
   const int row_z = row_b / a.G;                                   // last row
@@ -238,9 +256,9 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
       for (int s = 0; s < NS; ++s)
 #pragma unroll
         for (int y = 0; y < KW; ++y)
-          b.k[x][s][y] = __builtin_nontemporal_load((global_ptr<KRaw>)(kb + (s * 512 + 8 * l) * ES + 16 * y));
+          b.k[x][s][y] = ld_page<SH, KRaw>(kb + (s * 512 + 8 * l) * ES + 16 * y);
 #pragma unroll
-      for (int d = 0; d < ND; ++d) b.v[x][d] = __builtin_nontemporal_load((global_ptr<VRaw>)(vb + (d * 256 + 4 * l) * ES));
+      for (int d = 0; d < ND; ++d) b.v[x][d] = ld_page<SH, VRaw>(vb + (d * 256 + 4 * l) * ES);
       if constexpr (I8) {
         b.ks[x] = ld_global<f32x4>((const char*)a.kpool + a.scales + slot * 64 + 16 * lg);
         b.vs[x] = ld_global<f32x4>((const char*)a.vpool + a.scales + slot * 64 + 16 * lg);
@@ -991,10 +1009,13 @@ static hipError_t launch_kind(int kind, const AttendArgs& a, hipStream_t s) {
     return hipErrorInvalidValue;
   }
   if (kind == 1) {
-    if constexpr (sizeof(KT) <= 2 && sizeof(IT) == 2) return launch_k(k_attend_rows<KT, IT, HD, 2>, grid, block, s, a);
+    if constexpr (sizeof(KT) <= 2 && sizeof(IT) == 2)
+      return a.shared ? launch_k(k_attend_rows<KT, IT, HD, 2, true>, grid, block, s, a)
+                      : launch_k(k_attend_rows<KT, IT, HD, 2, false>, grid, block, s, a);
     return hipErrorInvalidValue;
   }
-  return launch_k(k_attend_rows<KT, IT, HD, 1>, grid, block, s, a);
+  return a.shared ? launch_k(k_attend_rows<KT, IT, HD, 1, true>, grid, block, s, a)
+                  : launch_k(k_attend_rows<KT, IT, HD, 1, false>, grid, block, s, a);
 }
 
 hipError_t launch_attend(int kind, int kv_type, int io, int hd, const AttendArgs& a, hipStream_t s) {

@@ -348,6 +348,7 @@ struct AttendArgs {
   float* part;       // partial outputs [partial][hd]
   float* ml;         // their (m, l)
   int n_spans;
+  int shared;        // row kernels: a span has several tiles, which read the same pages
   unsigned n_items;
   AttendSpan sp[kAttendSpans];
 };

@@ -2527,7 +2527,7 @@ static laser_status attend(laser_kv* kv, int layer, int n_spans, const laser_att
     const bool merge = pass >= kAttendKinds, few = pass == kAttendKinds + 1;
     const int heads = merge ? 1 : d.n_kv_heads;  // workgroups per item
     for (size_t i = 0; i < job.sp.size();) {
-      a.n_spans = 0;
+      a.n_spans = a.shared = 0;
       uint64_t items = 0;
       for (; i < job.sp.size() && a.n_spans < kAttendSpans; ++i) {
         const AttendSpan& x = job.sp[i];
@@ -2535,6 +2535,7 @@ static laser_status attend(laser_kv* kv, int layer, int n_spans, const laser_att
         const uint64_t rows = (uint64_t)x.n * d.n_q_heads, per = few ? 1024 / d.head_dim : 1;
         const uint64_t mine = merge ? (rows + per - 1) / per : (uint64_t)job.size[i].tiles * x.nsplit;
         if ((items + mine) * heads >= attend_max_wgs(pass)) break;  // (one span fits: plan_attend_call)
+        a.shared |= job.size[i].tiles > 1;
         a.sp[a.n_spans] = x;
         a.sp[a.n_spans++].first = (unsigned)items;
         items += mine;
