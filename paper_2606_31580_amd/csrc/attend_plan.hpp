@@ -24,7 +24,7 @@ inline int attend_ceil(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 // Columns (rows x query heads of a kv head) of a tile of each kernel.
 inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256; }
 
-// es: bytes of a cached element; io16: 16-bit rows.  fp32 pools have only the row kernel with 16 columns,
+// es: bytes of a cached element (i8: integers); io16: 16-bit rows.  fp32 pools have only the row kernel with 16 columns,
 // and fp32 rows not the one with 32 (three parts of everything would not fit the registers).
 //
 // The tile kernel converts a page once for 256 columns and not for 32, but has 8 times fewer, longer workgroups: it
@@ -32,6 +32,12 @@ inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256;
 // prompt of 512 rows, 28 per CU, 26.2 and 15.8, of 1,024, 112, 41 and 34, of 2,048, 450, 68 and 84; 512 rows
 // behind 2,000 positions, 246, 44 and 57; bf16 pools: 20 rows behind 14,000, 68, 24 and 32; fp32 rows: a prompt of
 // 1,024 70 and 49, of 2,048 137 and 139).
+// A tile takes about as long with few of its 256 columns in use as with all, a row kernel as many times longer as it
+// has tiles: a span goes through tiles if these are filled to 6 of 8 parts with INT8 pools and bf16 rows, 4 with E4M3
+// or bf16 pools; fp32 rows: 7.5 with 8-bit pools, 6 with bf16 (us, tiles and rows, 8B heads, 16 sequences of
+// 1,000-9,000: INT8, 80 columns, 3 parts, 126 and 91, 192, 6, 140 and 142, 240, 8, 148 and 178; E4M3, 4, 114 and 129;
+// bf16, 3, 124 and 117, 4, 131 and 131; fp32 rows: INT8, 5, 325 and 200, a chunk of 1,000 rows 254 and 296; bf16,
+// 5, 254 and 247, 8, 275 and 388).
 //
 // Row kernels: pages per wave.  Every CU runs one workgroup of 4 waves, or two on 8-bit pools (fewer
 // registers).  Long runs stream best when two workgroups per CU share the pages; where that leaves a wave only
@@ -49,16 +55,20 @@ inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256;
 // Tile kernel: see tile_splits.
 inline int tile_splits(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus);
 // mode: 0 the kernels as above, 1 only row kernels, 2 the tile kernel wherever it can be (laser_model_set_attend_kernel).
-inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool io16, int mode) {
+inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool i8, bool io16, int mode) {
   int64_t work = 0, wide = 0, wgs = 0;
+  const int half_parts = io16 ? (i8 ? 12 : 8) : (es == 1 ? 15 : 12);
+  auto fills = [&](int64_t cols) {  // tiles filled far enough
+    return cols > kAttendFewCols && (mode == 2 || 2 * (int64_t)attend_ceil(cols, 32) >= half_parts * (int64_t)attend_ceil(cols, 256));
+  };
   for (int i = 0; i < n; ++i) {
     const int64_t cols = (int64_t)s[i].n * (q_heads / kv_heads);
-    if (cols > kAttendFewCols) wide += (int64_t)attend_ceil(cols, 32) * kv_heads * (s[i].pages - s[i].rows_pages / 2);
+    if (fills(cols)) wide += (int64_t)attend_ceil(cols, 32) * kv_heads * (s[i].pages - s[i].rows_pages / 2);
   }
   const bool tiles = es <= 2 && mode != 1 && (mode == 2 || wide > (int64_t)cus * (io16 ? (es == 1 ? 130 : 60) : 300));
   for (int i = 0; i < n; ++i) {
     const int64_t cols = (int64_t)s[i].n * (q_heads / kv_heads);
-    s[i].kind = cols > kAttendFewCols && tiles ? 2 : es == 4 || cols <= 16 || !io16 ? 0 : 1;
+    s[i].kind = tiles && fills(cols) ? 2 : es == 4 || cols <= 16 || !io16 ? 0 : 1;
     s[i].tiles = attend_ceil(cols, attend_cols(s[i].kind));
     if (s[i].kind == 2) continue;
     work += (int64_t)s[i].pages * s[i].tiles * kv_heads;

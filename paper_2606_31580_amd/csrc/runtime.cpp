@@ -2401,7 +2401,7 @@ laser_status plan_attend_call(const laser_kv* kv, int n_spans, const laser_atten
     job.sp.push_back(a);
     job.size.push_back(z);
   }
-  plan_attend(job.size.data(), (int)job.size.size(), d.n_q_heads, d.n_kv_heads, d.head_dim, m->cus, m->kv_es,
+  plan_attend(job.size.data(), (int)job.size.size(), d.n_q_heads, d.n_kv_heads, d.head_dim, m->cus, m->kv_es, m->kv_i8 != 0,
               io == LASER_DTYPE_BF16, m->attend_kernel);
   for (size_t i = 0; i < job.sp.size(); ++i) {
     job.sp[i].nsplit = job.size[i].nsplit;

@@ -12,11 +12,11 @@ MAIN = """
 #include <vector>
 #include "attend_plan.hpp"
 int main() {
-  int n, hq, hkv, hd, cus, es, io16, mode;
-  while (std::scanf("%d %d %d %d %d %d %d %d", &n, &hq, &hkv, &hd, &cus, &es, &io16, &mode) == 8) {
+  int n, hq, hkv, hd, cus, es, i8, io16, mode;
+  while (std::scanf("%d %d %d %d %d %d %d %d %d", &n, &hq, &hkv, &hd, &cus, &es, &i8, &io16, &mode) == 9) {
     std::vector<laser::AttendSize> s(n);
     for (auto& x : s) std::scanf("%d %d %d", &x.n, &x.pages, &x.rows_pages);
-    laser::plan_attend(s.data(), n, hq, hkv, hd, cus, es, io16, mode);
+    laser::plan_attend(s.data(), n, hq, hkv, hd, cus, es, i8, io16, mode);
     for (auto& x : s) std::printf("%d %d %d ", x.kind, x.tiles, x.nsplit);
     std::printf("\\n");
   }
@@ -30,8 +30,8 @@ def plan(tmp_path_factory):
     (d / "main.cpp").write_text(MAIN)
     subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", f"-I{CSRC}", "-o", str(d / "plan"), str(d / "main.cpp")], check=True)
 
-    def call(spans, hq=28, hkv=4, hd=128, cus=256, es=1, io16=1, mode=0):
-        line = f"{len(spans)} {hq} {hkv} {hd} {cus} {es} {io16} {mode} " + " ".join(f"{n} {p} {r}" for n, p, r in spans)
+    def call(spans, hq=28, hkv=4, hd=128, cus=256, es=1, io16=1, mode=0, i8=None):
+        line = f"{len(spans)} {hq} {hkv} {hd} {cus} {es} {int(es == 1 if i8 is None else i8)} {io16} {mode} " + " ".join(f"{n} {p} {r}" for n, p, r in spans)
         out = [int(x) for x in subprocess.run([str(d / "plan")], input=line, capture_output=True, text=True, check=True).stdout.split()]
         return [tuple(out[3 * i:3 * i + 3]) for i in range(len(spans))]
 
@@ -91,3 +91,16 @@ def test_tiles_pay_from_some_work_on(plan):
     """Prompts of a few hundred rows through row kernels, long ones and chunks behind long contexts through tiles."""
     for n, end, kind in ((64, 64, 1), (512, 512, 1), (2048, 2048, 2), (512, 14000, 2), (4096, 16384, 2)):
         assert plan([span(n, end)])[0][0] == kind, (n, end)
+
+
+def test_tiles_are_filled(plan):
+    """Long contexts, so that work is no question: tiles of which few columns are in use go through the row kernels, per span."""
+    def kinds(n, **kw):
+        return [k for k, _, _ in plan([span(n, 9000)] * 16, 32, 8, **kw)]
+    for kw, few, enough in ((dict(), 40, 48), (dict(i8=0), 24, 28), (dict(es=2), 24, 28), (dict(es=2, io16=0), 40, 44),
+                            (dict(io16=0), 50, 64)):
+        assert set(kinds(few, **kw)) <= {0, 1} and set(kinds(enough, **kw)) == {2}, kw
+    assert [k for k, _, _ in plan([span(20, 9000)] * 8 + [span(64, 9000)] * 8, 32, 8)] == [1] * 8 + [2] * 8
+    assert set(kinds(20, mode=2)) == {2}
+    for es, i8, io16 in ((1, 1, 1), (1, 0, 1), (2, 0, 1), (1, 1, 0), (2, 0, 0)):
+        assert plan([span(1000, 8000)], 32, 8, es=es, i8=i8, io16=io16)[0][0] == 2
