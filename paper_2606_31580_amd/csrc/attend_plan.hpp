@@ -24,6 +24,10 @@ inline int attend_ceil(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 // Columns (rows x query heads of a kv head) of a tile of each kernel.
 inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256; }
 
+// Splits of a span of the tile kernel at `run` pages a workgroup, a step of 4 at least.
+inline int tile_split(const AttendSize& s, int run) { return std::max(1, std::min(attend_ceil(s.pages, run), s.pages / 4)); }
+inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus);
+
 // es: bytes of a cached element (i8: integers); io16: 16-bit rows.  fp32 pools have only the row kernel with 16 columns,
 // and fp32 rows not the one with 32 (three parts of everything would not fit the registers).
 //
@@ -52,8 +56,7 @@ inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256;
 // All splits together are at most 64 workgroups per CU beyond one per tile: more rounds than that even out nothing, and
 // the partials (8 or 17 KB per workgroup) stay below some 300 MB however many rows a call has (16 per CU cost 4%
 // at 128 sequences of 3,000-14,000 and 256 of 1,000-6,000 positions).
-// Tile kernel: see tile_splits.
-inline int tile_splits(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus);
+// Tile kernel: see tile_run.
 // mode: 0 the kernels as above, 1 only row kernels, 2 the tile kernel wherever it can be (laser_model_set_attend_kernel).
 inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool i8, bool io16, int mode) {
   int64_t work = 0, wide = 0, wgs = 0;
@@ -77,26 +80,29 @@ inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd,
   const int two = attend_ceil(work, (int64_t)cus * 8);  // pages per wave, two workgroups per CU
   const int run = two <= (es == 1 ? 4 : 8) ? std::max(2, attend_ceil(work, (int64_t)cus * 4)) : std::min(two, 32);
   const int most = std::max(1, attend_ceil(64 * (int64_t)cus, std::max<int64_t>(wgs, 1)));
-  const int tile = tile_splits(s, n, kv_heads, q_heads, hd, cus);
+  const int tile = tile_run(s, n, kv_heads, q_heads, hd, cus);
   for (int i = 0; i < n; ++i) {
     if (s[i].kind == 2)
-      s[i].nsplit = std::max(1, std::min(tile, s[i].pages / 4));
+      s[i].nsplit = tile_split(s[i], tile);
     else
       s[i].nsplit = s[i].pages <= (two >= 4 || (int64_t)s[i].n * q_heads > 512 ? 64 : 32) ? 1 : std::min({128, attend_ceil(s[i].pages, 4 * run), most});
   }
 }
 
-// Splits of the tile kernel's spans (the same for all, but never less than a step of 4 pages each): the
-// number that makes the call shortest, counting 2.2 us for a step of a CU's workgroup, 2 us to start one, the
+// Pages of a workgroup of the tile kernel, the same for all spans (8B heads, INT8, 16 sequences of 1,000-9,000, 60
+// rows: 127 us, 150 with the same number of splits for all): those that make the call shortest, counting 2.2 us for a step of a CU's workgroup, 2 us to start one, the
 // partials written and read at 5 TB/s and 5 us for joining them.
-inline int tile_splits(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus) {
-  int best = 1;
+inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus) {
+  int longest_span = 1, best = 0;
+  for (int i = 0; i < n; ++i)
+    if (s[i].kind == 2) longest_span = std::max(longest_span, s[i].pages);
   double best_us = 1e300;
   for (int k : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+    const int run = attend_ceil(longest_span, k);
     double all = 0, longest = 0, parts = 0, wgs = 0;
     for (int i = 0; i < n; ++i) {
       if (s[i].kind != 2) continue;
-      const int mine = std::max(1, std::min(k, s[i].pages / 4));
+      const int mine = tile_split(s[i], run);
       const double us = 2 + 2.2 * attend_ceil(s[i].pages, 4 * mine);
       const double mean = 2 + 2.2 * (s[i].pages - 0.5 * s[i].rows_pages) / (4.0 * mine);
       const double w = (double)s[i].tiles * kv_heads * mine;
@@ -105,13 +111,13 @@ inline int tile_splits(const AttendSize* s, int n, int kv_heads, int heads, int 
       longest = std::max(longest, us);
       if (mine > 1) parts += (double)s[i].n * heads * mine;
     }
-    if (wgs == 0) return 1;
+    if (wgs == 0) break;
     // workgroups of like length run in whole rounds; many of them even out
     const double rounds = wgs / cus, whole = wgs <= 3.0 * cus ? attend_ceil((int64_t)wgs, cus) : rounds;
     const double us = std::max(all / cus * (whole / rounds > 1 && rounds > 1 ? whole / rounds : 1.0), longest) +
                       (parts > 0 ? 5 + parts * (hd + 2) * 8 / 5e6 : 0);
     if (us < best_us) {
-      best = k;
+      best = run;
       best_us = us;
     }
   }

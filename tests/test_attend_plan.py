@@ -104,3 +104,14 @@ def test_tiles_are_filled(plan):
     assert set(kinds(20, mode=2)) == {2}
     for es, i8, io16 in ((1, 1, 1), (1, 0, 1), (2, 0, 1), (1, 1, 0), (2, 0, 0)):
         assert plan([span(1000, 8000)], 32, 8, es=es, i8=i8, io16=io16)[0][0] == 2
+
+
+def test_ragged_tiles_get_like_shares(plan):
+    """Spans of different lengths: a workgroup's pages differ by less than a factor of two where spans are split."""
+    spans = [span(60, 1000 + 530 * i) for i in range(16)]
+    got = plan(spans, 32, 8)
+    assert {k for k, _, _ in got} == {2}
+    shares = [-(-p // s) for (_, p, _), (_, _, s) in zip(spans, got)]
+    split = [x for x, (_, _, s) in zip(shares, got) if s > 1]
+    assert split and max(shares) <= 2 * min(split)
+    assert got[-1][2] > got[4][2] >= got[0][2]
