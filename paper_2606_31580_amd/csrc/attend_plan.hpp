@@ -38,10 +38,10 @@ inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd,
 // 1,024 70 and 49, of 2,048 137 and 139).
 // A tile takes about as long with few of its 256 columns in use as with all, a row kernel as many times longer as it
 // has tiles: a span goes through tiles if these are filled to 6 of 8 parts with INT8 pools and bf16 rows, 4 with E4M3
-// or bf16 pools; fp32 rows: 7.5 with 8-bit pools, 6 with bf16 (us, tiles and rows, 8B heads, 16 sequences of
-// 1,000-9,000: INT8, 80 columns, 3 parts, 126 and 91, 192, 6, 140 and 142, 240, 8, 148 and 178; E4M3, 4, 114 and 129;
-// bf16, 3, 124 and 117, 4, 131 and 131; fp32 rows: INT8, 5, 325 and 200, a chunk of 1,000 rows 254 and 296; bf16,
-// 5, 254 and 247, 8, 275 and 388).
+// or bf16 pools; fp32 rows: 7.5, 6 with E4M3, 5 with bf16 (us, tiles and rows, 8B heads, 16 sequences of 1,000-9,000:
+// INT8, 120 columns, 4 parts, 122 and 100, 192, 6, 121 and 142; E4M3, 96, 3, 111 and 114, 160, 5, 104 and 153;
+// bf16, 3, 125 and 120, 4, 123 and 131; fp32 rows: INT8, 7, 308 and 252, 8, 308 and 307, a chunk of 1,000 rows 253 and
+// 298; E4M3, 5, 205 and 183, 8, 218 and 278; bf16, 5, 234 and 248).
 //
 // Row kernels: pages per wave.  Every CU runs one workgroup of 4 waves, or two on 8-bit pools (fewer
 // registers).  Long runs stream best when two workgroups per CU share the pages; where that leaves a wave only
@@ -60,7 +60,7 @@ inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd,
 // mode: 0 the kernels as above, 1 only row kernels, 2 the tile kernel wherever it can be (laser_model_set_attend_kernel).
 inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool i8, bool io16, int mode) {
   int64_t work = 0, wide = 0, wgs = 0;
-  const int half_parts = io16 ? (i8 ? 12 : 8) : (es == 1 ? 15 : 12);
+  const int half_parts = io16 ? (i8 ? 12 : 8) : i8 ? 15 : es == 1 ? 12 : 10;
   auto fills = [&](int64_t cols) {  // tiles filled far enough
     return cols > kAttendFewCols && (mode == 2 || 2 * (int64_t)attend_ceil(cols, 32) >= half_parts * (int64_t)attend_ceil(cols, 256));
   };
@@ -90,8 +90,8 @@ inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd,
 }
 
 // Pages of a workgroup of the tile kernel, the same for all spans (8B heads, INT8, 16 sequences of 1,000-9,000, 60
-// rows: 127 us, 150 with the same number of splits for all): those that make the call shortest, counting 2.2 us for a step of a CU's workgroup, 2 us to start one, the
-// partials written and read at 5 TB/s and 5 us for joining them.
+// rows: 127 us, 150 with the same number of splits for all): those that make the call shortest, counting 2.2 us for a step of a CU's workgroup, 5 us to start and end one, the
+// partials written and read at 7 TB/s (mostly from the memory-side cache) and 9 us for joining them (eleven calls with 1 to 32 splits took that, most within 15%).
 inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus) {
   int longest_span = 1, best = 0;
   for (int i = 0; i < n; ++i)
@@ -103,8 +103,8 @@ inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd,
     for (int i = 0; i < n; ++i) {
       if (s[i].kind != 2) continue;
       const int mine = tile_split(s[i], run);
-      const double us = 2 + 2.2 * attend_ceil(s[i].pages, 4 * mine);
-      const double mean = 2 + 2.2 * (s[i].pages - 0.5 * s[i].rows_pages) / (4.0 * mine);
+      const double us = 5 + 2.2 * attend_ceil(s[i].pages, 4 * mine);
+      const double mean = 5 + 2.2 * (s[i].pages - 0.5 * s[i].rows_pages) / (4.0 * mine);
       const double w = (double)s[i].tiles * kv_heads * mine;
       all += w * mean;
       wgs += w;
@@ -112,10 +112,10 @@ inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd,
       if (mine > 1) parts += (double)s[i].n * heads * mine;
     }
     if (wgs == 0) break;
-    // workgroups of like length run in whole rounds; many of them even out
-    const double rounds = wgs / cus, whole = wgs <= 3.0 * cus ? attend_ceil((int64_t)wgs, cus) : rounds;
-    const double us = std::max(all / cus * (whole / rounds > 1 && rounds > 1 ? whole / rounds : 1.0), longest) +
-                      (parts > 0 ? 5 + parts * (hd + 2) * 8 / 5e6 : 0);
+    // workgroups of like length run in whole rounds; many of them even out but for the last
+    const double rounds = wgs / cus;
+    const double busy = wgs > 3.0 * cus ? all / cus + longest / 2 : all / cus * (rounds > 1 ? attend_ceil((int64_t)wgs, cus) / rounds : 1.0);
+    const double us = std::max(busy, longest) + (parts > 0 ? 9 + parts * (hd + 2) * 8 / 7e6 : 0);
     if (us < best_us) {
       best = run;
       best_us = us;

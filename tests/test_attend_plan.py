@@ -97,7 +97,7 @@ def test_tiles_are_filled(plan):
     """Long contexts, so that work is no question: tiles of which few columns are in use go through the row kernels, per span."""
     def kinds(n, **kw):
         return [k for k, _, _ in plan([span(n, 9000)] * 16, 32, 8, **kw)]
-    for kw, few, enough in ((dict(), 40, 48), (dict(i8=0), 24, 28), (dict(es=2), 24, 28), (dict(es=2, io16=0), 40, 44),
+    for kw, few, enough in ((dict(), 40, 48), (dict(i8=0), 24, 28), (dict(es=2), 24, 28), (dict(es=2, io16=0), 32, 40), (dict(i8=0, io16=0), 40, 48),
                             (dict(io16=0), 50, 64)):
         assert set(kinds(few, **kw)) <= {0, 1} and set(kinds(enough, **kw)) == {2}, kw
     assert [k for k, _, _ in plan([span(20, 9000)] * 8 + [span(64, 9000)] * 8, 32, 8)] == [1] * 8 + [2] * 8
