@@ -399,7 +399,8 @@ typedef struct {
  * change with the other spans of the call (they decide how keys are split over workgroups).
  * The workspace (laser_attend_workspace bytes, 16-byte aligned; NULL if 0) holds the partial results of
  * spans whose keys are split; calls that may run at the same time, captured ones included, need
- * workspaces of their own.  A sequence may be in several spans; a row may not (INVALID_ARG). */
+ * workspaces of their own.  A sequence may be in several spans; a row may not (INVALID_ARG).
+ * A span of more rows than a grid's 2^32 threads take is UNSUPPORTED. */
 laser_status laser_attend_workspace(const laser_kv* kv, int n_spans, const laser_attend_span* spans, int dtype, int causal,
                                     int window, size_t* bytes);
 laser_status laser_attend(laser_kv* kv, int layer, int n_spans, const laser_attend_span* spans, float scale, int causal,
