@@ -466,3 +466,19 @@ def test_random_calls(seed):
         spans.append(L.attend_span(s, n, pos, row0=at, kv_begin=lo, kv_end=hi))
         at += n + int(rng.integers(0, 3))
     check_device(kv, io, spans, queries(rng, at + 1, hq, hd, io), causal=causal, window=window, hkv=hkv)
+
+
+@pytest.mark.parametrize("kernels", [ROWS], indirect=True, ids=["rows"])
+@pytest.mark.parametrize("hq,hkv,hd", [(15, 3, 128), (10, 5, 128), (28, 4, 128), (16, 8, 64), (11, 11, 64)])
+@pytest.mark.parametrize("kind,io", [("int8", "bf16"), ("bf16", "f32"), ("fp8", "bf16"), ("f32", "f32")])
+def test_tiles_that_read_the_same_pages(hq, hkv, hd, kind, io):
+    """Row kernels, spans of several tiles beside spans of one: workgroups are dealt out so that a page's tiles share an
+    XCD, over numbers of splits and kv heads that no 8 divides."""
+    lens = [2900, 1300, 700, 40]
+    kv = cache(kind, hq, hkv, hd, pages=320, seqs=4, per_seq=190)
+    fill(kv, kind, lens, hkv, hd, 35)
+    rng = np.random.default_rng(36)
+    spans = [L.attend_span(0, 37, 2863), L.attend_span(1, 1, 1299, row0=40), L.attend_span(2, 90, 610, row0=41),
+             L.attend_span(3, 2, 38, row0=131), L.attend_span(0, 9, 2500, row0=133, kv_begin=17, kv_end=2450)]
+    check_device(kv, io, spans, queries(rng, 143, hq, hd, io), hkv=hkv)
+    check_device(kv, io, spans[2:3], queries(rng, 143, hq, hd, io), window=100, hkv=hkv)
