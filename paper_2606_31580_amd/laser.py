@@ -492,6 +492,14 @@ def attend_span(seq: int, n: int, pos: int, row0: int = 0, kv_begin: int = 0, kv
     return laser_attend_span(seq, n, row0, pos, kv_begin, kv_end)
 
 
+def _joined(T, items) -> bytes:
+    """Structures one after another, as C reads them.  (Their bytes joined: an array made of 33 takes 5 us, this 0.6.)"""
+    data = b"".join(items)
+    if len(data) != len(items) * C.sizeof(T):
+        raise TypeError(f"expected a sequence of {T.__name__}")
+    return data
+
+
 _row_dtypes: Dict["object", int] = {}
 
 
@@ -528,7 +536,7 @@ def _kv_rows(fn, kv, layer, runs, k, v, stream):
     arr = rk = rv = None
     if n:
         heads = kv.model.shape.n_kv_heads
-        arr = (laser_kv_run * n)(*runs)
+        arr = _joined(laser_kv_run, runs)
         rk, rv = C.byref(_rows(k, "k", kv, heads)), C.byref(_rows(v, "v", kv, heads))
     _call(fn, kv.h, layer, n, arr, rk, rv, _stream_of(kv, stream))
 
@@ -546,7 +554,7 @@ def laser_kv_read(kv: KVCache, layer: int, runs: Sequence[laser_kv_run], k, v, s
 def laser_attend_workspace(kv: KVCache, spans: Sequence[laser_attend_span], dtype: int = DTYPE_BF16, causal: bool = True,
                            window: int = 0) -> int:
     """Bytes of workspace that laser_attend needs for these spans."""
-    arr = (laser_attend_span * len(spans))(*spans)
+    arr = _joined(laser_attend_span, spans)
     nb = C.c_size_t()
     _call("laser_attend_workspace", kv.h, len(spans), arr, dtype, int(causal), window, C.byref(nb))
     return nb.value
@@ -568,7 +576,7 @@ def laser_attend(kv: KVCache, layer: int, spans: Sequence[laser_attend_span], q,
         if not lse.is_contiguous() or lse.device != q.device:
             raise ValueError("lse: not contiguous, or on another device")
     n = len(spans)
-    arr = (laser_attend_span * n)(*spans)
+    arr = _joined(laser_attend_span, spans)
     if workspace is None:
         nb = C.c_size_t()
         _call("laser_attend_workspace", kv.h, n, arr, rq.dtype, int(causal), window, C.byref(nb))

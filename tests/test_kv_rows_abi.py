@@ -261,3 +261,14 @@ def test_attend_kernel_modes():
         L._call("laser_model_set_attend_kernel", m, mode)
         code, nb = _bytes(kv, [L.attend_span(0, 400, 600)])
         assert code == L.OK and nb % 4 == 0
+
+
+def test_binding_passes_runs_and_spans_whole():
+    runs = [L.kv_run(3, 5, 7, 9), L.kv_run(1, 0, 2)]
+    data = L._joined(L.laser_kv_run, runs)
+    assert list((C.c_int32 * 8).from_buffer_copy(data)) == [3, 5, 7, 9, 1, 0, 2, 0]
+    assert bytes((L.laser_attend_span * 1)(L.attend_span(0, 4, 6))) == L._joined(L.laser_attend_span, (L.attend_span(0, 4, 6),))
+    assert L._joined(L.laser_kv_run, []) == b""
+    for bad in ([L.attend_span(0, 1, 0)], [(0, 1, 2, 3)], [1], [None]):
+        with pytest.raises(TypeError):
+            L._joined(L.laser_kv_run, bad)
