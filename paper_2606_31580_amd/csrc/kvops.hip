@@ -12,9 +12,10 @@
 // every access is of 8 to 32 bytes; the hd / 8 lanes of a row find its amax without LDS.  A workgroup
 // belongs to one run of rows, whose page ids it looks up.
 //
-// Measured within a graph, 14,336 bf16 rows of 8 heads x 128, bytes read and written: into INT8 23.8 us (3.7 TB/s),
-// bf16 29.6 us (4.0), E4M3 17.5 us (5.0); out of INT8 20.6 us (4.3), bf16 24.5 us (4.8), E4M3 20.5 us (4.3).  A copy of
-// 1 GiB reaches 5.1 TB/s.  What INT8 rows cost over E4M3 is the quantisation's arithmetic.  A single row is latency: 3.5 us.
+// Measured within a graph, 14,336 bf16 rows of 8 heads x 128, bytes read and written: into INT8 19.4 us (4.6 TB/s),
+// bf16 29.6 us (4.0), E4M3 17.5 us (5.0); out of INT8 20.1 us (4.4), bf16 24.5 us (4.8), E4M3 20.1 us (4.4).  A copy of
+// 1 GiB reaches 5.1 TB/s.  INT8 was bound by the quantisation's instructions: 23.8 us with a rounding, a clamp and a
+// division per row and lane more.  A single row is latency: 3.5 us.
 #include "device_common.hpp"
 #include "kernels.hpp"
 
@@ -34,43 +35,58 @@ __device__ __forceinline__ uint32_t row_umax(uint32_t v) {
   return v;
 }
 
-// A row's scale, and what its elements are multiplied by and divided by: rows far from 1 are moved by a
+// Largest magnitude of 8 elements, as bits (a NaN is the largest).
+__device__ __forceinline__ uint32_t amax8(const float* x) {
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, fabsf(x[e])), fabsf(x[e + 1]));
+  return __float_as_uint(m) & 0x7fffffffu;
+}
+
+// A row's scale.
+__device__ __forceinline__ float scale_of(uint32_t amax_bits) {
+  const float amax = __uint_as_float(amax_bits);
+  return amax_bits >= 0x7f800000u ? amax : amax / 127.f;
+}
+
+// What a row's elements are multiplied by and divided by: rows far from 1 are moved by a
 // power of two first, so that neither 127 x nor 1 / amax leaves the normal range.
 struct RowScale {
-  float scale, pre, top, inv, off0;
+  float pre, top, inv, off0;
   __device__ __forceinline__ explicit RowScale(uint32_t amax_bits) {
     const float amax = __uint_as_float(amax_bits);
     const float c = amax > 0x1p100f ? 0x1p-32f : (amax < 0x1p-60f ? 0x1p64f : 1.f);
-    scale = amax_bits >= 0x7f800000u ? amax : amax / 127.f;
     pre = 127.f * c;
     top = amax * c;
     const bool small = amax < 0x1p-100f;  // (127 / amax may leave the range: divided)
     inv = amax_bits >= 0x7f800000u || amax == 0.f ? 0.f : small ? 1.f : pre * __builtin_amdgcn_rcpf(top);
     off0 = small ? 1.f : 0.f;
   }
-  // rint(127 x / amax) of 8 elements, packed.  The products with 127 / amax are off by less than 2^-14 steps;
-  // only next to half a step does that matter, and then the division decides.
-  __device__ __forceinline__ void quant8(const float* x, uint32_t* w) const {
-    float q[8], off = off0;
+  // rint(127 x / amax) of 8 elements in the low bytes of t.  The sum of a product with 127 / amax and 1.5 2^23 is rounded
+  // to the integer by itself and has it in its low bits.  127 / amax from the 1-ulp reciprocal is off by less than
+  // 2^-23 + 2^-24 of itself, a product by less than 2^-15 steps; only next to half a step does that matter, and then the
+  // division decides.
+  __device__ __forceinline__ void quant8(const float* x, uint32_t* t) const {
+    constexpr float kInt = 0x1.8p23f;
+    float off = off0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float r = x[e] * inv;
-      q[e] = rintf(r);
-      off = fmaxf(off, fabsf(r - q[e]));
+      const float y = __builtin_fmaf(x[e], inv, kInt);
+      t[e] = __float_as_uint(y);
+      off = fmaxf(off, fabsf(__builtin_fmaf(x[e], inv, kInt - y)));
     }
-    if (off > 0.4999f)
+    if (off > 0.5f - 0x1p-15f)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) q[e] = rintf(x[e] * pre / top);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t b[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) b[e] = (uint32_t)(int)fminf(fmaxf(q[4 * h + e], -127.f), 127.f);
-      const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
-      w[h] = inv == 0.f ? 0u : lo | hi;
-    }
+      for (int e = 0; e < 8; ++e) t[e] = (uint32_t)(int)rintf(x[e] * pre / top);
   }
+  // What the integers of a row without a scale (zeros, NaN, infinities) are taken as: zeros.
+  __device__ __forceinline__ uint32_t keep() const { return inv == 0.f ? 0u : ~0u; }
 };
+
+// The low bytes of four words.
+__device__ __forceinline__ uint32_t low4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(b, a, 0x0c0c0400u) | __builtin_amdgcn_perm(d, c, 0x04000c0cu);
+}
 
 // Four values as E4M3 (to nearest even, saturated at +-448; NaN stays NaN).
 __device__ __forceinline__ uint32_t pk_fp8x4(const float* x) {
@@ -102,7 +118,10 @@ __device__ __forceinline__ Piece<KT> pack(const float* x, const RowScale* rs) {
       p.w[0] = pk_fp8x4(x);
       p.w[1] = pk_fp8x4(x + 4);
     } else {
-      rs->quant8(x, p.w);
+      uint32_t t[8];
+      rs->quant8(x, t);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) p.w[h] = low4(t[4 * h], t[4 * h + 1], t[4 * h + 2], t[4 * h + 3]) & rs->keep();
     }
   }
   return p;
@@ -175,8 +194,8 @@ __device__ __forceinline__ void st_words(char* p, const uint32_t* w) {
 }
 
 // 8 elements of a caller's row (VEC: 16-byte aligned pieces).  Rows of 16 bits are read non-temporally, so
-// that the block lines under assembly stay (14,336 rows x 8 heads x 128 into INT8: 23.8 us, 25.4 without); in fp32 a
-// lane's two loads share lines, and it costs (8,000 rows x 4 heads x 128: 11.5 us, 10.8 without).
+// that the block lines under assembly stay (14,336 rows x 8 heads x 128 into E4M3: 17.5 us, 18.9 without); in fp32 a
+// lane's two loads share lines, and it costs (8,000 rows x 4 heads x 128, INT8: 7% more).
 template <class IT, bool VEC>
 __device__ __forceinline__ void ld_row8(const void* base, int64_t e, float* x) {
   if constexpr (VEC) {
@@ -240,21 +259,25 @@ __global__ __launch_bounds__(256) void k_kv_rows(KvRowsArgs a) {
   float x[4][8];
   if constexpr (WRITE) {
     Piece<KT> p[4];
+    [[maybe_unused]] uint32_t t8[4][8], keep = 0, mine = 0;  // INT8: the integers; bytes that stay; row d8 % 4's maximum
 #pragma unroll
     for (int j = 0; j < 4; ++j) ld_row8<IT, VEC>(dense, e0 + min(max(j, lo), hi - 1) * row_stride, x[j]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if constexpr (std::is_same_v<KT, i8_t>) {
-        uint32_t m = 0;
+        const uint32_t amax = row_umax<LD8>(amax8(x[j]));
+        const RowScale rs(amax);
+        if ((d8 & 3) == j) mine = amax;
+        rs.quant8(x[j], t8[j]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[j][e]) & 0x7fffffffu);
-        const RowScale rs(row_umax<LD8>(m));
-        p[j] = pack<KT>(x[j], &rs);
-        if (d8 == 0 && j >= lo && j < hi) sc[j] = rs.scale;
+        for (int h = 0; h < 2; ++h) p[j].w[h] = low4(t8[j][4 * h], t8[j][4 * h + 1], t8[j][4 * h + 2], t8[j][4 * h + 3]) & rs.keep();
+        keep |= rs.keep() & (0xffu << (8 * j));
       } else {
         p[j] = pack<KT>(x[j], nullptr);
       }
     }
+    if constexpr (std::is_same_v<KT, i8_t>)  // (each lane one row's scale: a division is ten instructions)
+      if (d8 < 4 && d8 >= lo && d8 < hi) sc[d8] = scale_of(mine);
     if (hi - lo == 4) {  // 32 elements: 8 e + j of a K block (dim j, position e), 4 e + j of a V block (position j, dim e)
       uint32_t t[4 * Piece<KT>::W] = {};
       if (!is_v) {
@@ -262,6 +285,9 @@ __global__ __launch_bounds__(256) void k_kv_rows(KvRowsArgs a) {
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int e = 0; e < Piece<KT>::W; ++e) t[j * Piece<KT>::W + e] = p[j].w[e];
+      } else if constexpr (std::is_same_v<KT, i8_t>) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = low4(t8[0][e], t8[1][e], t8[2][e], t8[3][e]) & keep;
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -322,10 +348,8 @@ __global__ __launch_bounds__(256) void k_kv_quant(const Plan* plan, const float*
   ld_row8<float, true>(rows, ((int64_t)m * 2 * hkv + kh) * HD + 8 * d8, x);
   const RowDesc rd = row_desc(plan, m);
   const int page = bt[(size_t)rd.seq * max_pps + (rd.pos >> 4)], t = rd.pos & 15;
-  uint32_t top = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  const RowScale rs(row_umax<LD8>(top));
+  const uint32_t amax = row_umax<LD8>(amax8(x));
+  const RowScale rs(amax);
   const Piece<i8_t> p = pack<i8_t>(x, &rs);
   const bool is_v = kh >= hkv;
   char* pool = (char*)(is_v ? vpool : kpool);
@@ -337,7 +361,7 @@ __global__ __launch_bounds__(256) void k_kv_quant(const Plan* plan, const float*
   } else {
     st_words<i8_t>(blk, p.w);
   }
-  if (d8 == 0) ((float*)(pool + scales))[slot * 16 + t] = rs.scale;
+  if (d8 == 0) ((float*)(pool + scales))[slot * 16 + t] = scale_of(amax);
 }
 
 hipError_t launch_kv_quant(const Plan* plan, int M, const float* rows, void* kpool, void* vpool, size_t scales, const int* bt,
