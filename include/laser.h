@@ -572,7 +572,7 @@ laser_status laser_model_set_gemm_kernel(laser_model* m, int mode);
 /* Kernels of laser_attend.  Spans of up to 64 columns (rows times query heads of a kv head) go through
  * row kernels, 16 or 32 columns to a workgroup, which read the pages straight into registers; longer ones
  * may go through a tile kernel, which converts a page once for 256 columns.  mode 0 (the default): the
- * tile kernel when a call has work enough for it; 1: only row kernels; 2: the tile kernel for every
+ * tile kernel for spans that fill its tiles, when a call has work enough; 1: only row kernels; 2: the tile kernel for every
  * span of more than 64 columns (not on fp32 caches).  Results may differ in the last bits, and so may the
  * workspace.  Errors: LASER_ERR_STATE (bad model), LASER_ERR_INVALID_ARG (mode). */
 laser_status laser_model_set_attend_kernel(laser_model* m, int mode);
