@@ -54,6 +54,26 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t* p) {
   }
 }
 
+// Parts and infinities.  A product with parts adds 0 x inf = NaN where a number has an infinity opposite whose
+// lower parts are zero (as those of 1.0 are), and an infinity's own lower parts are inf - inf.  So only leading parts
+// may meet an infinite element, and they give what the number itself gives: inf, -inf or NaN.  Queries are split so
+// once; K and V are only looked at closely (finite_parts) where a sum has become infinite or NaN (that look costs calls
+// without infinities up to 2%: fp32 rows, bf16 pool, 7B heads, 4 sequences to 14,000 20.3 and 20.8 us, 16 sequences of
+// 1,000-9,000, 40 rows, 217 and 221; a chunk of 1,000 rows behind 8,000 356 and 359).
+//
+// The ones of a pair whose leading part is finite, as a mask.
+__device__ __forceinline__ uint32_t finite_bf16(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+}
+__device__ __forceinline__ bf16x8 finite_parts(bf16x8 x, bf16x8 lead) {
+  u32x4 w = __builtin_bit_cast(u32x4, x), t = __builtin_bit_cast(u32x4, lead);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] &= finite_bf16(t[i]);
+  return __builtin_bit_cast(bf16x8, w);
+}
+// A NaN's leading part is a NaN as well (and not an infinity, where only low bits tell it from one).
+__device__ __forceinline__ uint32_t quiet(uint32_t w) { return (w & 0x7fffffffu) > 0x7f800000u ? w | 0x400000u : w; }
+
 // The span of a work item (spans are listed by their first item), read from the argument segment itself: an
 // index into an argument would have the compiler copy all of it to scratch.  With one span its fields come in the
 // first round of loads.
@@ -125,9 +145,11 @@ __device__ __forceinline__ void ld_query8(const AttendArgs& a, int64_t e, bf16x8
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t s[3];
-      split3(x[i >> 1][2 * (i & 1)], x[i >> 1][2 * (i & 1) + 1], s);
+      split3(__uint_as_float(quiet(__float_as_uint(x[i >> 1][2 * (i & 1)]))),
+             __uint_as_float(quiet(__float_as_uint(x[i >> 1][2 * (i & 1) + 1]))), s);
+      const uint32_t fin = finite_bf16(s[0]);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) w[k][i] = s[k] ^ (flip | (flip >> 16));
+      for (int k = 0; k < 3; ++k) w[k][i] = (k == 0 ? s[k] : s[k] & fin) ^ (flip | (flip >> 16));
     }
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) out[k] = __builtin_bit_cast(bf16x8, w[k]);
@@ -168,6 +190,7 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
   constexpr int PARTS = std::is_same_v<IT, float> ? 3 : 1;    // of a query or weight
   constexpr int KP = std::is_same_v<KT, float> ? 3 : 1;       // of a key or value
   constexpr bool I8 = std::is_same_v<KT, i8_t>;
+  constexpr bool INF = KP == 3 || (PARTS == 3 && sizeof(KT) == 2);  // infinities meet parts (8-bit pools have none)
   constexpr int NS = HD / 32, ND = HD / 16, NC = 16 * NT;
   constexpr int OS = HD + 4;  // LDS row stride (floats): 16 rows fall in different banks
   constexpr int ES = (int)sizeof(KT);
@@ -266,7 +289,7 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
     }
     look(pg + 2);
   };
-  auto key = [&](const KRaw* raw, bf16x8* k) {
+  auto key = [&](const KRaw* raw, bf16x8* k, auto careful) {
     if constexpr (ES == 1) {
       uint32_t w4[4];
       if constexpr (I8) {
@@ -284,7 +307,9 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t s[3];
-        split3(__uint_as_float(raw[i >> 1][2 * (i & 1)]), __uint_as_float(raw[i >> 1][2 * (i & 1) + 1]), s);
+        uint32_t a = raw[i >> 1][2 * (i & 1)], b = raw[i >> 1][2 * (i & 1) + 1];
+        if constexpr (decltype(careful)::value) a = quiet(a), b = quiet(b);
+        split3(__uint_as_float(a), __uint_as_float(b), s);
 #pragma unroll
         for (int z = 0; z < 3; ++z) p[z][i] = s[z];
       }
@@ -293,7 +318,7 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
     }
   };
   // dims 16 d + lc of positions 4 lg .. of both pages
-  auto value = [&](const VRaw& va, const VRaw& vb, bf16x8* v) {
+  auto value = [&](const VRaw& va, const VRaw& vb, bf16x8* v, auto careful) {
     if constexpr (ES == 1) {
       uint32_t w4[4];
       if constexpr (I8) {
@@ -312,7 +337,9 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
       for (int i = 0; i < 4; ++i) {
         uint32_t s[3];
         const VRaw& src = i < 2 ? va : vb;
-        split3(__uint_as_float(src[2 * (i & 1)]), __uint_as_float(src[2 * (i & 1) + 1]), s);
+        uint32_t a = src[2 * (i & 1)], b = src[2 * (i & 1) + 1];
+        if constexpr (decltype(careful)::value) a = quiet(a), b = quiet(b);
+        split3(__uint_as_float(a), __uint_as_float(b), s);
 #pragma unroll
         for (int z = 0; z < 3; ++z) p[z][i] = s[z];
       }
@@ -321,15 +348,21 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
     }
   };
   // products of parts i and j with i + j < 3 (the others are below 2^-24)
-  auto mma = [&](const bf16x8* x, const bf16x8* y, f32x4 acc) {
+  auto mma = [&](const bf16x8* x, const bf16x8* y, f32x4 acc, auto careful) {
 #pragma unroll
     for (int i = KP - 1; i >= 0; --i)
 #pragma unroll
-      for (int j = PARTS - 1; j >= 0; --j)
-        if (i + j < 3) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], y[j], acc, 0, 0, 0);
+      for (int j = PARTS - 1; j >= 0; --j) {
+        if (i + j >= 3) continue;
+        if constexpr (decltype(careful)::value)  // (only the leading parts meet an infinity)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(i + j > 0 ? finite_parts(x[i], x[0]) : x[0],
+                                                        i + j > 0 ? finite_parts(y[j], y[0]) : y[0], acc, 0, 0, 0);
+        else
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], y[j], acc, 0, 0, 0);
+      }
     return acc;
   };
-  auto compute = [&](const Pair& b, int pg) {
+  auto compute = [&](const Pair& b, int pg, auto careful) {
     const bool whole = 16 * pg >= flo && 16 * pg + 32 <= fhi && pg + 1 < p1;  // (uniform)
     f32x4 s[NT][2];
 #pragma unroll
@@ -339,9 +372,9 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
 #pragma unroll
       for (int k = 0; k < NS; ++k) {
         bf16x8 kk[KP];
-        key(b.k[x][k], kk);
+        key(b.k[x][k], kk, careful);
 #pragma unroll
-        for (int u = 0; u < NT; ++u) s[u][x] = mma(kk, q[u][k], s[u][x]);
+        for (int u = 0; u < NT; ++u) s[u][x] = mma(kk, q[u][k], s[u][x], careful);
       }
     bf16x8 p[NT][PARTS];
     uint32_t seen[NT];  // this lane's 8 positions (bits 0-3 page pg, 4-7 page pg + 1)
@@ -402,7 +435,7 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
       for (int k = 0; k < PARTS; ++k) p[u][k] = __builtin_bit_cast(bf16x8, pw[k]);
     }
     bool odd = false;
-    if (!I8 && !whole) {  // an infinite or NaN V anywhere in the pair?
+    if (!I8 && (decltype(careful)::value || !whole)) {  // an infinite or NaN V anywhere in the pair?
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -423,9 +456,9 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
         bf16x8 v[KP];
-        value(b.v[0][d], b.v[1][d], v);
+        value(b.v[0][d], b.v[1][d], v, careful);
 #pragma unroll
-        for (int u = 0; u < NT; ++u) o[u][d] = mma(v, p[u], o[u][d]);
+        for (int u = 0; u < NT; ++u) o[u][d] = mma(v, p[u], o[u][d], careful);
       }
     } else if constexpr (!I8) {
       // row by row: V of the positions that the row does not see is zero, and the row's columns take
@@ -460,10 +493,10 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
             }
           }
           bf16x8 v[KP];
-          value(va, vb, v);
+          value(va, vb, v, careful);
 #pragma unroll
           for (int u = 0; u < NT; ++u) {
-            const f32x4 t = mma(v, p[u], o[u][d]);
+            const f32x4 t = mma(v, p[u], o[u][d], careful);
             if (crow[u] == r) o[u][d] = t;
           }
         }
@@ -475,10 +508,36 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
     load(buf[0], p0);
     for (int pg = p0; pg < p1; pg += 4) {
       load(buf[1], pg + 2);
-      compute(buf[0], pg);
+      compute(buf[0], pg, std::false_type{});
       if (pg + 2 >= p1) break;
       load(buf[0], pg + 4);
-      compute(buf[1], pg + 2);
+      compute(buf[1], pg + 2, std::false_type{});
+    }
+    if constexpr (INF) {  // a sum that is infinite or NaN stays so: the run once more, parts and infinities apart
+      float z = 0.f;
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        z = fmaf(ls[u], 0.f, z);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z = fmaf(o[u][d][i], 0.f, z);
+      }
+      if (__builtin_expect(__ballot(z != 0.f) != 0, 0)) {
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+          m[u] = -INFINITY;
+          ls[u] = 0.f;
+#pragma unroll
+          for (int d = 0; d < ND; ++d) o[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll 1
+        for (int pg = p0; pg < p1; pg += 2) {
+          look(pg);
+          load(buf[0], pg);
+          compute(buf[0], pg, std::true_type{});
+        }
+      }
     }
   }
 
@@ -543,6 +602,7 @@ template <class KT, class IT, int HD>
 __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
   constexpr int PARTS = std::is_same_v<IT, float> ? 3 : 1;
   constexpr bool I8 = std::is_same_v<KT, i8_t>;
+  constexpr bool INF = PARTS == 3 && sizeof(KT) == 2;  // infinities meet parts
   constexpr int ES = (int)sizeof(KT), NK = HD / 16, ND = HD / 32, SP = 4;  // SP: pages of a step
   constexpr int PB = 32 * HD;             // bytes of a page's K or V in LDS (bf16)
   constexpr int NL = 16 * HD * ES / 1024; // 16-byte loads per lane for a page's K or V
@@ -700,7 +760,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
   // 32 x + 8 (i / 4) + 4 h + i % 4.  Integer pages: in exp2 units, plus log2 of the position's V scale (as it
   // is: without); otherwise before the scale.
   f32x16 s[2];
-  auto scores = [&](int buf, bool as_is) {
+  auto scores = [&](int buf, bool as_is, auto careful) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
@@ -710,7 +770,8 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
       for (int k = 0; k < NK; ++k) {
         const bf16x8 kk = *(const bf16x8*)(b + 512 * k);
 #pragma unroll
-        for (int z = PARTS - 1; z >= 0; --z) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, q[k][z], s[x], 0, 0, 0);
+        for (int z = PARTS - 1; z >= 0; --z)
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decltype(careful)::value && z > 0 ? finite_parts(kk, kk) : kk, q[k][z], s[x], 0, 0, 0);
       }
     }
     if constexpr (I8)
@@ -781,17 +842,20 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
       }
     }
   };
-  auto product = [&](u32x4 v, int y, f32x16 acc) {
+  auto product = [&](u32x4 vw, int y, f32x16 acc, auto careful) {
+    const bf16x8 v = __builtin_bit_cast(bf16x8, vw);
 #pragma unroll
     for (int z = PARTS - 1; z >= 0; --z)
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pw[y & 1][z]), acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decltype(careful)::value && z > 0 ? finite_parts(v, v) : v,
+                                                    __builtin_bit_cast(bf16x8, pw[y & 1][z]), acc, 0, 0, 0);
     return acc;
   };
+  using Careful = std::bool_constant<INF>;
   // What is rare (positions that not every column sees, a maximum that moves) stands in branches of its own
   // that change the registers in place, and odd steps come after all others: so the loop keeps its
   // accumulators where they are.
   auto step = [&](int buf, int pg, bool odd) {
-    scores(buf, false);
+    scores(buf, false, std::false_type{});
     if constexpr (PARTS == 1) {  // operands ahead of their products
       __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
@@ -807,15 +871,17 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
 #pragma unroll
     for (int y = 0; y < SP; ++y) {
 #pragma unroll
-      for (int d = 0; d < ND; ++d) o[d] = product(*(const u32x4*)(vb + y * PB + d * 512), y, o[d]);
+      for (int d = 0; d < ND; ++d) o[d] = product(*(const u32x4*)(vb + y * PB + d * 512), y, o[d], std::false_type{});
       if (y + 1 < SP) weights(buf, y + 1, false);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   // A step with odd values, row by row as in the row kernel: V of the positions that the row does not see is
-  // zero (an integer page: their weights), and the row's columns take the result.
-  auto odd_step = [&](int buf, int pg) {
-    scores(buf, true);
+  // zero (an integer page: their weights), and the row's columns take the result; parts and infinities apart.  (INF, V
+  // not odd: all columns at once.)
+  auto odd_step = [&](int buf, int pg, bool odd) {
+    if constexpr (!INF) odd = true;
+    scores(buf, true, Careful{});
     hide(pg, clo, chi);
     raise_max();
     const char* vb = s_v[buf] + (h * HD + lc) * 16;
@@ -823,13 +889,13 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
     for (int y = 0; y < SP; ++y) {
       weights(buf, y, true);
 #pragma unroll 1
-      for (int r = row_a; r <= row_z; ++r) {
+      for (int r = odd ? row_a : row_z; r <= row_z; ++r) {
         const int begin = first_key(r), end = min(end_key(r), 16 * s1);
         u32x4 keep;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int t = 16 * (pg + y) + 8 * (j >> 2) + 4 * h + (j & 3);
-          const uint32_t k16 = t >= begin && t < end ? 0xffffu : 0u;
+          const uint32_t k16 = !odd || (t >= begin && t < end) ? 0xffffu : 0u;
           keep[j >> 1] = (j & 1) ? keep[j >> 1] | (k16 << 16) : k16;
         }
         if constexpr (I8)  // (a lane's own column decides; the others' results are not taken)
@@ -839,9 +905,9 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
           const u32x4 v = *(const u32x4*)(vb + y * PB + d * 512);
-          const f32x16 t = product(I8 ? v : v & keep, y, o[d]);
+          const f32x16 t = product(I8 ? v : v & keep, y, o[d], Careful{});
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] = row == r ? t[i] : o[d][i];
+          for (int i = 0; i < 16; ++i) o[d][i] = row == r || !odd ? t[i] : o[d][i];
         }
       }
     }
@@ -860,13 +926,26 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
       if (more) stage(buf ^ 1, pg + SP, false);
       __syncthreads();
     }
-    if (__builtin_expect(left, 0)) {
+    bool again = false;
+    if constexpr (INF) {  // a score is NaN, perhaps by its parts: all steps once more
+      again = __syncthreads_or(ls != ls);
+      if (__builtin_expect(again, 0)) {
+        m = -INFINITY;
+        ls = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+      }
+    }
+    if (__builtin_expect(left || again, 0)) {
 #pragma unroll 1
       for (int pg = s0; pg < s1; pg += SP) {
         fetch(pg);
         stage(0, pg, true);
         __syncthreads();
-        if (is_odd(0)) odd_step(0, pg);
+        const bool odd = is_odd(0);
+        if (odd || again) odd_step(0, pg, odd);
         __syncthreads();
       }
     }

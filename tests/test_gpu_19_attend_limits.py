@@ -1,0 +1,139 @@
+"""laser_attend at the edges of its number types, against the definition in float64: infinities that a row sees in
+K, V or its own query, for every type of rows and cache that can hold them and both kernels."""
+import numpy as np
+import pytest
+import torch
+
+from paged_ref import attend
+from paper_2606_31580_amd import laser as L
+from test_gpu_16_kv_rows import IO, cache, f64
+from test_gpu_17_attend import both, check, fill, kernels, queries  # noqa: F401  (kernels: an automatic fixture)
+
+pytestmark = pytest.mark.gpu
+POOLS = pytest.mark.parametrize("kind,io", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
+
+
+def put(kv, kind, held, seq, pos, is_v, head, dim, value):
+    """One element of a cached position replaced, in the cache and in the reference's copy."""
+    held[seq][is_v][pos, head, dim] = value
+    rows = [torch.from_numpy(x[pos:pos + 1].astype(np.float32)).to(torch.float32 if kind == "f32" else torch.bfloat16).cuda()
+            for x in held[seq]]
+    L.laser_kv_write(kv, 1, [L.kv_run(seq, pos, 1)], *rows)
+
+
+def check_all(kv, kind, io, held, spans, q, **kw):
+    """`check`, and infinities of the same sign in the same places; returns the reference's rows of each span."""
+    o, lse = check(kv, kind, io, held, spans, q, **kw)
+    out = []
+    for s in spans:
+        k, v = held[s.seq]
+        r = slice(s.row0, s.row0 + s.n)
+        with np.errstate(over="ignore", invalid="ignore"):
+            ro, rl = attend(f64(q)[r], k, v, s.pos, q.shape[-1] ** -0.5, True, kw.get("window", 0))
+        for got, ref in ((f64(o)[r], ro), (f64(lse)[r], rl)):
+            assert np.array_equal(np.isposinf(got), np.isposinf(ref)) and np.array_equal(np.isneginf(got), np.isneginf(ref))
+        out.append((ro, rl))
+    return out
+
+
+@both
+@POOLS
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n,length", [(2, 330), (90, 330), (1, 3001), (90, 2100)])
+def test_seen_infinities(kind, io, hd, n, length):
+    """Keys of -infinity weigh nothing, values of either infinity come out, next to queries that parts of bf16 hold
+    exactly (1.0: the lower parts are zero) and others; keys of +infinity make the row NaN."""
+    hq, hkv = 6, 2
+    kv = cache(kind, hq, hkv, hd, pages=2 * (length // 16 + 1), seqs=2, per_seq=190)
+    held = fill(kv, kind, [length, length], hkv, hd, 41)
+    q = queries(np.random.default_rng(42), 2 * n, hq, hd, io).abs() + 0.25
+    q[:, 1::2, :] = 1.0
+    q = q.to(IO[io])
+    for pos, head, dim in ((3, 0, 5), (length - n, 0, 9), (length // 2, 1, 0), (length // 2 + 1, 1, 63)):
+        put(kv, kind, held, 0, pos, False, head, dim, -np.inf)
+    for pos, dim, val in ((7, 3, np.inf), (length // 2, 4, -np.inf), (length - n, 8, np.inf)):
+        put(kv, kind, held, 0, pos, True, 0, dim, val)
+    put(kv, kind, held, 1, length // 3, False, 0, 7, np.inf)
+    spans = [L.attend_span(0, n, length - n), L.attend_span(1, n, length - n, row0=n)]
+    (o, lse), (o1, lse1) = check_all(kv, kind, io, held, spans, q)
+    # (the case is what it says: finite rows beside infinite dims, NaN only where an infinity has weight zero)
+    assert np.isfinite(lse).all() and np.isposinf(o[:, 0, 3]).all() and np.isfinite(o[:, 3:]).all()
+    assert np.isnan(o1[:, :3]).all() and np.isfinite(o1[:, 3:]).all()
+
+
+@both
+@POOLS
+@pytest.mark.parametrize("n", [1, 90])
+def test_only_scores_of_minus_infinity(kind, io, n):
+    """All keys that a row sees score -infinity: o = 0 and lse = -infinity."""
+    hq, hkv, hd, length = 4, 2, 64, 300
+    kv = cache(kind, hq, hkv, hd, pages=40, seqs=1, per_seq=40)
+    held = fill(kv, kind, [length], hkv, hd, 43)
+    held[0][0][:, 0, 11] = -np.inf
+    t = torch.float32 if kind == "f32" else torch.bfloat16
+    k, v = (torch.from_numpy(x.astype(np.float32)).to(t).cuda() for x in held[0])
+    L.laser_kv_write(kv, 1, [L.kv_run(0, 0, length)], k, v)
+    q = queries(np.random.default_rng(44), n, hq, hd, io)
+    q[:, :2, 11] = 1.0
+    ((o, lse),) = check_all(kv, kind, io, held, [L.attend_span(0, n, length - n)], q)
+    assert np.isneginf(lse[:, :2]).all() and (o[:, :2] == 0).all()
+
+
+@both
+@pytest.mark.parametrize("kind,io", [("bf16", "f32"), ("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("int8", "f32"), ("fp8", "f32")])
+def test_infinite_queries(kind, io):
+    """A query of -infinity against keys of one sign scores -infinity everywhere (o = 0), of both signs NaN; a NaN
+    whose upper half alone would be an infinity is a NaN."""
+    hq, hkv, hd, length, n = 4, 2, 64, 300, 80
+    kv = cache(kind, hq, hkv, hd, pages=40, seqs=1, per_seq=40)
+    kv.add_seq(0, length)
+    rng = np.random.default_rng(45)
+    t = torch.float32 if kind == "f32" else torch.bfloat16
+    k, v = (rng.standard_normal((length, hkv, hd)).astype(np.float32) for _ in range(2))
+    k[:, :, 7] = np.abs(k[:, :, 7]) + 0.5
+    k, v = (torch.from_numpy(x).to(t).cuda() for x in (k, v))
+    L.laser_kv_write(kv, 1, [L.kv_run(0, 0, length)], k, v)
+    back = [torch.empty(length, hkv, hd, device="cuda") for _ in range(2)]
+    L.laser_kv_read(kv, 1, [L.kv_run(0, 0, length)], *back)
+    held = [tuple(f64(x) for x in back)]
+    q = queries(rng, n, hq, hd, io)
+    q[3, 0, 7] = q[40, 3, 7] = -np.inf
+    q[5, 1, 8] = np.inf
+    spans = [L.attend_span(0, n, length - n)]
+    if io == "f32":
+        q[8, 2, 1] = torch.tensor([0x7f800001], dtype=torch.int32).view(torch.float32).cuda()[0]
+    else:
+        q[8, 2, 1] = np.nan
+    assert torch.isnan(q[8, 2, 1])
+    ref = attend(f64(q), *held[0], length - n, hd ** -0.5)
+    assert np.isneginf(ref[1][3, 0]) and np.isnan(ref[1][5, 1]) and np.isnan(ref[1][8, 2])
+    o, lse = torch.full_like(q, 5.0), torch.full((n, hq), 5.0, device="cuda")
+    L.laser_attend(kv, 1, spans, q, o, lse=lse)
+    torch.cuda.synchronize()
+    o, lse = f64(o), f64(lse)
+    for got, want in ((o, ref[0]), (lse, ref[1])):
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isneginf(got), np.isneginf(want))
+    assert (o[3, 0] == 0).all() and (o[40, 3] == 0).all()
+    fine = np.isfinite(ref[1])
+    # (bf16 weights and output: 2^-8 of the largest V and of the output; fp32: the scores' roundings, below 2^-18 here)
+    tol = (2.0 ** -8 * np.abs(held[0][1]).max() * 2 if io == "bf16" else 2.0 ** -18 * np.abs(held[0][1]).max())
+    assert np.abs(o - ref[0])[fine].max() <= tol
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_low_nan_bits_in_the_cache(io):
+    """An fp32 cache keeps a NaN's lowest bits, whose upper half alone is an infinity: it stays a NaN."""
+    hq, hkv, hd, length = 2, 2, 64, 100
+    kv = cache("f32", hq, hkv, hd, pages=10, seqs=1, per_seq=10)
+    fill(kv, "f32", [length], hkv, hd, 46)
+    low = torch.tensor([0x7f800001], dtype=torch.int32).view(torch.float32)
+    k, v = torch.zeros(1, hkv, hd), torch.zeros(1, hkv, hd)
+    k.view(torch.int32)[0, 0, 3] = low.view(torch.int32)[0]
+    v.view(torch.int32)[0, 1, 5] = low.view(torch.int32)[0]
+    L.laser_kv_write(kv, 1, [L.kv_run(0, 20, 1)], k.cuda(), v.cuda())
+    q = queries(np.random.default_rng(47), 1, hq, hd, io)
+    o = torch.empty_like(q)
+    L.laser_attend(kv, 1, [L.attend_span(0, 1, length - 1)], q, o)
+    torch.cuda.synchronize()
+    bad = torch.isnan(o[0]).cpu()
+    assert bad[0].all() and bad[1, 5] and int(bad[1].sum()) == 1 and torch.isfinite(o[0, 1, :5]).all()
