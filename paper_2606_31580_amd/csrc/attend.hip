@@ -91,6 +91,14 @@ __device__ __forceinline__ AttendSpan item_span(int n_spans, unsigned item) {
   return get(sp + W * __builtin_amdgcn_readfirstlane(__builtin_popcountll(__ballot(first <= item)) - 1));
 }
 
+// O / l; zero where no weight is (whatever 0 x V gave, V of seen keys that score -infinity being infinite).
+__device__ __forceinline__ f32x4 normed(f32x4 o, float l) {
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
+  return o;
+}
+
 // Four output dims of a row, in the rows' type.
 template <class IT>
 __device__ __forceinline__ void st_out4(const AttendArgs& a, int row, int head, int d, f32x4 v) {
@@ -572,7 +580,7 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
     }
     const int r = (col0 + c) / a.G, h = kvh * a.G + col0 + c - r * a.G;
     if (sp.nsplit == 1) {
-      st_out4<IT>(a, sp.row0 + r, h, 4 * d4, acc * (L == 0.f ? 0.f : 1.f / L));
+      st_out4<IT>(a, sp.row0 + r, h, 4 * d4, normed(acc, L));
       if (d4 == 0 && a.lse != nullptr)
         a.lse[(size_t)(sp.row0 + r) * a.hq + h] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
     } else {
@@ -953,13 +961,12 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
   if (wc0 + lc >= ncol) return;
   ls = sum_x32(ls);
   if (sp.nsplit == 1) {
-    const float inv = ls == 0.f ? 0.f : 1.f / ls;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int b = 0; b < 4; ++b)
         st_out4<IT>(a, sp.row0 + row, head, 32 * d + 8 * b + 4 * h,
-                    f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * inv);
+                    normed(f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]}, ls));
     if (h == 0 && a.lse != nullptr)
       a.lse[(size_t)(sp.row0 + row) * a.hq + head] = ls == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(ls)) * kLn2;
   } else {
@@ -1041,7 +1048,7 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
     Lt += s_l[v] * f;
     Ot += *(const f32x4*)&s_o[v][4 * d4] * f;
   }
-  st_out4<IT>(a, sp.row0 + r, h, 4 * d4, Ot * (Lt == 0.f ? 0.f : 1.f / Lt));
+  st_out4<IT>(a, sp.row0 + r, h, 4 * d4, normed(Ot, Lt));
   if (d4 == 0 && a.lse != nullptr)
     a.lse[(size_t)(sp.row0 + r) * a.hq + h] = Lt == 0.f ? -INFINITY : (Mt + __builtin_amdgcn_logf(Lt)) * kLn2;
 }
@@ -1075,7 +1082,7 @@ __global__ __launch_bounds__(256) void k_attend_merge_few(AttendArgs a) {
     L += lv[s] * f;
     O += ov[s] * f;
   }
-  st_out4<IT>(a, sp.row0 + r, h, 4 * d4, O * (L == 0.f ? 0.f : 1.f / L));
+  st_out4<IT>(a, sp.row0 + r, h, 4 * d4, normed(O, L));
   if (d4 == 0 && a.lse != nullptr)
     a.lse[(size_t)(sp.row0 + r) * a.hq + h] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
 }

@@ -80,6 +80,25 @@ def test_only_scores_of_minus_infinity(kind, io, n):
 
 
 @both
+@POOLS
+@pytest.mark.parametrize("n,length", [(1, 300), (90, 300), (1, 3000), (90, 3000)])
+def test_only_scores_of_minus_infinity_and_odd_values(kind, io, n, length):
+    """The same where V is infinite or NaN at seen positions; keys in one workgroup and in several."""
+    hq, hkv, hd = 6, 2, 64
+    kv = cache(kind, hq, hkv, hd, pages=length // 16 + 1, seqs=1, per_seq=190)
+    held = fill(kv, kind, [length], hkv, hd, 48)
+    held[0][0][:, 0, 11] = -np.inf
+    held[0][1][5, 0, 1], held[0][1][length - n, 0, 2], held[0][1][length // 2, 0, 3] = np.inf, np.nan, -np.inf
+    t = torch.float32 if kind == "f32" else torch.bfloat16
+    k, v = (torch.from_numpy(x.astype(np.float32)).to(t).cuda() for x in held[0])
+    L.laser_kv_write(kv, 1, [L.kv_run(0, 0, length)], k, v)
+    q = queries(np.random.default_rng(49), n, hq, hd, io)
+    q[:, :3, 11] = 1.0
+    ((o, lse),) = check_all(kv, kind, io, held, [L.attend_span(0, n, length - n)], q)
+    assert np.isneginf(lse[:, :3]).all() and (o[:, :3] == 0).all() and np.isfinite(lse[:, 3:]).all()
+
+
+@both
 @pytest.mark.parametrize("kind,io", [("bf16", "f32"), ("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("int8", "f32"), ("fp8", "f32")])
 def test_infinite_queries(kind, io):
     """A query of -infinity against keys of one sign scores -infinity everywhere (o = 0), of both signs NaN; a NaN
