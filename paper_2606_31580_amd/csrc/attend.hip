@@ -4,9 +4,9 @@
 // and t > pos + i - window (window > 0):
 //   s_t = scale q.k_t,  m = max s_t,  l = sum exp(s_t - m),  o = sum exp(s_t - m) v_t / l,
 //   lse = m + log l;  nothing seen: o = 0, lse = -inf.
-// The keys are taken once, in exp2 units, with a running m and l per row.  m is only moved, and what
-// has been summed rescaled, when a score exceeds it by more than kSlack: exp2 of up to that much keeps
-// every sum far inside fp32, and the weights' relative rounding does not change.
+// The keys are taken once, in exp2 units, with a running m and l per row.  m is moved, and what has been summed
+// rescaled, when a score exceeds it, and then to kSlack above that score: so it moves rarely, no weight is above 1 (the
+// sums stay inside fp32 for V up to its largest divided by the keys), and the largest is at least 2^-8 of 1.
 //
 // The G query heads of a kv head and the rows of a span are the columns of one matrix: column c is row
 // c / G, head kvh G + c % G, so that K and V are read once for all of them.  Matrix-core products, K or V
@@ -409,9 +409,9 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) mx = fmaxf(mx, sv[i]);
       mx = max_x32(max_x16(mx));
-      const bool grow = mx > m[u] + kSlack;
+      const bool grow = mx > m[u];
       if (__ballot(grow)) {
-        const float mn = grow ? mx : m[u];
+        const float mn = grow ? mx + kSlack : m[u];
         const float alpha = grow ? __builtin_amdgcn_exp2f(m[u] - mn) : 1.f;  // (m = -inf: 0)
         ls[u] *= alpha;
 #pragma unroll
@@ -681,9 +681,9 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
   };
   // What V holds past the last key is taken as zero.  A page with an odd value is flagged; unless it is
   // asked for as it is, its V is zero too, and its step is left for the end.  Odd are infinities and NaN,
-  // and V scales s of an integer page outside 2^-40 .. 2^40: there the weights p s are computed as
+  // and V scales s of an integer page outside 2^-36 .. 2^36: there the weights p s are computed as
   // exp2(score + log2 s), and the sum of the p as that of the p s times 1 / s, which saves an operation per
-  // weight but would lose some p below 2^-46 of the largest if the scales lay further apart.  (All zeros:
+  // weight but would lose some p below 2^-46 of the largest (126 - 8 of m - 2 x 36) if the scales lay further apart.  (All zeros:
   // any scale will do.)
   auto stage = [&](int buf, int pg, bool as_is) {
     if (!st_v) {  // as in the page: chunk (8 dims, position) at 16 bytes each
@@ -714,7 +714,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
         }
         if ((l & 15) >= left) raw_s = 0.f;
       }
-      bool odd = I8 && raw_s != 0.f && !(raw_s >= 0x1p-40f && raw_s <= 0x1p40f);
+      bool odd = I8 && raw_s != 0.f && !(raw_s >= 0x1p-36f && raw_s <= 0x1p36f);
       if constexpr (!I8)
 #pragma unroll
         for (int i = 0; i < NL; ++i)
@@ -754,7 +754,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
         }
       }
       if (I8 && l < 16) {
-        const float s = raw_s == 0.f ? 0x1p-40f : raw_s;
+        const float s = raw_s == 0.f ? 0x1p-36f : raw_s;
         s_lv[buf][16 * st_p + l] = __builtin_amdgcn_logf(s);
         s_vs[buf][16 * st_p + l] = as_is ? raw_s : 1.f / s;
       }
@@ -812,9 +812,9 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
     mx = max_x32(mx) * (I8 ? 1.f : sc);
-    const bool grow = mx > m + kSlack;
+    const bool grow = mx > m;
     if (__builtin_expect(__ballot(grow) != 0, 0)) {
-      const float mn = grow ? mx : m;
+      const float mn = grow ? mx + kSlack : m;
       const float alpha = grow ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
       ls *= alpha;
 #pragma unroll

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from paged_ref import attend
+from paged_ref import attend, kept
 from paper_2606_31580_amd import laser as L
 from test_gpu_16_kv_rows import IO, cache, f64
 from test_gpu_17_attend import both, check, fill, kernels, queries  # noqa: F401  (kernels: an automatic fixture)
@@ -156,3 +156,25 @@ def test_low_nan_bits_in_the_cache(io):
     torch.cuda.synchronize()
     bad = torch.isnan(o[0]).cpu()
     assert bad[0].all() and bad[1, 5] and int(bad[1].sum()) == 1 and torch.isfinite(o[0, 1, :5]).all()
+
+
+@both
+@pytest.mark.parametrize("kind,io", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("f32", "bf16"), ("int8", "bf16"), ("int8", "f32")])
+@pytest.mark.parametrize("n", [2, 90])
+def test_values_near_the_largest(kind, io, n):
+    """V of 2^122, at keys that score 5.4 above all before them (2^7.8 times their weight): no sum leaves fp32."""
+    hq, hkv, hd, length = 4, 2, 64, 480
+    kv = cache(kind, hq, hkv, hd, pages=40, seqs=1, per_seq=40)
+    kv.add_seq(0, length)
+    k, v = np.zeros((length, hkv, hd)), np.random.default_rng(50).standard_normal((length, hkv, hd)) * 2.0 ** 110
+    for pos in (100, 310, length - n):
+        k[pos, :, 0] = 43.0 if pos == 310 else 21.5  # (times q 2 and 1/8: 10.75 and 5.375)
+        v[pos] = 2.0 ** 122 * (1 - 2 * (np.arange(hd) % 2))
+    t = torch.float32 if kind == "f32" else torch.bfloat16
+    dk, dv = (torch.from_numpy(x.astype(np.float32)).to(t).cuda() for x in (k, v))
+    L.laser_kv_write(kv, 1, [L.kv_run(0, 0, length)], dk, dv)
+    held = [(kept(kind, f64(dk)), kept(kind, f64(dv)))]
+    q = torch.zeros(n, hq, hd, dtype=IO[io], device="cuda")
+    q[:, :, 0] = 2.0
+    o, _ = check(kv, kind, io, held, [L.attend_span(0, n, length - n)], q)
+    assert bool(torch.isfinite(o).all()) and float(o.float().abs().max()) > 2.0 ** 120
