@@ -397,7 +397,7 @@ typedef struct {
  * rounded to bf16 before they meet V; with fp32 rows nothing is rounded below fp32.  Sums, maxima and the
  * log-sum-exp are fp32 in both.  Results do not depend on what else runs, but a row's last bits may
  * change with the other spans of the call (they decide how keys are split over workgroups).
- * The workspace (laser_attend_workspace bytes, 16-byte aligned; NULL if 0) holds the partial results of
+ * The workspace (laser_attend_workspace bytes, 16-byte aligned; NULL if 0; below 289 MiB) holds the partial results of
  * spans whose keys are split; calls that may run at the same time, captured ones included, need
  * workspaces of their own.  A sequence may be in several spans; a row may not (INVALID_ARG).
  * A span of more rows than a grid's 2^32 threads take is UNSUPPORTED. */

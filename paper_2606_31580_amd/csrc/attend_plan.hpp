@@ -9,6 +9,9 @@ namespace laser {
 
 constexpr int kAttendKinds = 3;  // row kernel with 16 columns, with 32; tile kernel
 constexpr int kAttendFewCols = 64;
+// All partials of a call, at most.  Splits beyond it are not made, whichever kernel takes the rows: calls that would
+// make them have workgroups enough without (30,000 rows of the 8B heads are 3,752 tiles).
+constexpr int64_t kAttendPartBytes = (int64_t)288 << 20;
 
 // A span as the planner sees it, and what it decides.
 struct AttendSize {
@@ -26,7 +29,11 @@ inline int attend_cols(int kind) { return kind == 0 ? 16 : kind == 1 ? 32 : 256;
 
 // Splits of a span of the tile kernel at `run` pages a workgroup, a step of 4 at least.
 inline int tile_split(const AttendSize& s, int run) { return std::max(1, std::min(attend_ceil(s.pages, run), s.pages / 4)); }
-inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus);
+inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus, int64_t part_bytes);
+// Bytes of a span's partials at `splits` workgroups a tile: O, m and l per row, head and split.
+inline int64_t span_part_bytes(const AttendSize& s, int splits, int heads, int hd) {
+  return splits > 1 ? (int64_t)s.n * heads * splits * (hd + 2) * 4 : 0;
+}
 
 // es: bytes of a cached element (i8: integers); io16: 16-bit rows.  fp32 pools have only the row kernel with 16 columns,
 // and fp32 rows not the one with 32 (three parts of everything would not fit the registers).
@@ -53,9 +60,9 @@ inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd,
 // A span of up to 32 pages stays whole, since joining splits is a launch of its own, up to 64 where there
 // are spans enough to fill the CUs (64 sequences of 50-600 positions: 18.2 us split, 14.4 whole) or rows enough to
 // make the join long.
-// All splits together are at most 64 workgroups per CU beyond one per tile: more rounds than that even out nothing, and
-// the partials (8 or 17 KB per workgroup) stay below some 300 MB however many rows a call has (16 per CU cost 4%
-// at 128 sequences of 3,000-14,000 and 256 of 1,000-6,000 positions).
+// All splits together are at most 64 workgroups per CU beyond one per tile: more rounds than that even out nothing (16
+// per CU cost 4% at 128 sequences of 3,000-14,000 and 256 of 1,000-6,000 positions).  And no span has more than the
+// number of splits at which all partials (8 or 17 KB per workgroup) fit kAttendPartBytes.
 // Tile kernel: see tile_run.
 // mode: 0 the kernels as above, 1 only row kernels, 2 the tile kernel wherever it can be (laser_model_set_attend_kernel).
 inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool i8, bool io16, int mode) {
@@ -80,19 +87,36 @@ inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd,
   const int two = attend_ceil(work, (int64_t)cus * 8);  // pages per wave, two workgroups per CU
   const int run = two <= (es == 1 ? 4 : 8) ? std::max(2, attend_ceil(work, (int64_t)cus * 4)) : std::min(two, 32);
   const int most = std::max(1, attend_ceil(64 * (int64_t)cus, std::max<int64_t>(wgs, 1)));
-  const int tile = tile_run(s, n, kv_heads, q_heads, hd, cus);
+  int widest = 1;
   for (int i = 0; i < n; ++i) {
-    if (s[i].kind == 2)
-      s[i].nsplit = tile_split(s[i], tile);
-    else
-      s[i].nsplit = s[i].pages <= (two >= 4 || (int64_t)s[i].n * q_heads > 512 ? 64 : 32) ? 1 : std::min({128, attend_ceil(s[i].pages, 4 * run), most});
+    if (s[i].kind == 2) continue;
+    s[i].nsplit = s[i].pages <= (two >= 4 || (int64_t)s[i].n * q_heads > 512 ? 64 : 32) ? 1 : std::min({128, attend_ceil(s[i].pages, 4 * run), most});
+    widest = std::max(widest, s[i].nsplit);
   }
+  auto row_bytes = [&](int cap) {
+    int64_t bytes = 0;
+    for (int i = 0; i < n; ++i)
+      if (s[i].kind != 2) bytes += span_part_bytes(s[i], std::min(s[i].nsplit, cap), q_heads, hd);
+    return bytes;
+  };
+  int cap = widest;
+  if (row_bytes(cap) > kAttendPartBytes) {  // the largest cap that fits (1 does)
+    int over = cap;
+    cap = 1;
+    while (over - cap > 1) {
+      const int mid = (cap + over) / 2;
+      (row_bytes(mid) <= kAttendPartBytes ? cap : over) = mid;
+    }
+  }
+  const int tile = tile_run(s, n, kv_heads, q_heads, hd, cus, kAttendPartBytes - row_bytes(cap));
+  for (int i = 0; i < n; ++i) s[i].nsplit = s[i].kind == 2 ? tile_split(s[i], tile) : std::min(s[i].nsplit, cap);
 }
 
 // Pages of a workgroup of the tile kernel, the same for all spans (8B heads, INT8, 16 sequences of 1,000-9,000, 60
 // rows: 127 us, 150 with the same number of splits for all): those that make the call shortest, counting 2.2 us for a step of a CU's workgroup, 5 us to start and end one, the
 // partials written and read at 7 TB/s (mostly from the memory-side cache) and 9 us for joining them (eleven calls with 1 to 32 splits took that, most within 15%).
-inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus) {
+// Only runs whose partials take part_bytes at most (the longest, one per span, has none).
+inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd, int cus, int64_t part_bytes) {
   int longest_span = 1, best = 0;
   for (int i = 0; i < n; ++i)
     if (s[i].kind == 2) longest_span = std::max(longest_span, s[i].pages);
@@ -100,6 +124,7 @@ inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd,
   for (int k : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
     const int run = attend_ceil(longest_span, k);
     double all = 0, longest = 0, parts = 0, wgs = 0;
+    int64_t bytes = 0;
     for (int i = 0; i < n; ++i) {
       if (s[i].kind != 2) continue;
       const int mine = tile_split(s[i], run);
@@ -110,8 +135,10 @@ inline int tile_run(const AttendSize* s, int n, int kv_heads, int heads, int hd,
       wgs += w;
       longest = std::max(longest, us);
       if (mine > 1) parts += (double)s[i].n * heads * mine;
+      bytes += span_part_bytes(s[i], mine, heads, hd);
     }
     if (wgs == 0) break;
+    if (bytes > part_bytes) continue;
     // workgroups of like length run in whole rounds; many of them even out but for the last
     const double rounds = wgs / cus;
     const double busy = wgs > 3.0 * cus ? all / cus + longest / 2 : all / cus * (rounds > 1 ? attend_ceil((int64_t)wgs, cus) / rounds : 1.0);
