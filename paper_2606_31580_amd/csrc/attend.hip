@@ -656,8 +656,9 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-  // the scale, positive (the queries carry its sign; a score of -infinity stays one)
-  const float sc = fmaxf(fabsf(a.scale_log2), 1e-37f);
+  // the scale, positive (the queries carry its sign).  Zero is taken as the smallest number above it: a score of
+  // -infinity stays one, and the largest finite one comes to 2^-21.
+  const float sc = fmaxf(fabsf(a.scale_log2), 0x1p-149f);
 
   // staging: waves 0-3 K, 4-7 V of page w % 4 of the step
   const bool st_v = w >= SP;

@@ -178,3 +178,22 @@ def test_values_near_the_largest(kind, io, n):
     q[:, :, 0] = 2.0
     o, _ = check(kv, kind, io, held, [L.attend_span(0, n, length - n)], q)
     assert bool(torch.isfinite(o).all()) and float(o.float().abs().max()) > 2.0 ** 120
+
+
+@both
+@pytest.mark.parametrize("kind,io", [("bf16", "bf16"), ("bf16", "f32"), ("int8", "bf16")])
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -126, -(2.0 ** -126), 2.0 ** -140])
+def test_smallest_scales(kind, io, scale):
+    """Products of 2^124 times a scale of next to nothing: scores of 1/4 or none."""
+    hq, hkv, hd, length, n = 4, 2, 64, 300, 90
+    kv = cache(kind, hq, hkv, hd, pages=40, seqs=1, per_seq=40)
+    kv.add_seq(0, length)
+    rng = np.random.default_rng(51)
+    k, v = np.zeros((length, hkv, hd)), rng.standard_normal((length, hkv, hd))
+    k[:, :, 3] = 2.0 ** 62 * np.where(np.arange(length) % 3 == 0, 1.0, -0.5)[:, None]
+    k, v = (torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16).cuda() for x in (k, v))
+    L.laser_kv_write(kv, 1, [L.kv_run(0, 0, length)], k, v)
+    q = torch.zeros(n, hq, hd, dtype=IO[io], device="cuda")
+    q[:, :, 3] = 2.0 ** 62
+    # (the scores' own error: a scale of 2^-126 is exact, products with it below 1 are; `check` counts far more)
+    check(kv, kind, io, [(kept(kind, f64(k)), kept(kind, f64(v)))], [L.attend_span(0, n, length - n)], q, scale=scale)
