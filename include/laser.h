@@ -391,7 +391,8 @@ typedef struct {
  *   o = sum_t softmax_t(scale q.k_t) v_t   in o,    log sum_t exp(scale q.k_t)   in d_lse
  * (d_lse: [rows][n_q_heads] fp32, or NULL), so that outputs over parts of the keys can be combined.  A row
  * that sees nothing (or only scores of -infinity) gets o = 0 and lse = -infinity.  A position that a
- * row does not see does not touch it, whatever it holds.  Rows outside the spans keep what they hold.
+ * row does not see does not touch it, whatever it holds.  scale is finite, and so is scale times log2(e) in fp32
+ * (INVALID_ARG).  Rows outside the spans keep what they hold.
  * q and o have the same element type; o may be q itself (the same pointer and strides), and overlaps it in
  * no other way.  With bf16 rows the softmax weights are
  * rounded to bf16 before they meet V; with fp32 rows nothing is rounded below fp32.  Sums, maxima and the

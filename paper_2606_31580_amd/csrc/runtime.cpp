@@ -2463,7 +2463,8 @@ static laser_status attend(laser_kv* kv, int layer, int n_spans, const laser_att
   if (st != LASER_OK) return st;
   laser_model* m = const_cast<laser_model*>(kv->m);
   const laser_model_desc& d = m->desc;
-  if (!std::isfinite(scale)) return laser_fail(LASER_ERR_INVALID_ARG, "scale is not finite");
+  const float scale_log2 = (float)((double)scale * 1.4426950408889634);
+  if (!std::isfinite(scale_log2)) return laser_fail(LASER_ERR_INVALID_ARG, "scale times log2(e) is not finite");
   st = check_rows(q, "q", d.n_q_heads, d.head_dim, false);
   if (st == LASER_OK) st = check_rows(o, "o", d.n_q_heads, d.head_dim, true);
   if (st != LASER_OK) return st;
@@ -2503,7 +2504,7 @@ static laser_status attend(laser_kv* kv, int layer, int n_spans, const laser_att
   a.hq = d.n_q_heads;
   a.hkv = d.n_kv_heads;
   a.G = d.n_q_heads / d.n_kv_heads;
-  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.scale_log2 = scale_log2;
   a.causal = causal != 0;
   a.window = window;
   a.q_row = q->row_stride;
