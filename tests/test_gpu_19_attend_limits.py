@@ -197,3 +197,58 @@ def test_smallest_scales(kind, io, scale):
     q[:, :, 3] = 2.0 ** 62
     # (the scores' own error: a scale of 2^-126 is exact, products with it below 1 are; `check` counts far more)
     check(kv, kind, io, [(kept(kind, f64(k)), kept(kind, f64(v)))], [L.attend_span(0, n, length - n)], q, scale=scale)
+
+
+@both
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["bf16", "int8", "fp8"])
+def test_large_scores_in_chunks(kind, io):
+    """Scores of some hundreds of either sign that grow along the keys, in chunks that fill tiles: the running maximum
+    moves at every page, and rows of the other sign never move it."""
+    hq, hkv, hd, length, n = 4, 2, 64, 700, 96
+    kv = cache(kind, hq, hkv, hd, pages=60, seqs=1, per_seq=60)
+    kv.add_seq(0, length)
+    rng = np.random.default_rng(52)
+    k = rng.standard_normal((length, hkv, hd)) * 0.1 + np.linspace(-4, 4, length)[:, None, None]
+    k, v = (torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16).cuda() for x in (k, rng.standard_normal((length, hkv, hd))))
+    L.laser_kv_write(kv, 1, [L.kv_run(0, 0, length)], k, v)
+    k, v = kept(kind, f64(k)), kept(kind, f64(v))
+    q = (torch.tensor([1.0, -1.0, 0.5] * (n // 3))[:, None, None].expand(n, hq, hd)).to(IO[io]).cuda()
+    o, lse = torch.empty(n, hq, hd, dtype=IO[io], device="cuda"), torch.empty(n, hq, device="cuda")
+    L.laser_attend(kv, 1, [L.attend_span(0, n, length - n)], q, o, lse=lse, scale=2.0)
+    torch.cuda.synchronize()
+    ref, rl = attend(f64(q), k, v, length - n, 2.0)
+    # Scores: 64 fp32 additions of terms of one size and two products, 2^-24 of a sum below 600 each at most, 66 x 600 x
+    # 2^-24 = 2.4e-3 if all erred one way; errors of both signs leave the root of their number, 3e-4, and 1e-3 is
+    # allowed: every weight is off by that factor, top and bottom.  bf16 rows: weights and output by 2^-8 each.
+    top = np.abs(v).max()
+    tol = 2.0e-3 * top + (2.0 ** -8 * (top + np.abs(ref)) if io == "bf16" else 0.0)
+    assert np.abs(rl).max() > 300 and np.all(np.abs(f64(o) - ref) <= tol)
+    assert np.all(np.abs(f64(lse) - rl) <= 1.0e-3)
+
+
+@both
+@pytest.mark.parametrize("kind,io", [("int8", "bf16"), ("bf16", "f32")])
+def test_captured_chunks(kind, io):
+    """Chunks in one piece and in several, captured, replayed with other queries beside eager calls: equal bits."""
+    hq, hkv, hd = 8, 2, 128
+    lens, rowsn = [2600, 300], [200, 120]
+    kv = cache(kind, hq, hkv, hd, pages=190, seqs=2, per_seq=170)
+    fill(kv, kind, lens, hkv, hd, 53)
+    base = queries(np.random.default_rng(54), sum(rowsn), hq, hd, io)
+    spans = [L.attend_span(0, rowsn[0], lens[0] - rowsn[0]), L.attend_span(1, rowsn[1], lens[1] - rowsn[1], row0=rowsn[0])]
+    dtype = L.DTYPE_BF16 if io == "bf16" else L.DTYPE_F32
+    assert L.laser_attend_workspace(kv, spans, dtype) > 0
+    L.laser_kv_write(kv, 1, [])
+    q, o, lse = base.clone(), torch.full_like(base, 5.0), torch.full(base.shape[:2], 5.0, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        L.laser_attend(kv, 1, spans, q, o, lse=lse)
+    for i in range(4):
+        q.copy_(base * (1.0 - 0.5 * i))
+        g.replay()
+        eager, el = torch.full_like(base, 7.0), torch.empty_like(lse)
+        L.laser_attend(kv, 1, spans, q, eager, lse=el)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, o) and torch.equal(el, lse), i
