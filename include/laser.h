@@ -394,9 +394,9 @@ typedef struct {
  * row does not see does not touch it, whatever it holds.  scale is finite, and so is scale times log2(e) in fp32
  * (INVALID_ARG).  Rows outside the spans keep what they hold.
  * q and o have the same element type; o may be q itself (the same pointer and strides), and overlaps it in
- * no other way.  With bf16 rows the softmax weights are
- * rounded to bf16 before they meet V; with fp32 rows nothing is rounded below fp32.  Sums, maxima and the
- * log-sum-exp are fp32 in both.  Results do not depend on what else runs, but a row's last bits may
+ * no other way.  With bf16 rows the softmax weights are rounded before they meet V: to 16 significant bits for spans of
+ * up to 16 columns (rows times query heads of a kv head) and on fp32 caches, to bf16's 8 for longer spans; with fp32
+ * rows nothing is rounded below fp32.  Sums, maxima and the log-sum-exp are fp32 in all.  Results do not depend on what else runs, but a row's last bits may
  * change with the other spans of the call (they decide how keys are split over workgroups).
  * The workspace (laser_attend_workspace bytes, 16-byte aligned; NULL if 0; below 289 MiB) holds the partial results of
  * spans whose keys are split; calls that may run at the same time, captured ones included, need

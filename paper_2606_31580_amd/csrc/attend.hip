@@ -15,9 +15,14 @@
 // the second takes P^T as the first leaves it in its accumulators: which position stands in which slot
 // of the contraction is free, as long as V is read in the same order.
 // Types: K and V as bf16 (bf16, E4M3 and 8-bit integers are exact in it; an integer row's scale goes
-// onto the scores, and onto the weights).  bf16 queries are exact; the weights are rounded to bf16, each off
-// by at most 2^-8 of itself, as the bf16 output is anyway.  With fp32 queries and output, queries and weights
-// (and fp32 K and V) are split into three bf16 parts, which hold all 24 bits.  m, l, O: fp32.
+// onto the scores, and onto the weights).  bf16 queries are exact.  Their weights are two bf16 parts in workgroups of
+// 16 columns (one or two new tokens, and all rows of an fp32 pool; off by at most 2^-16 of themselves), where the second
+// costs about 1% (64 sequences of 3,000-14,000, 8B heads, INT8: 191.7 and 193.2 us; a chunk of 200 rows of an fp32 pool
+// 22.7 and 23.8).  In wider ones they are rounded to bf16, each off by at most 2^-8 of itself, as the bf16 output is
+// anyway: a second part there takes the time of another product (32 columns, 16 sequences of 1,000-9,000, 30 rows, 102
+// and 115 us; tiles, 4,096 rows behind 12,288, 1,040 and 1,363).  With
+// fp32 queries and output, queries and weights (and fp32 K and V) are split into three bf16 parts, which hold all 24
+// bits.  m, l, O: fp32.
 // A key that a row does not see may hold anything: its score is replaced, an integer row's weight too
 // (whatever the scale), and where the stored V itself can be infinite or NaN, pages that not every
 // column sees whole are looked through and, if one has such a value, taken row by row with the
@@ -193,12 +198,15 @@ __device__ __forceinline__ T ld_page(const char* p) {
 // pool behind 8,000 positions 125 and 92 us), and the tiles of a page share an XCD (8 rows of the 7B heads behind
 // 14,001, bf16 pool, 18.7 and 15.8 us).  Where each page is read once, cached loads cost 7%: 32 sequences, 5 rows, 94
 // us against 87.
+// (bf16 pools and rows: 254 registers, so that two workgroups fit a CU; left to itself the compiler takes 257: 8 sequences of
+// 3,000-14,000 50.8 and 52.2 us.)
 template <class KT, class IT, int HD, int NT, bool SH>
-__global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
-  constexpr int PARTS = std::is_same_v<IT, float> ? 3 : 1;    // of a query or weight
+__global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 ? 2 : 1) void k_attend_rows(AttendArgs a) {
+  constexpr int PARTS = std::is_same_v<IT, float> ? 3 : 1;    // of a query
+  constexpr int WP = PARTS == 3 ? 3 : NT == 1 ? 2 : 1;        // of a weight
   constexpr int KP = std::is_same_v<KT, float> ? 3 : 1;       // of a key or value
   constexpr bool I8 = std::is_same_v<KT, i8_t>;
-  constexpr bool INF = KP == 3 || (PARTS == 3 && sizeof(KT) == 2);  // infinities meet parts (8-bit pools have none)
+  constexpr bool INF = KP == 3 || (WP > 1 && sizeof(KT) == 2);  // infinities meet parts (8-bit pools have none)
   constexpr int NS = HD / 32, ND = HD / 16, NC = 16 * NT;
   constexpr int OS = HD + 4;  // LDS row stride (floats): 16 rows fall in different banks
   constexpr int ES = (int)sizeof(KT);
@@ -356,11 +364,11 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
     }
   };
   // products of parts i and j with i + j < 3 (the others are below 2^-24)
-  auto mma = [&](const bf16x8* x, const bf16x8* y, f32x4 acc, auto careful) {
+  auto mma = [&](const bf16x8* x, const auto& y, f32x4 acc, auto careful) {
 #pragma unroll
     for (int i = KP - 1; i >= 0; --i)
 #pragma unroll
-      for (int j = PARTS - 1; j >= 0; --j) {
+      for (int j = (int)std::extent_v<std::remove_reference_t<decltype(y)>> - 1; j >= 0; --j) {
         if (i + j >= 3) continue;
         if constexpr (decltype(careful)::value)  // (only the leading parts meet an infinity)
           acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(i + j > 0 ? finite_parts(x[i], x[0]) : x[0],
@@ -384,7 +392,7 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
 #pragma unroll
         for (int u = 0; u < NT; ++u) s[u][x] = mma(kk, q[u][k], s[u][x], careful);
       }
-    bf16x8 p[NT][PARTS];
+    bf16x8 p[NT][WP];
     uint32_t seen[NT];  // this lane's 8 positions (bits 0-3 page pg, 4-7 page pg + 1)
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
@@ -427,20 +435,21 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs a) {
         pv[i] = e;
         if constexpr (I8) pv[i] = whole || ((seen[u] >> i) & 1) ? e * b.vs[i >> 2][i & 3] : 0.f;
       }
-      u32x4 pw[PARTS];
+      u32x4 pw[WP];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (PARTS == 1) {
-          pw[0][i] = pk_bf16(pv[2 * i], pv[2 * i + 1]);
+        if constexpr (WP < 3) {
+          const uint32_t t = pw[0][i] = pk_bf16(pv[2 * i], pv[2 * i + 1]);
+          if constexpr (WP == 2) pw[1][i] = pk_bf16(pv[2 * i] - __uint_as_float(t << 16), pv[2 * i + 1] - __uint_as_float(t & 0xffff0000u));
         } else {
           uint32_t s3[3];
           split3(pv[2 * i], pv[2 * i + 1], s3);
 #pragma unroll
-          for (int k = 0; k < PARTS; ++k) pw[k][i] = s3[k];
+          for (int k = 0; k < WP; ++k) pw[k][i] = s3[k];
         }
       }
 #pragma unroll
-      for (int k = 0; k < PARTS; ++k) p[u][k] = __builtin_bit_cast(bf16x8, pw[k]);
+      for (int k = 0; k < WP; ++k) p[u][k] = __builtin_bit_cast(bf16x8, pw[k]);
     }
     bool odd = false;
     if (!I8 && (decltype(careful)::value || !whole)) {  // an infinite or NaN V anywhere in the pair?

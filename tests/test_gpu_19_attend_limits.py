@@ -252,3 +252,24 @@ def test_captured_chunks(kind, io):
         L.laser_attend(kv, 1, spans, q, eager, lse=el)
         torch.cuda.synchronize()
         assert torch.equal(eager, o) and torch.equal(el, lse), i
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8", "bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,hd,n", [(4, 2, 64, 1), (7, 1, 128, 2), (16, 1, 64, 1)])
+@pytest.mark.parametrize("length", [40, 500, 3000])
+def test_weights_of_few_columns_keep_16_bits(kind, hq, hkv, hd, n, length):
+    """bf16 rows, up to 16 columns: the output is off by its own rounding, and by 2^-16 of the values' largest."""
+    kv = cache(kind, hq, hkv, hd, pages=length // 16 + 1, seqs=1, per_seq=190)
+    held = fill(kv, kind, [length], hkv, hd, 55)
+    q = queries(np.random.default_rng(56), n, hq, hd, "bf16") * 2
+    o = torch.empty_like(q)
+    L.laser_attend(kv, 1, [L.attend_span(0, n, length - n)], q, o)
+    torch.cuda.synchronize()
+    k, v = held[0]
+    ref, _ = attend(f64(q), k, v, length - n, hd ** -0.5)
+    # Two bf16 parts: the second is what the first is off by (2^-8 of the weight at most), off by 2^-8 of that.  Scores
+    # as `tolerance` of test_gpu_17_attend has them; E4M3 and INT8 values are exact, and a scale and product of three
+    # fp32 roundings.  The output's half step is 2^-8 of itself.
+    top, terms = np.abs(v).max(), hd ** -0.5 * np.abs(f64(q)).max() * np.abs(k).max() * hd ** 0.5
+    tol = 2.0 ** -8 * np.abs(ref) * (1 + 2.0 ** -8) + (2.0 ** -16 + (4 * terms + 64) * 2.0 ** -24) * top
+    assert np.all(np.abs(f64(o) - ref) <= tol), (np.abs(f64(o) - ref) - tol).max()
