@@ -2,6 +2,7 @@
 #include "pages.hpp"
 
 #include <algorithm>
+#include <limits>
 #include <new>
 
 #include "laser.h"
@@ -52,9 +53,9 @@ int PagePool::pages_needed(int seq, int n) const {
 int PagePool::append(int seq, int n, std::vector<PageUpdate>* upd) {
   if (!live(seq)) return laser_fail(LASER_ERR_INVALID_ARG, "seq_id %d not present", seq);
   if (n < 0) return laser_fail(LASER_ERR_INVALID_ARG, "negative growth");
-  int need = pages_needed(seq, n);
-  if (pages_for(lens_[seq] + n) > max_pages_per_seq_)
+  if (n > std::numeric_limits<int>::max() - lens_[seq] || pages_for(lens_[seq] + n) > max_pages_per_seq_)
     return laser_fail(LASER_ERR_INVALID_ARG, "seq %d would exceed max_pages_per_seq", seq);
+  const int need = pages_needed(seq, n);
   if (need > (int)free_.size()) return laser_fail(LASER_ERR_OUT_OF_PAGES, "need %d pages, %d free", need, (int)free_.size());
   // (room first: an allocation that fails leaves everything as it is)
   auto room = [&](auto& v) {

@@ -28,7 +28,7 @@ class PagePool {
   bool live(int seq) const { return seq >= 0 && seq < max_seqs_ && live_[seq]; }
   int len(int seq) const { return lens_[seq]; }
   const std::vector<int>& table(int seq) const { return tables_[seq]; }
-  int pages_for(int n) const { return (n + page_size_ - 1) / page_size_; }
+  int pages_for(int n) const { return n / page_size_ + (n % page_size_ != 0); }
 
   // All of these validate first and change nothing when they fail (laser_status codes).
   int add_seq(int seq, int length, std::vector<PageUpdate>* upd);

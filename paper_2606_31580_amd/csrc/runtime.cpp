@@ -1717,8 +1717,8 @@ static laser_status check_growth(laser_model* m, laser_kv* kv, const std::vector
     const int sq = seqs[i];
     if (!kv->pool.live(sq)) return laser_fail(LASER_ERR_INVALID_ARG, "seq_id %d not present", sq);
     if (!seen.insert(sq).second) return laser_fail(LASER_ERR_INVALID_ARG, "seq_id %d repeated", sq);
+    if (grow[i] > m->desc.max_positions - kv->pool.len(sq)) return laser_fail(LASER_ERR_INVALID_ARG, "seq %d would exceed max_positions", sq);
     const int nl = kv->pool.len(sq) + grow[i];
-    if (nl > m->desc.max_positions) return laser_fail(LASER_ERR_INVALID_ARG, "seq %d would exceed max_positions", sq);
     if (kv->pool.pages_for(nl) > kv->pool.max_pages_per_seq())
       return laser_fail(LASER_ERR_INVALID_ARG, "seq %d would exceed max_pages_per_seq", sq);
     need += kv->pool.pages_needed(sq, grow[i]);
