@@ -251,7 +251,8 @@ typedef struct {
    * new key and value rounded to nearest even and saturated at +-448, decoded exactly; or
    * LASER_DTYPE_INT8 (bf16 models only): the integers q = rint(127 x / amax) (ties to even) and
    * one fp32 scale s = amax / 127 per (layer, position, kv head) for K and one for V, amax the
-   * largest magnitude of the head's vector; the cache stands for q s.  A vector with a NaN or an
+   * largest magnitude of the head's vector; the cache stands for q s.  (In fp32: exact for bf16
+   * vectors; an fp32 element within 2^-16 steps of half a step may go either way.)  A vector with a NaN or an
    * infinity reads back as NaN.  The pools of an INT8 cache are 16-byte aligned (UNSUPPORTED). */
   int kv_dtype;
 } laser_model_desc;

@@ -184,13 +184,13 @@ __device__ __forceinline__ T ld_page(const char* p) {
 
 // ---------------------------------------------------------------------------------- few columns
 // One token per sequence, or a few: every position's K and V comes once from memory and is used for
-// at most 32 columns, so memory bounds it (8-bit keys at 14k positions: 8.4 KB per page and kv head
-// for 64 matrix instructions).  A workgroup takes a tile of 16 NT columns over a share of the span's
+// at most 32 columns, so memory bounds it (INT8, head dim 128: 8.4 KB per pair of pages and kv head for 24 matrix
+// instructions with 16 columns, 32 with 32, 48 with fp32 rows).  A workgroup takes a tile of 16 NT columns over a share of the span's
 // pages; each of its 4 waves walks a run of pages by itself, straight from memory into operands (the
 // page layout makes every load contiguous), two pages ahead of the pair that it computes; no barrier
 // until the waves' (m, l, O) are joined in LDS.
-// INT8, 8B heads, 64 sequences of 3,000-14,000 positions: 192 us, 6.0 TB/s (a copy reaches 5.07); 7B heads, one
-// sequence of 14,336: 10.2 us with the join, mostly latency: a round of loads each for the arguments, the queries
+// INT8, 8B heads, 64 sequences of 3,000-14,000 positions: 193 us, 5.9 TB/s (a copy reaches 5.07); 7B heads, one
+// sequence of 14,336: 10.2-10.6 us with the join, mostly latency: a round of loads each for the arguments, the queries
 // and the first pages, some 1 us per pair of pages, the join's launch.  Workgroups of 8 waves were slower
 // at every size measured (12.1 and 208 us there), and so was a third pair in flight.
 // SH: a span of the launch has several tiles.  They read the same pages, so these stay in the caches (without SH every
