@@ -59,7 +59,13 @@ typedef enum {
   LASER_ERR_STATE = -5          /* call out of order (e.g. before finalize, destroyed handle) */
 } laser_status;
 
-typedef enum { LASER_DTYPE_F32 = 0, LASER_DTYPE_BF16 = 1, LASER_DTYPE_FP8_E4M3 = 2, LASER_DTYPE_INT8 = 3 } laser_dtype;
+typedef enum {
+  LASER_DTYPE_F32 = 0,
+  LASER_DTYPE_BF16 = 1,
+  LASER_DTYPE_FP8_E4M3 = 2,
+  LASER_DTYPE_INT8 = 3,
+  LASER_DTYPE_MXFP4 = 5
+} laser_dtype;
 
 /* Message of the last failing call on this thread ("" if none).  Owned by the library. */
 const char* laser_last_error(void);
@@ -240,7 +246,7 @@ laser_status laser_pages_destroy(laser_page_pool* pool);
  * Supported: head_dim in {64, 128}; n_q_heads a multiple of n_kv_heads with
  * G = n_q_heads/n_kv_heads <= 16; d_model a multiple of 64; d_ffn a multiple of 8;
  * n_q_heads*head_dim a multiple of 64; dtype F32 or BF16 for every tensor (and the KV
- * cache unless kv_dtype says FP8_E4M3); max_positions <= 65536. */
+ * cache unless kv_dtype says otherwise); max_positions <= 65536. */
 typedef struct {
   int n_layers, d_model, n_q_heads, n_kv_heads, head_dim, d_ffn, vocab;
   int tied_embeddings, qkv_bias, dtype;
@@ -253,7 +259,12 @@ typedef struct {
    * one fp32 scale s = amax / 127 per (layer, position, kv head) for K and one for V, amax the
    * largest magnitude of the head's vector; the cache stands for q s.  (In fp32: exact for bf16
    * vectors; an fp32 element within 2^-16 steps of half a step may go either way.)  A vector with a NaN or an
-   * infinity reads back as NaN.  The pools of an INT8 cache are 16-byte aligned (UNSUPPORTED). */
+   * infinity reads back as NaN.  The pools of an INT8 cache are 16-byte aligned (UNSUPPORTED).  Or
+   * LASER_DTYPE_MXFP4 (bf16 models only): 4-bit codes of E2M1 (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives) and one
+   * scale byte per 32 dims of a (layer, position, kv head): the block stands for code 2^e, e the smallest integer with
+   * amax <= 7 2^e, in -100 .. 125; each code the nearest, ties to the even one, at most 6 (so that nothing is off by
+   * more than half a step; blocks below 2^-102 are zeros).  A block of 32 with a NaN or an infinity reads back as NaN.
+   * 4.25 bits an element; pools aligned as INT8's. */
   int kv_dtype;
 } laser_model_desc;
 
@@ -312,7 +323,10 @@ laser_status laser_model_set_tiles(laser_model* m, void* d_buf, size_t bytes, vo
  * positions x head_dim values in the order the attention kernel's matrix-core
  * operands read them: K element (t, d) at ((d/32*4 + (d%32)/8)*16 + t)*8 + d%8, V element
  * (t, d) at ((d/16*4 + t/4)*16 + d%16)*4 + t%4 (t = position within the page).  Behind the
- * blocks of an INT8 pool are its scales, fp32 [n_layers][num_pages][n_kv_heads][16].  The
+ * blocks of an INT8 pool are its scales, fp32 [n_layers][num_pages][n_kv_heads][16].  An MXFP4 block: K word (of 8 codes,
+ * dims 8 (d/8) .. in nibbles 0 .. 7) at ((d%32)/8*16 + t)*(head_dim/32) + d/32, V word at (t/4*16 + d%16)*(head_dim/32) +
+ * d/32, position t in its byte t%4, dims d%32 < 16 in the low nibble; its scales behind the blocks, bytes
+ * [n_layers][num_pages][n_kv_heads][16][head_dim/32], exponent e as e + 127 (NaN 255).  The
  * block table is int32 [max_seqs][max_pages_per_seq].  Page size is 16. */
 typedef struct laser_kv laser_kv;
 
@@ -323,7 +337,7 @@ laser_status laser_kv_create(const laser_model* m, int num_pages, int max_seqs, 
  * undefined until imported).  OUT_OF_PAGES / INVALID_ARG leave the cache unchanged. */
 laser_status laser_kv_add_seq(laser_kv* kv, int seq_id, int length);
 /* Writes positions 0..length-1 of seq_id from d_k, d_v laid out [n_layers][length]
- * [n_kv_heads][head_dim] (KV-cache element type, bf16 for an INT8 cache; keys already rotated).  length must equal the
+ * [n_kv_heads][head_dim] (KV-cache element type, bf16 for INT8 and MXFP4 caches; keys already rotated).  length must equal the
  * sequence's length. */
 laser_status laser_kv_import(laser_kv* kv, int seq_id, const void* d_k, const void* d_v, int length, void* stream);
 /* Inverse of import: gathers all positions of seq_id into [n_layers][len][hkv][hd]. */
@@ -368,14 +382,14 @@ laser_status laser_kv_truncate(laser_kv* kv, int seq_id, int length);
 
 /* Stores rows of k and v (n_kv_heads heads; keys already rotated) in layer `layer` at the runs'
  * positions, converted to the cache's element type: fp32 as it is, bf16 rounded to nearest even, E4M3
- * rounded to nearest even and saturated at +-448, INT8 quantised as laser_model_desc says.  Positions
+ * rounded to nearest even and saturated at +-448, INT8 and MXFP4 quantised as laser_model_desc says.  Positions
  * lie below the sequence's length; no position twice, none on a page that a fork shares
  * (INVALID_ARG).  Other positions keep what they hold.  n_runs = 0 only sends the block table (k and v
  * may then be NULL). */
 laser_status laser_kv_write(laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k,
                             const laser_rows* v, void* stream);
 /* Reads the runs' positions into rows of k and v: the values that the cache stands for (INT8: q s, one
- * fp32 product), rounded once to the rows' type.  No row twice, and k and v apart (INVALID_ARG); other
+ * fp32 product; MXFP4: code 2^e, exact), rounded once to the rows' type.  No row twice, and k and v apart (INVALID_ARG); other
  * rows keep what they hold. */
 laser_status laser_kv_read(const laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k,
                            const laser_rows* v, void* stream);

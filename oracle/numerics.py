@@ -1,4 +1,4 @@
-"""bf16 and fp8 (E4M3) storage rounding, written from the formats' definitions.
+"""bf16, fp8 (E4M3), INT8 and MXFP4 storage rounding, written from the formats' definitions.
 
 Oracle (test infrastructure).  bf16 has an 8-bit significand (7 stored bits
 plus the implicit one) and fp32's exponent range.  Storing a real x in bf16
@@ -60,6 +60,45 @@ def round_int8_rows(x) -> np.ndarray:
     top = np.max(np.abs(x), axis=-1, keepdims=True)
     safe = np.where(top > 0, top, 1.0)
     return np.where(top > 0, np.rint(127.0 * x / safe) * (top / 127.0), 0.0)
+
+
+# E2M1: 1 sign bit, 2 exponent bits with bias 1, 1 fraction bit; magnitudes by code.
+E2M1_VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+MXFP4_BLOCK = 32
+MXFP4_MIN_EXP, MXFP4_MAX_EXP = -100, 125
+
+
+def mxfp4_blocks(x):
+    """Codes (0 .. 15, bit 3 the sign) and exponents of the blocks of 32 along the last axis: the exponent is the
+    smallest e with max |x| <= 7 * 2**e, held in [-100, 125], each code the nearest to x / 2**e, ties to the even code,
+    at most 6.  An exponent of 128 stands for a block with a NaN or an infinity (codes 0)."""
+    x = np.asarray(x, dtype=np.float64)
+    blocks = x.reshape(x.shape[:-1] + (x.shape[-1] // MXFP4_BLOCK, MXFP4_BLOCK))
+    odd = ~np.isfinite(blocks).all(-1, keepdims=True)
+    blocks = np.where(odd, 0.0, blocks)
+    top = np.max(np.abs(blocks), axis=-1, keepdims=True)
+    m, e = np.frexp(top)  # top = m * 2**e, 1/2 <= m < 1: 7 * 2**(e - 3) is 0.875 * 2**e
+    exp = np.clip(np.where(m > 0.875, e - 2, e - 3), MXFP4_MIN_EXP, MXFP4_MAX_EXP)
+    exp = np.where(top > 0, exp, MXFP4_MIN_EXP)
+    y = np.abs(np.ldexp(blocks, -exp))
+    mid = (E2M1_VALUES[1:] + E2M1_VALUES[:-1]) / 2
+    above = np.searchsorted(mid, y, side="left")  # borders strictly below y
+    tie = np.searchsorted(mid, y, side="right") > above
+    codes = above + (tie & (above % 2 == 1))
+    codes = np.where(odd, 0, codes + 8 * (np.signbit(blocks)))
+    return codes.reshape(x.shape), np.where(odd, 128, exp)[..., 0]
+
+
+def round_mxfp4_rows(x) -> np.ndarray:
+    """The values that the codes of mxfp4_blocks stand for; a block with a NaN or an infinity is NaN.
+
+    Returns float64 values.
+    """
+    codes, exp = mxfp4_blocks(x)
+    val = E2M1_VALUES[codes & 7] * np.where(codes & 8, -1.0, 1.0)
+    val = val.reshape(val.shape[:-1] + (val.shape[-1] // MXFP4_BLOCK, MXFP4_BLOCK))
+    e = exp[..., None]
+    return np.where(e == 128, np.nan, np.ldexp(val, np.where(e == 128, 0, e))).reshape(codes.shape)
 
 
 def fp8_e4m3_bits_to_float(bits) -> np.ndarray:

@@ -34,7 +34,7 @@ from typing import List, Mapping, Optional, Sequence
 
 import numpy as np
 
-from .numerics import as_dtype, as_float64, round_bf16, round_fp8_e4m3, round_int8_rows
+from .numerics import as_dtype, as_float64, round_bf16, round_fp8_e4m3, round_int8_rows, round_mxfp4_rows
 
 
 # --------------------------------------------------------------------------- blocks
@@ -153,7 +153,7 @@ class DecoderOracle:
     """Random-initialised decoder in float64 (or float32) with the storage rounding of its KV cache.
 
     weights: name -> array; uint16 arrays are bf16 bit patterns, other arrays are values.
-    kv_storage: "bf16", "fp8" (E4M3), "int8" (a scale per position and head), "f32" or None (no rounding, for the exact recompute invariant);
+    kv_storage: "bf16", "fp8" (E4M3), "int8" (a scale per position and head), "mxfp4" (4 bits, a scale per 32 dims), "f32" or None (no rounding, for the exact recompute invariant);
     defaults to the shape's storage dtype.
     """
 
@@ -190,6 +190,8 @@ class DecoderOracle:
             return round_fp8_e4m3(x).astype(self.dtype)
         if self.kv_storage == "int8":  # a scale per (position, head): rows are the head's vectors
             return round_int8_rows(x).astype(self.dtype)
+        if self.kv_storage == "mxfp4":
+            return round_mxfp4_rows(x).astype(self.dtype)
         if self.kv_storage == "f32":
             return x.astype(np.float32).astype(self.dtype)
         return x

@@ -25,7 +25,7 @@ PROBES = os.path.join(LIBDIR, "design_probes")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
-HIP_SOURCES = ["gemm.hip", "gemm_frag.hip", "attn.hip", "attend.hip", "kvops.hip", "misc.hip", "runtime.cpp", "pages.cpp"]
+HIP_SOURCES = ["gemm.hip", "gemm_frag.hip", "attn.hip", "attend.hip", "kvops.hip", "kvput.hip", "misc.hip", "runtime.cpp", "pages.cpp"]
 C_SOURCES = ["controller.c", "sim.c"]
 HIP_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result",

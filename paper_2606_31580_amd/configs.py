@@ -29,7 +29,7 @@ class ModelShape:
     dtype: str  # "bf16" or "f32": weight storage type (and the KV cache's unless kv_dtype is set)
     rope_theta: float
     rms_eps: float
-    kv_dtype: str = ""  # "" = dtype, "fp8" (OCP E4M3 KV cache) or "int8" (scales per position and head): bf16 models
+    kv_dtype: str = ""  # "" = dtype, "fp8" (E4M3), "int8" (a scale per position and head) or "mxfp4" (4 bits, a scale per 32 dims): bf16 models
 
     @property
     def kv_storage(self) -> str:
@@ -50,9 +50,9 @@ class ModelShape:
         return es * (self.n_layers * per_layer + self.vocab * d + d)
 
     def kv_bytes_per_token(self) -> int:
-        es = {"fp8": 1, "int8": 1, "bf16": 2}.get(self.kv_storage, 4)
-        scale = 4 if self.kv_storage == "int8" else 0
-        return self.n_layers * 2 * self.n_kv_heads * (self.head_dim * es + scale)
+        hd = self.head_dim
+        vector = {"fp8": hd, "int8": hd + 4, "mxfp4": hd // 2 + hd // 32, "bf16": 2 * hd}.get(self.kv_storage, 4 * hd)
+        return self.n_layers * 2 * self.n_kv_heads * vector
 
 
 @dataclass(frozen=True)
@@ -85,8 +85,13 @@ QWEN_1P5B_INT8KV = replace(QWEN_1P5B, name="qwen2-1.5B-shape-int8kv", kv_dtype="
 QWEN_7B_INT8KV = replace(QWEN_7B, name="qwen2-7B-shape-int8kv", kv_dtype="int8")
 LLAMA_8B_INT8KV = replace(LLAMA_8B, name="llama-8B-shape-int8kv", kv_dtype="int8")
 
+# and with a 4-bit one
+QWEN_1P5B_FP4KV = replace(QWEN_1P5B, name="qwen2-1.5B-shape-mxfp4kv", kv_dtype="mxfp4")
+QWEN_7B_FP4KV = replace(QWEN_7B, name="qwen2-7B-shape-mxfp4kv", kv_dtype="mxfp4")
+LLAMA_8B_FP4KV = replace(LLAMA_8B, name="llama-8B-shape-mxfp4kv", kv_dtype="mxfp4")
+
 SHAPES = {s.name: s for s in (TINY, QWEN_1P5B, QWEN_7B, LLAMA_8B, QWEN_1P5B_FP8KV, QWEN_7B_FP8KV, LLAMA_8B_FP8KV,
-                             QWEN_1P5B_INT8KV, QWEN_7B_INT8KV, LLAMA_8B_INT8KV)}
+                             QWEN_1P5B_INT8KV, QWEN_7B_INT8KV, LLAMA_8B_INT8KV, QWEN_1P5B_FP4KV, QWEN_7B_FP4KV, LLAMA_8B_FP4KV)}
 
 WORKLOADS = {
     w.name: w
@@ -98,9 +103,11 @@ WORKLOADS = {
         Workload("7B-b1-kv14336", QWEN_7B, 1, (14336,), 256, 64),
         Workload("7B-b1-kv14336-fp8kv", QWEN_7B_FP8KV, 1, (14336,), 256, 64),
         Workload("7B-b1-kv14336-int8kv", QWEN_7B_INT8KV, 1, (14336,), 256, 64),
+        Workload("7B-b1-kv14336-mxfp4kv", QWEN_7B_FP4KV, 1, (14336,), 256, 64),
         Workload("8B-b8-mixed", LLAMA_8B, 8, (), 64, 1, mixed=True),
         Workload("8B-b8-mixed-fp8kv", LLAMA_8B_FP8KV, 8, (), 64, 1, mixed=True),
         Workload("8B-b8-mixed-int8kv", LLAMA_8B_INT8KV, 8, (), 64, 1, mixed=True),
+        Workload("8B-b8-mixed-mxfp4kv", LLAMA_8B_FP4KV, 8, (), 64, 1, mixed=True),
     )
 }
 

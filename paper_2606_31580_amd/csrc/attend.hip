@@ -205,8 +205,8 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
   constexpr int PARTS = std::is_same_v<IT, float> ? 3 : 1;    // of a query
   constexpr int WP = PARTS == 3 ? 3 : NT == 1 ? 2 : 1;        // of a weight
   constexpr int KP = std::is_same_v<KT, float> ? 3 : 1;       // of a key or value
-  constexpr bool I8 = std::is_same_v<KT, i8_t>;
-  constexpr bool INF = KP == 3 || (WP > 1 && sizeof(KT) == 2);  // infinities meet parts (8-bit pools have none)
+  constexpr bool I8 = std::is_same_v<KT, i8_t>, F4 = std::is_same_v<KT, fp4_t>;
+  constexpr bool INF = KP == 3 || (WP > 1 && sizeof(KT) == 2);  // infinities meet parts (8- and 4-bit pools have none)
   constexpr int NS = HD / 32, ND = HD / 16, NC = 16 * NT;
   constexpr int OS = HD + 4;  // LDS row stride (floats): 16 rows fall in different banks
   constexpr int ES = (int)sizeof(KT);
@@ -267,13 +267,17 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
   }
 
   // Raw words of a pair of pages: K (position lc, dims 32 s + 8 lg ..), V (dims 16 d + lc, positions 4 lg ..).
-  using KRaw = std::conditional_t<ES == 1, u32x2, u32x4>;
-  using VRaw = std::conditional_t<ES == 1, uint32_t, std::conditional_t<ES == 2, u32x2, u32x4>>;
-  constexpr int KW = ES == 4 ? 2 : 1;
+  // (4-bit pages: a lane's words of all dims side by side, a word for 8 dims of K or for 2 dims x 4 positions of V; the
+  // scales of position lc and of positions 4 lg ..)
+  using Words = std::conditional_t<NS == 4, u32x4, u32x2>;
+  using KRaw = std::conditional_t<F4, Words, std::conditional_t<ES == 1, u32x2, u32x4>>;
+  using VRaw = std::conditional_t<F4, Words, std::conditional_t<ES == 1, uint32_t, std::conditional_t<ES == 2, u32x2, u32x4>>>;
+  constexpr int KW = ES == 4 ? 2 : 1, BB = kv_block_bytes<KT>(HD), SB = kv_scale_bytes<KT>(HD);
   struct Pair {
-    KRaw k[2][NS][KW];
-    VRaw v[2][ND];
-    f32x4 ks[2], vs[2];
+    KRaw k[2][F4 ? 1 : NS][KW];
+    VRaw v[2][F4 ? 1 : ND];
+    std::conditional_t<F4, uint32_t, f32x4> ks[2];
+    std::conditional_t<F4, Words, f32x4> vs[2];
   };
   Pair buf[2];
   // The next pair's page ids, through the scalar unit.  Past the run they are its last page's again: a pair's
@@ -289,24 +293,34 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
     for (int x = 0; x < 2; ++x) {
       const int pid = __builtin_amdgcn_readfirstlane(id[x]);
       const size_t slot = ((size_t)a.layer * a.num_pages + pid) * a.hkv + kvh;
-      const char* kb = (const char*)a.kpool + slot * (16 * HD * ES);
-      const char* vb = (const char*)a.vpool + slot * (16 * HD * ES);
+      const char* kb = (const char*)a.kpool + slot * BB;
+      const char* vb = (const char*)a.vpool + slot * BB;
+      [[maybe_unused]] const char* ksb = (const char*)a.kpool + a.scales + slot * SB;
+      [[maybe_unused]] const char* vsb = (const char*)a.vpool + a.scales + slot * SB;
+      if constexpr (F4) {
+        b.k[x][0][0] = ld_page<SH, KRaw>(kb + 4 * NS * l);
+        b.v[x][0] = ld_page<SH, VRaw>(vb + 4 * NS * l);
+        b.ks[x] = NS == 4 ? ld_global<uint32_t>(ksb + 4 * lc) : (uint32_t)ld_global<uint16_t>(ksb + 2 * lc);
+        b.vs[x] = ld_global<Words>(vsb + 4 * NS * lg);
+      } else {
 #pragma unroll
-      for (int s = 0; s < NS; ++s)
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
-        for (int y = 0; y < KW; ++y)
-          b.k[x][s][y] = ld_page<SH, KRaw>(kb + (s * 512 + 8 * l) * ES + 16 * y);
+          for (int y = 0; y < KW; ++y)
+            b.k[x][s][y] = ld_page<SH, KRaw>(kb + (s * 512 + 8 * l) * ES + 16 * y);
 #pragma unroll
-      for (int d = 0; d < ND; ++d) b.v[x][d] = ld_page<SH, VRaw>(vb + (d * 256 + 4 * l) * ES);
+        for (int d = 0; d < ND; ++d) b.v[x][d] = ld_page<SH, VRaw>(vb + (d * 256 + 4 * l) * ES);
+      }
       if constexpr (I8) {
-        b.ks[x] = ld_global<f32x4>((const char*)a.kpool + a.scales + slot * 64 + 16 * lg);
-        b.vs[x] = ld_global<f32x4>((const char*)a.vpool + a.scales + slot * 64 + 16 * lg);
+        b.ks[x] = ld_global<f32x4>(ksb + 16 * lg);
+        b.vs[x] = ld_global<f32x4>(vsb + 16 * lg);
       }
     }
     look(pg + 2);
   };
   auto key = [&](const KRaw* raw, bf16x8* k, auto careful) {
-    if constexpr (ES == 1) {
+    if constexpr (F4) {
+    } else if constexpr (ES == 1) {
       uint32_t w4[4];
       if constexpr (I8) {
         i8x4_to_bf16x4(raw[0][0], w4[0], w4[1]);
@@ -335,7 +349,8 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
   };
   // dims 16 d + lc of positions 4 lg .. of both pages
   auto value = [&](const VRaw& va, const VRaw& vb, bf16x8* v, auto careful) {
-    if constexpr (ES == 1) {
+    if constexpr (F4) {
+    } else if constexpr (ES == 1) {
       uint32_t w4[4];
       if constexpr (I8) {
         i8x4_to_bf16x4(va, w4[0], w4[1]);
@@ -363,6 +378,18 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
       for (int z = 0; z < KP; ++z) v[z] = __builtin_bit_cast(bf16x8, p[z]);
     }
   };
+  // (4-bit pages) dims 32 G + lc and 16 above of positions 4 lg .. of both pages, from their words and scales
+  auto value4 = [&](auto gc, const auto& va, const auto& vb, const auto& sa, const auto& sb, bf16x8& lo, bf16x8& hi) {
+    constexpr int G = decltype(gc)::value;
+    uint32_t x[NS], y[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) x[i] = sa[i], y[i] = sb[i];
+    u32x2 l0, h0, l1, h1;
+    fp4v_to_bf16<NS, G>(va[G], x, l0, h0);
+    fp4v_to_bf16<NS, G>(vb[G], y, l1, h1);
+    lo = __builtin_bit_cast(bf16x8, u32x4{l0[0], l0[1], l1[0], l1[1]});
+    hi = __builtin_bit_cast(bf16x8, u32x4{h0[0], h0[1], h1[0], h1[1]});
+  };
   // products of parts i and j with i + j < 3 (the others are below 2^-24)
   auto mma = [&](const bf16x8* x, const auto& y, f32x4 acc, auto careful) {
 #pragma unroll
@@ -385,13 +412,16 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
     for (int u = 0; u < NT; ++u) s[u][0] = s[u][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int k = 0; k < NS; ++k) {
+      static_for<NS>([&](auto kc) {
+        constexpr int k = decltype(kc)::value;
         bf16x8 kk[KP];
-        key(b.k[x][k], kk, careful);
+        if constexpr (F4)
+          kk[0] = __builtin_bit_cast(bf16x8, fp4x8_to_bf16(b.k[x][0][0][k], mx_arg<k>(b.ks[x])));
+        else
+          key(b.k[x][k], kk, careful);
 #pragma unroll
         for (int u = 0; u < NT; ++u) s[u][x] = mma(kk, q[u][k], s[u][x], careful);
-      }
+      });
     bf16x8 p[NT][WP];
     uint32_t seen[NT];  // this lane's 8 positions (bits 0-3 page pg, 4-7 page pg + 1)
 #pragma unroll
@@ -401,7 +431,11 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sv[4 * x + i] = s[u][x][i] * (I8 ? b.ks[x][i] * a.scale_log2 : a.scale_log2);
+        for (int i = 0; i < 4; ++i) {
+          float f = a.scale_log2;
+          if constexpr (I8) f *= b.ks[x][i];
+          sv[4 * x + i] = s[u][x][i] * f;
+        }
       if (!whole) {
         seen[u] = 0;
 #pragma unroll
@@ -456,8 +490,10 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          if constexpr (ES == 1) {
+        for (int d = 0; d < (F4 ? NS : ND); ++d) {
+          if constexpr (F4) {
+            odd |= mx_has_nan(b.vs[x][d]);
+          } else if constexpr (ES == 1) {
             uint32_t lo, hi;
             fp8x4_to_bf16x4(b.v[x][d], lo, hi);
             odd |= odd_bf16(lo) || odd_bf16(hi);
@@ -470,12 +506,24 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
         }
     }
     if (!__ballot(odd)) {
+      if constexpr (F4) {
+        static_for<NS>([&](auto gc) {
+          constexpr int G = decltype(gc)::value;
+          bf16x8 v[2][1];
+          value4(gc, b.v[0][0], b.v[1][0], b.vs[0], b.vs[1], v[0][0], v[1][0]);
 #pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        bf16x8 v[KP];
-        value(b.v[0][d], b.v[1][d], v, careful);
+          for (int y = 0; y < 2; ++y)
 #pragma unroll
-        for (int u = 0; u < NT; ++u) o[u][d] = mma(v, p[u], o[u][d], careful);
+            for (int u = 0; u < NT; ++u) o[u][2 * G + y] = mma(v[y], p[u], o[u][2 * G + y], careful);
+        });
+      } else {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          bf16x8 v[KP];
+          value(b.v[0][d], b.v[1][d], v, careful);
+#pragma unroll
+          for (int u = 0; u < NT; ++u) o[u][d] = mma(v, p[u], o[u][d], careful);
+        }
       }
     } else if constexpr (!I8) {
       // row by row: V of the positions that the row does not see is zero, and the row's columns take
@@ -489,6 +537,32 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
           const int t = 16 * (pg + (i >> 2)) + 4 * lg + (i & 3);
           vis |= (t >= begin && t <= last ? 1u : 0u) << i;
         }
+        if constexpr (F4) {  // (codes and scale of an unseen position: zeros)
+          Words va = b.v[0][0], vb = b.v[1][0], sa = b.vs[0], sb = b.vs[1];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int g = 0; g < NS; ++g) {
+              const int at = i * NS + g;
+              if (!((vis >> i) & 1)) va[g] &= ~(0xffu << (8 * i)), sa[at / 4] &= ~(0xffu << (8 * (at % 4)));
+              if (!((vis >> (4 + i)) & 1)) vb[g] &= ~(0xffu << (8 * i)), sb[at / 4] &= ~(0xffu << (8 * (at % 4)));
+            }
+          }
+          static_for<NS>([&](auto gc) {
+            constexpr int G = decltype(gc)::value;
+            bf16x8 v[2][1];
+            value4(gc, va, vb, sa, sb, v[0][0], v[1][0]);
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+              for (int u = 0; u < NT; ++u) {
+                const f32x4 t = mma(v[y], p[u], o[u][2 * G + y], careful);
+                if (crow[u] == r) o[u][2 * G + y] = t;
+              }
+          });
+          continue;
+        }
+        if constexpr (!F4)
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
           VRaw va = b.v[0][d], vb = b.v[1][d];
@@ -618,11 +692,13 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <class KT, class IT, int HD>
 __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
   constexpr int PARTS = std::is_same_v<IT, float> ? 3 : 1;
-  constexpr bool I8 = std::is_same_v<KT, i8_t>;
+  constexpr bool I8 = std::is_same_v<KT, i8_t>, F4 = std::is_same_v<KT, fp4_t>;
   constexpr bool INF = PARTS == 3 && sizeof(KT) == 2;  // infinities meet parts
   constexpr int ES = (int)sizeof(KT), NK = HD / 16, ND = HD / 32, SP = 4;  // SP: pages of a step
   constexpr int PB = 32 * HD;             // bytes of a page's K or V in LDS (bf16)
-  constexpr int NL = 16 * HD * ES / 1024; // 16-byte loads per lane for a page's K or V
+  constexpr int NL = F4 ? 1 : 16 * HD * ES / 1024; // loads per lane for a page's K or V (16 bytes; 4-bit pages, head dim 64: 8)
+  constexpr int NS = HD / 32, BB = kv_block_bytes<KT>(HD), SB = kv_scale_bytes<KT>(HD);
+  using Words = std::conditional_t<F4 && NS == 2, u32x2, u32x4>;
   static_assert(ES <= 2, "fp32 pools: the row kernel");
   constexpr int KB = PB + 128;            // (of a K page: two pages are read at once, from different banks)
   __shared__ __align__(16) char s_k[2][SP * KB], s_v[2][SP * PB];
@@ -672,15 +748,23 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
   // staging: waves 0-3 K, 4-7 V of page w % 4 of the step
   const bool st_v = w >= SP;
   const int st_p = w & (SP - 1);
-  u32x4 raw[NL];
+  Words raw[NL];
   float raw_s = 0.f;
+  [[maybe_unused]] Words raw_4 = {};  // (4-bit pages) the scales: K of position l % 16, in word 0; V of positions 4 (l / 16) ..
   auto fetch = [&](int pg) {
     const int pid = ld_const<int>(bt + min(pg + st_p, s1 - 1));  // (past the share: its last page again, unseen)
     const size_t slot = ((size_t)a.layer * a.num_pages + pid) * a.hkv + kvh;
     const char* pool = (const char*)(st_v ? a.vpool : a.kpool);
-    const char* b = pool + slot * (16 * HD * ES) + 16 * l;
+    const char* b = pool + slot * BB + (int)sizeof(Words) * l;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) raw[i] = ld_global<u32x4>(b + 1024 * i);
+    for (int i = 0; i < NL; ++i) raw[i] = ld_global<Words>(b + 1024 * i);
+    if constexpr (F4) {
+      const char* sb = pool + a.scales + slot * SB;
+      if (st_v)
+        raw_4 = ld_global<Words>(sb + 4 * NS * (l >> 4));
+      else
+        raw_4[0] = NS == 4 ? ld_global<uint32_t>(sb + 4 * (l & 15)) : (uint32_t)ld_global<uint16_t>(sb + 2 * (l & 15));
+    }
     if constexpr (I8) raw_s = ld_global<float>(pool + a.scales + slot * 64 + 4 * (l & 15));
   };
   auto convert = [&](uint32_t x, uint32_t& lo, uint32_t& hi) {
@@ -698,9 +782,15 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
   auto stage = [&](int buf, int pg, bool as_is) {
     if (!st_v) {  // as in the page: chunk (8 dims, position) at 16 bytes each
       char* d = s_k[buf] + st_p * KB;
+      if constexpr (F4)
+        static_for<NS>([&](auto gc) {
+          constexpr int G = decltype(gc)::value;
+          *(u32x4*)(d + (64 * G + l) * 16) = fp4x8_to_bf16(raw[0][G], mx_arg<G>(raw_4[0]));
+        });
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        if constexpr (ES == 2) {
+      for (int i = 0; i < (F4 ? 0 : NL); ++i) {
+        if constexpr (F4) {
+        } else if constexpr (ES == 2) {
           *(u32x4*)(d + (64 * i + l) * 16) = raw[i];
         } else {
           uint32_t t[8];
@@ -715,8 +805,16 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
       char* d = s_v[buf] + st_p * PB;
       const int left = sp.ke - 16 * (pg + st_p);  // keys of the page
       if (__builtin_expect(left < 16, 0)) {
+        if constexpr (F4) {
+          const int n = min(max(left - 4 * (l >> 4), 0), 4);
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int g = 0; g < NS; ++g)
+              if (i >= n) raw[0][g] &= ~(0xffu << (8 * i)), raw_4[(i * NS + g) / 4] &= ~(0xffu << (8 * ((i * NS + g) % 4)));
+        }
+#pragma unroll
+        for (int i = 0; i < (F4 ? 0 : NL); ++i) if constexpr (!F4) {
           const int n = min(max(left - 4 * ((64 * i + l) / (ES == 2 ? 8 : 4) % 4), 0), 4);  // keys of the 4
           const uint64_t keep = n == 4 ? ~0ull : (1ull << (8 * ES * n)) - 1;
           raw[i] &= ES == 2 ? u32x4{(uint32_t)keep, (uint32_t)(keep >> 32), (uint32_t)keep, (uint32_t)(keep >> 32)}
@@ -725,7 +823,10 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
         if ((l & 15) >= left) raw_s = 0.f;
       }
       bool odd = I8 && raw_s != 0.f && !(raw_s >= 0x1p-36f && raw_s <= 0x1p36f);
-      if constexpr (!I8)
+      if constexpr (F4)
+#pragma unroll
+        for (int i = 0; i < NS; ++i) odd |= mx_has_nan(raw_4[i]);
+      if constexpr (!I8 && !F4)
 #pragma unroll
         for (int i = 0; i < NL; ++i)
 #pragma unroll
@@ -741,13 +842,29 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
       if (l == 0) s_odd[buf][st_p] = any;
       if (__builtin_expect(any && !as_is, 0)) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) raw[i] = u32x4{0, 0, 0, 0};
+        for (int i = 0; i < NL; ++i) raw[i] = Words{};
         raw_s = 0.f;
+        raw_4 = Words{};
+      }
+      if constexpr (F4) {
+        uint32_t sw[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) sw[i] = raw_4[i];
+        const int x = l >> 4;
+        char* b = d + ((x & 1) * HD + (l & 15)) * 16 + (x >> 1) * 8;
+        static_for<NS>([&](auto gc) {
+          constexpr int G = decltype(gc)::value;
+          u32x2 lo, hi;
+          fp4v_to_bf16<NS, G>(raw[0][G], sw, lo, hi);
+          *(u32x2*)(b + 512 * G) = lo;
+          *(u32x2*)(b + 512 * G + 256) = hi;
+        });
       }
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
+      for (int i = 0; i < (F4 ? 0 : NL); ++i) {
         const int k = 64 * i + l;
-        if constexpr (ES == 2) {
+        if constexpr (F4) {
+        } else if constexpr (ES == 2) {
           const int d0 = k / 32 * 16 + 2 * (k % 8), x = k / 8 % 4;
           char* b = d + ((x & 1) * HD + d0) * 16 + (x >> 1) * 8;
           *(u32x2*)b = u32x2{raw[i][0], raw[i][1]};
@@ -1125,7 +1242,8 @@ hipError_t launch_attend(int kind, int kv_type, int io, int hd, const AttendArgs
     case 0: return go(float{});
     case 1: return go(bf16_t{});
     case 2: return go(fp8_t{});
-    default: return go(i8_t{});
+    case 3: return go(i8_t{});
+    default: return go(fp4_t{});
   }
 }
 

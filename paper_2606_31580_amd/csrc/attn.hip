@@ -47,9 +47,11 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
   constexpr int NC = 16 * NT;  // query columns of the item
   static_assert(RING || NT == 1, "two tiles: long runs");
   constexpr int OS = HD + 4;   // merge-slot row stride (floats; padded so that 16 rows fall in different bank groups)
-  constexpr int PB = 16 * HD * (int)sizeof(KT);  // bytes of a page's K (or V) block
+  constexpr int PB = kv_block_bytes<KT>(HD);     // bytes of a page's K (or V) block
   constexpr bool I8 = std::is_same_v<KT, i8_t>;  // 8-bit integers, a scale per position
-  constexpr int SB = I8 ? 256 : 0;               // the two pages' scales: K (64 bytes) and V of each
+  constexpr bool F4 = std::is_same_v<KT, fp4_t>; // 4-bit codes, a scale byte per position and 32 dims
+  constexpr int SP = kv_scale_bytes<KT>(HD);     // bytes of a page's scales of K (or V)
+  constexpr int SB = SP != 0 ? 256 : 0;          // the two pages' scales in LDS: K (in 64 bytes) and V of each
   constexpr int RBYTES = 4 * PB + SB;            // a wave's two pages, K and V of each
   constexpr int QS = HD + 8;                     // query row stride (bf16 elements; padded likewise), short runs
   constexpr int QB = RING ? NC * HD * 4 : 4 * NC * QS;  // the tile's queries: fp32, or bf16 hi rows, then lo rows
@@ -147,30 +149,53 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
   const char* ring = smem + QB + w * RBYTES;
   auto copy_page = [&](int pid, int slot) {
     const size_t blk = ((layer_base + pid) * a.hkv + kvh) * (size_t)PB + 16 * l;
+    if constexpr (PB == 512) {  // lanes 0-31 K, 32-63 V
+      copy_to_lds16<true>((const char*)(l < 32 ? a.kpool : a.vpool) + blk - 16 * (l & 32), ring0 + slot * 2 * PB);
+    } else {
 #pragma unroll
-    for (int u = 0; u < PB / 1024; ++u) {
-      copy_to_lds16<true>((const char*)a.kpool + blk + u * 1024, ring0 + slot * 2 * PB + u * 1024);
-      copy_to_lds16<true>((const char*)a.vpool + blk + u * 1024, ring0 + slot * 2 * PB + PB + u * 1024);
+      for (int u = 0; u < PB / 1024; ++u) {
+        copy_to_lds16<true>((const char*)a.kpool + blk + u * 1024, ring0 + slot * 2 * PB + u * 1024);
+        copy_to_lds16<true>((const char*)a.vpool + blk + u * 1024, ring0 + slot * 2 * PB + PB + u * 1024);
+      }
     }
-    if constexpr (I8) {  // lanes 0-3 the page's K scales, 4-7 its V scales
-      const size_t sc = a.scales + ((layer_base + pid) * a.hkv + kvh) * 64 + 16 * (l & 3);
+    if constexpr (SP != 0) {  // lanes 0-3 the page's K scales, 4-7 its V scales (32 bytes of them: twice)
+      const size_t sc = a.scales + ((layer_base + pid) * a.hkv + kvh) * SP + 16 * (l & (SP / 16 - 1));
       if (l < 8) copy_to_lds16<true>((const char*)(l < 4 ? a.kpool : a.vpool) + sc, ring0 + 4 * PB + slot * 128);
     }
   };
   constexpr int KW = sizeof(KT) == 4 ? 2 : 1;  // 16-byte K reads per k-step (fp8: one 8-byte read)
-  using KRaw = std::conditional_t<sizeof(KT) == 1, u32x2, u32x4>;
-  using VRaw = std::conditional_t<sizeof(KT) == 1, uint32_t, std::conditional_t<sizeof(KT) == 2, u32x2, u32x4>>;
-  KRaw kraw[2][NS][KW];
-  VRaw vraw[2][ND];
-  f32x4 kscale[2], vscale[2];  // (I8) of positions 4 lg ..
+  using Words = std::conditional_t<NS == 4, u32x4, u32x2>;  // (F4) a lane's words of all dims
+  using KRaw = std::conditional_t<F4, Words, std::conditional_t<sizeof(KT) == 1, u32x2, u32x4>>;
+  using VRaw = std::conditional_t<F4, Words, std::conditional_t<sizeof(KT) == 1, uint32_t, std::conditional_t<sizeof(KT) == 2, u32x2, u32x4>>>;
+  KRaw kraw[2][F4 ? 1 : NS][KW];
+  VRaw vraw[2][F4 ? 1 : ND];
+  std::conditional_t<F4, uint32_t, f32x4> kscale[2];  // (I8) of positions 4 lg ..; (F4) of position lc
+  std::conditional_t<F4, Words, f32x4> vscale[2];     // of positions 4 lg ..
+  auto read_f4 = [&](auto bufc, auto ld, const char* kb, const char* vb, const char* ksb, const char* vsb) {
+    constexpr int buf = decltype(bufc)::value;
+    kraw[buf][0][0] = ld(Words{}, kb + 4 * NS * l);
+    vraw[buf][0] = ld(Words{}, vb + 4 * NS * l);
+    if constexpr (NS == 4)
+      kscale[buf] = ld(uint32_t{}, ksb + 4 * lc);
+    else
+      kscale[buf] = ld(uint16_t{}, ksb + 2 * lc);
+    vscale[buf] = ld(Words{}, vsb + 4 * NS * lg);
+  };
   auto read_page = [&](auto bufc) {  // this lane's words of the page in a ring slot
     constexpr int buf = decltype(bufc)::value;
     const char* kb = ring + buf * 2 * PB;
     const char* vb = kb + PB;
+    if constexpr (F4) {
+      const char* sb = ring + 4 * PB + buf * 128;
+      read_f4(bufc, [](auto t, const char* p) { return *(const decltype(t)*)p; }, kb, vb, sb, sb + 64);
+      return;
+    }
+    if constexpr (!F4)
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int q = 0; q < KW; ++q) kraw[buf][s][q] = *(const KRaw*)(kb + (s * 512 + 8 * l) * sizeof(KT) + 16 * q);
+    if constexpr (!F4)
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) vraw[buf][dt] = *(const VRaw*)(vb + (dt * 256 + 4 * l) * sizeof(KT));
     if constexpr (I8) {
@@ -183,14 +208,20 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
     const size_t blk = ((layer_base + pid) * a.hkv + kvh) * (size_t)PB;
     const char* kb = (const char*)a.kpool + blk;
     const char* vb = (const char*)a.vpool + blk;
+    if constexpr (F4) {
+      const size_t sc = a.scales + ((layer_base + pid) * a.hkv + kvh) * SP;
+      read_f4(bufc, [](auto t, const char* p) { return __builtin_nontemporal_load((global_ptr<decltype(t)>)p); }, kb, vb,
+              (const char*)a.kpool + sc, (const char*)a.vpool + sc);
+    } else {
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
+      for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int q = 0; q < KW; ++q)
-        kraw[buf][s][q] = __builtin_nontemporal_load((global_ptr<KRaw>)(kb + (s * 512 + 8 * l) * sizeof(KT) + 16 * q));
+        for (int q = 0; q < KW; ++q)
+          kraw[buf][s][q] = __builtin_nontemporal_load((global_ptr<KRaw>)(kb + (s * 512 + 8 * l) * sizeof(KT) + 16 * q));
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-      vraw[buf][dt] = __builtin_nontemporal_load((global_ptr<VRaw>)(vb + (dt * 256 + 4 * l) * sizeof(KT)));
+      for (int dt = 0; dt < ND; ++dt)
+        vraw[buf][dt] = __builtin_nontemporal_load((global_ptr<VRaw>)(vb + (dt * 256 + 4 * l) * sizeof(KT)));
+    }
     if constexpr (I8) {
       const size_t sc = a.scales + ((layer_base + pid) * a.hkv + kvh) * 64 + 16 * lg;
       kscale[buf] = ld_global<f32x4>((const char*)a.kpool + sc);
@@ -207,7 +238,19 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
   };
   auto unpack = [&](int pg, auto cbc, PageOps& P) {
     constexpr int cb = decltype(cbc)::value;
-    if constexpr (sizeof(KT) == 1) {  // E4M3 and integers -> bf16 is exact: no lo part
+    if constexpr (F4) {  // 4-bit codes times their scales: exact as well
+      uint32_t sw[NS];
+#pragma unroll
+      for (int i = 0; i < NS; ++i) sw[i] = vscale[cb][i];
+      static_for<NS>([&](auto gc) {
+        constexpr int g = decltype(gc)::value;
+        P.khi[g] = __builtin_bit_cast(bf16x8, fp4x8_to_bf16(kraw[cb][0][0][g], mx_arg<g>(kscale[cb])));
+        u32x2 lo, hi;
+        fp4v_to_bf16<NS, g>(vraw[cb][0][g], sw, lo, hi);
+        P.vhi[2 * g] = __builtin_bit_cast(s16x4, lo);
+        P.vhi[2 * g + 1] = __builtin_bit_cast(s16x4, hi);
+      });
+    } else if constexpr (sizeof(KT) == 1) {  // E4M3 and integers -> bf16 is exact: no lo part
       auto to_bf16 = [](uint32_t w, uint32_t& lo, uint32_t& hi) {
         if constexpr (I8)
           i8x4_to_bf16x4(w, lo, hi);
@@ -379,7 +422,8 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int ta = pgA * 16 + 4 * lg + i, tb = pgB * 16 + 4 * lg + i;
-        const float ka = I8 ? kscale[ca][i] * a.scale_log2 : a.scale_log2, kb = I8 ? kscale[cbB][i] * a.scale_log2 : a.scale_log2;
+        float ka = a.scale_log2, kb = a.scale_log2;
+        if constexpr (I8) ka *= kscale[ca][i], kb *= kscale[cbB][i];
         sv[i] = (ta <= cpos[u]) ? sa[i] * ka : -INFINITY;
         sv[4 + i] = (hasB && tb <= cpos[u]) ? sb[i] * kb : -INFINITY;
         mloc = fmaxf(mloc, fmaxf(sv[i], sv[4 + i]));
@@ -691,7 +735,10 @@ static hipError_t launch_hd(const AttnArgs& a, dim3 grid, hipStream_t s) {
 }
 
 hipError_t launch_attn(int dtype, int hd, const AttnArgs& a, dim3 grid, hipStream_t s) {
-  if (dtype == 3) {
+  if (dtype == 4) {
+    if (hd == 128) return launch_hd<fp4_t, 128>(a, grid, s);
+    if (hd == 64) return launch_hd<fp4_t, 64>(a, grid, s);
+  } else if (dtype == 3) {
     if (hd == 128) return launch_hd<i8_t, 128>(a, grid, s);
     if (hd == 64) return launch_hd<i8_t, 64>(a, grid, s);
   } else if (dtype == 2) {

@@ -37,6 +37,22 @@ struct i8_t {
   int8_t bits;
 };
 
+// MXFP4 caches: codes of E2M1 (sign, two exponent bits, one fraction bit: 0, 1/2, 1, 3/2, 2, 3, 4, 6), two to a byte, in
+// blocks of 32 dims of a position that share a power of two 2^(b - 127), kept as the byte b (255: the block is NaN).
+struct fp4_t {
+  uint8_t bits;
+};
+
+// Bytes of a page's K or V of one kv head, and of its scales, behind all blocks of the pool.
+template <class KT>
+constexpr int kv_block_bytes(int hd) {
+  return std::is_same_v<KT, fp4_t> ? 8 * hd : 16 * hd * (int)sizeof(KT);
+}
+template <class KT>
+constexpr int kv_scale_bytes(int hd) {
+  return std::is_same_v<KT, i8_t> ? 64 : std::is_same_v<KT, fp4_t> ? hd / 2 : 0;
+}
+
 // fp32 -> E4M3 bits: round to nearest even on the E4M3 grid (spacing 2^(e-3) in binade
 // [2^e, 2^(e+1)) for e >= -6, 2^-9 below), magnitudes that round past 448 saturate to 448,
 // NaN stays NaN.
@@ -69,6 +85,41 @@ __device__ __forceinline__ void i8x4_to_bf16x4(uint32_t w, uint32_t& lo, uint32_
   lo = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
   hi = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x07060302u);
 }
+
+// MXFP4 page blocks, head dim 32 NS.  K: word s of the NS at (16 (d % 32 / 8) + t) NS holds the 8 dims d of group s (32
+// dims) at position t, dim d in nibble d % 8.  V: word g at (16 (t / 4) + d % 16) NS holds position t in byte t % 4, dim
+// 32 g + d % 16 in its low nibble and the dim 16 above in the high one: a byte has one position, so that a position is
+// written without its neighbours.  Scales: byte NS t + g.  A lane's words lie side by side (16 bytes at head dim 128).
+//
+// Byte K of a word of scales as the conversions' operand: they read its exponent field (bits 23 to 30) alone.
+template <int K>
+__device__ __forceinline__ float mx_arg(uint32_t w) {
+  return __uint_as_float(K < 3 ? w << (23 - 8 * (K < 3 ? K : 0)) : w >> 1);
+}
+// Scale of position I of four and group G, from the four positions' bytes.
+template <int NS, int I, int G>
+__device__ __forceinline__ float mx_arg_v(const uint32_t* w) {
+  return mx_arg<(I * NS + G) % 4>(w[(I * NS + G) / 4]);
+}
+// Eight codes times their scale as bf16 (exact; a NaN scale gives NaN).
+__device__ __forceinline__ u32x4 fp4x8_to_bf16(uint32_t w, float scale) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+}
+// A V word of group G as bf16, four positions of a dim: lo the dim below 16, hi the one above.
+template <int NS, int G>
+__device__ __forceinline__ void fp4v_to_bf16(uint32_t w, const uint32_t* scales, u32x2& lo, u32x2& hi) {
+  const uint32_t a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, mx_arg_v<NS, 0, G>(scales), 0));
+  const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, mx_arg_v<NS, 1, G>(scales), 1));
+  const uint32_t c = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, mx_arg_v<NS, 2, G>(scales), 2));
+  const uint32_t d = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, mx_arg_v<NS, 3, G>(scales), 3));
+  lo = u32x2{__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(d, c, 0x05040100u)};
+  hi = u32x2{__builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u)};
+}
+// Some byte of a word of scales is 255.
+__device__ __forceinline__ bool mx_has_nan(uint32_t w) { return ((((w & 0x7f7f7f7fu) + 0x01010101u) & w) & 0x80808080u) != 0; }
 
 __device__ __forceinline__ float bf2f(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
 

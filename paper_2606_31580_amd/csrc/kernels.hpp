@@ -138,7 +138,7 @@ struct GemmArgs {
   const int* bt;
   int max_pps, num_pages, layer;
   int kv_fp8;  // K/V stored as E4M3 (else in the weight type)
-  float* kv_rows;  // INT8 cache: K and V of the rows go here, [M][K, V][hkv][hd], for launch_kv_quant
+  float* kv_rows;  // INT8 and MXFP4 caches: K and V of the rows go here, [M][K, V][hkv][hd], for launch_kv_quant
   // EPI_RESID
   float* h;  // [M][N]
   // MFMA path, EPI_RESID only: K split across `ksplit` workgroups per row group (1: none).
@@ -179,7 +179,7 @@ struct AttnArgs {
   int ring;       // workspace and pools are 16-byte aligned: long runs through the LDS rings
   int tiles;      // query tiles per item (1; 2 where a group has more than 16 columns)
   char* ofrag;  // the output as fragments for the O-projection (null: fp32 rows in o)
-  size_t scales;  // INT8 pools: byte offset of the scales
+  size_t scales;  // INT8 and MXFP4 pools: byte offset of the scales
   uint32_t part_bytes, ml_bytes;
   unsigned* cnt;  // fused groups' arrival counters [hkv][kMaxGroups] x kAttnCntStride; zero between kernels
 };
@@ -263,7 +263,7 @@ hipError_t launch_resid_norm(float* h, const float* kpart, int ksplit, int M, in
 // Writes the tile-order copy of one projection's weights (the MFMA path's 16-row groups of
 // `a`, as weight_row maps them) to dst: a.n_groups groups x ceil(K/32) steps.
 hipError_t launch_tile_weights(int dtype, int epi, const GemmArgs& a, char* dst, hipStream_t s);
-// dtype: the KV element type, 0 fp32, 1 bf16, 2 fp8 (E4M3), 3 INT8.
+// dtype: the KV element type, 0 fp32, 1 bf16, 2 fp8 (E4M3), 3 INT8, 4 MXFP4.
 hipError_t launch_attn(int dtype, int hd, const AttnArgs& a, dim3 grid, hipStream_t s);
 hipError_t launch_attn_merge(const AttnArgs& a, int M, int hd, int nslots, hipStream_t s);  // nslots >= every group's nwg
 hipError_t launch_lm_reduce(const Plan* plan, const LmPart* part, int n_groups, int n_out, hipStream_t s);
@@ -306,7 +306,7 @@ struct KvRun {
 struct KvRowsArgs {
   void* kpool;
   void* vpool;
-  size_t scales;  // INT8: byte offset of the scales in a pool, [layers][pages][kv heads][16] fp32
+  size_t scales;  // byte offset of the scales in a pool: [layers][pages][kv heads][16] fp32 (INT8), [16][hd / 32] bytes (MXFP4)
   const int* bt;
   int max_pps, num_pages, layer, hkv;
   void* k;  // rows; written by the read
@@ -315,11 +315,47 @@ struct KvRowsArgs {
   int n_runs;
   KvRun runs[kKvRuns];
 };
-// kv_type: 0 fp32, 1 bf16, 2 E4M3, 3 INT8 (the cache); io: 0 fp32, 1 bf16 (the rows).
+// kv_type: 0 fp32, 1 bf16, 2 E4M3, 3 INT8, 4 MXFP4 (the cache); io: 0 fp32, 1 bf16 (the rows).
 hipError_t launch_kv_rows(int kv_type, int io, int hd, KvRowsArgs& a, int n_layers, bool write, hipStream_t s);
 
-// A forward's new rows (GemmArgs::kv_rows) into an INT8 cache at their positions.
-hipError_t launch_kv_quant(const Plan* plan, int M, const float* rows, void* kpool, void* vpool, size_t scales, const int* bt,
+// Rotation of pairs of the first rot dims of a head: element i with i + rot / 2, or 2 i with 2 i + 1.
+constexpr int kRotPairs = 128;  // of a head, at most
+struct RotArgs {
+  int rot, interleaved;
+  double amplitude;
+  double turns[kRotPairs];  // turns per position
+};
+// The same from a caller's arrays with keys rotated to their positions on the way, and queries into rows of their own
+// (laser_kv_write_rotated); MXFP4 caches are written through it without a rotation too (rotate false).
+struct KvPutArgs {
+  KvRowsArgs kv;
+  const void* q;  // or null
+  void* q_out;
+  int hq;
+  int64_t q_row, q_head, qo_row, qo_head;
+  RotArgs rot;
+};
+hipError_t launch_kv_put(int kv_type, int io, int hd, KvPutArgs& a, bool rotate, int n_layers, int cus, hipStream_t s);
+// Out of an MXFP4 cache.
+hipError_t launch_kv_get4(int io, int hd, KvRowsArgs& a, int n_layers, hipStream_t s);
+// Rows of x rotated into out (laser_rotate).
+struct RotRun {
+  int n, pos, row0, step;  // row row0 + i at position pos + step i
+  unsigned first;          // (set by the launch)
+};
+struct RotRowsArgs {
+  const void* x;
+  void* out;
+  int heads, hd;
+  int64_t x_row, x_head, out_row, out_head;
+  RotArgs rot;
+  int n_runs;
+  RotRun runs[kKvRuns];
+};
+hipError_t launch_rotate(int io, RotRowsArgs& a, int cus, hipStream_t s);
+
+// A forward's new rows (GemmArgs::kv_rows) into an INT8 or MXFP4 cache at their positions.
+hipError_t launch_kv_quant(int kv_type, const Plan* plan, int M, const float* rows, void* kpool, void* vpool, size_t scales, const int* bt,
                            int max_pps, int num_pages, int layer, int hkv, int hd, hipStream_t s);
 
 // Attention of a caller's query rows over the paged cache (laser_attend).
@@ -362,8 +398,8 @@ hipError_t launch_attend_merge(int io, int hd, bool few, const AttendArgs& a, hi
 hipError_t launch_confidence(const float* p, int T, int n, float* conf, hipStream_t s);
 hipError_t launch_fill_u32(unsigned* p, int n, unsigned v, hipStream_t s);
 hipError_t launch_atp_match(const int* tokens, int n, const unsigned* bitmap, int vocab, int* flags, hipStream_t s);
-// scales: byte offset of an INT8 pool's scales, which go with the page (0: none).
-hipError_t launch_page_copy(int kv_es, void* kpool, void* vpool, int num_pages, int n_layers, int hkv, int hd, size_t scales,
-                            int src, int dst, hipStream_t s);
+// scales: byte offset of a pool's scales, scale_bytes of which go with a block (0: none).
+hipError_t launch_page_copy(int blk_bytes, int scale_bytes, void* kpool, void* vpool, int num_pages, int n_layers, int hkv,
+                            size_t scales, int src, int dst, hipStream_t s);
 
 }  // namespace laser

@@ -18,215 +18,9 @@
 // division per row and lane more.  A single row is latency: 3.5 us.
 #include "device_common.hpp"
 #include "kernels.hpp"
+#include "kv_pack.hpp"
 
 namespace laser {
-
-namespace {
-
-// Largest of v over the hd/8 lanes that hold a row.  (Absolute values as unsigned bits order like the
-// floats, with infinity and NaN on top: a NaN is not lost.)
-template <int LD8>
-__device__ __forceinline__ uint32_t row_umax(uint32_t v) {
-  auto dpp = [](uint32_t x, auto c) { return (uint32_t)__builtin_amdgcn_update_dpp(0u, x, decltype(c)::value, 0xf, 0xf, false); };
-  v = max(v, dpp(v, std::integral_constant<int, kDppQuad1032>{}));
-  v = max(v, dpp(v, std::integral_constant<int, kDppQuad2301>{}));
-  v = max(v, dpp(v, std::integral_constant<int, kDppHalfMirror>{}));
-  if (LD8 == 4) v = max(v, dpp(v, std::integral_constant<int, kDppRowRor8>{}));
-  return v;
-}
-
-// Largest magnitude of 8 elements, as bits (a NaN is the largest).
-__device__ __forceinline__ uint32_t amax8(const float* x) {
-  float m = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; e += 2) m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, fabsf(x[e])), fabsf(x[e + 1]));
-  return __float_as_uint(m) & 0x7fffffffu;
-}
-
-// A row's scale.
-__device__ __forceinline__ float scale_of(uint32_t amax_bits) {
-  const float amax = __uint_as_float(amax_bits);
-  return amax_bits >= 0x7f800000u ? amax : amax / 127.f;
-}
-
-// What a row's elements are multiplied by and divided by: rows far from 1 are moved by a
-// power of two first, so that neither 127 x nor 1 / amax leaves the normal range.
-struct RowScale {
-  float pre, top, inv, off0;
-  __device__ __forceinline__ explicit RowScale(uint32_t amax_bits) {
-    const float amax = __uint_as_float(amax_bits);
-    const float c = amax > 0x1p100f ? 0x1p-32f : (amax < 0x1p-60f ? 0x1p64f : 1.f);
-    pre = 127.f * c;
-    top = amax * c;
-    const bool small = amax < 0x1p-100f;  // (127 / amax may leave the range: divided)
-    inv = amax_bits >= 0x7f800000u || amax == 0.f ? 0.f : small ? 1.f : pre * __builtin_amdgcn_rcpf(top);
-    off0 = small ? 1.f : 0.f;
-  }
-  // rint(127 x / amax) of 8 elements in the low bytes of t.  The sum of a product with 127 / amax and 1.5 2^23 is rounded
-  // to the integer by itself and has it in its low bits.  127 / amax from the 1-ulp reciprocal is off by less than
-  // 2^-23 + 2^-24 of itself, a product by less than 2^-15 steps; only next to half a step does that matter, and then the
-  // division decides.
-  __device__ __forceinline__ void quant8(const float* x, uint32_t* t) const {
-    constexpr float kInt = 0x1.8p23f;
-    float off = off0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float y = __builtin_fmaf(x[e], inv, kInt);
-      t[e] = __float_as_uint(y);
-      off = fmaxf(off, fabsf(__builtin_fmaf(x[e], inv, kInt - y)));
-    }
-    if (off > 0.5f - 0x1p-15f)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) t[e] = (uint32_t)(int)rintf(x[e] * pre / top);
-  }
-  // What the integers of a row without a scale (zeros, NaN, infinities) are taken as: zeros.
-  __device__ __forceinline__ uint32_t keep() const { return inv == 0.f ? 0u : ~0u; }
-};
-
-// The low bytes of four words.
-__device__ __forceinline__ uint32_t low4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  return __builtin_amdgcn_perm(b, a, 0x0c0c0400u) | __builtin_amdgcn_perm(d, c, 0x04000c0cu);
-}
-
-// Four values as E4M3 (to nearest even, saturated at +-448; NaN stays NaN).
-__device__ __forceinline__ uint32_t pk_fp8x4(const float* x) {
-  float c[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) c[i] = x[i] != x[i] ? x[i] : fminf(fmaxf(x[i], -448.f), 448.f);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false), true);
-}
-
-__device__ __forceinline__ uint16_t f2bf_any(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
-
-// 8 elements of one position in the cache's type.
-template <class KT>
-struct Piece {
-  static constexpr int W = 2 * (int)sizeof(KT);  // words
-  uint32_t w[W];
-};
-template <class KT>
-__device__ __forceinline__ Piece<KT> pack(const float* x, const RowScale* rs) {
-  Piece<KT> p;
-  if constexpr (std::is_same_v<KT, float>) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p.w[e] = __float_as_uint(x[e]);
-  } else if constexpr (std::is_same_v<KT, bf16_t>) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) p.w[e] = (uint32_t)f2bf_any(x[2 * e]) | ((uint32_t)f2bf_any(x[2 * e + 1]) << 16);
-  } else {
-    if constexpr (std::is_same_v<KT, fp8_t>) {
-      p.w[0] = pk_fp8x4(x);
-      p.w[1] = pk_fp8x4(x + 4);
-    } else {
-      uint32_t t[8];
-      rs->quant8(x, t);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) p.w[h] = low4(t[4 * h], t[4 * h + 1], t[4 * h + 2], t[4 * h + 3]) & rs->keep();
-    }
-  }
-  return p;
-}
-template <class KT>
-__device__ __forceinline__ void unpack(const Piece<KT>& p, float scale, float* x) {
-  if constexpr (std::is_same_v<KT, float>) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(p.w[e]);
-  } else if constexpr (std::is_same_v<KT, bf16_t>) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float((e & 1) ? (p.w[e >> 1] & 0xffff0000u) : (p.w[e >> 1] << 16));
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if constexpr (std::is_same_v<KT, fp8_t>) {
-        uint32_t lo, hi;
-        fp8x4_to_bf16x4(p.w[h], lo, hi);
-        x[4 * h + 0] = __uint_as_float(lo << 16);
-        x[4 * h + 1] = __uint_as_float(lo & 0xffff0000u);
-        x[4 * h + 2] = __uint_as_float(hi << 16);
-        x[4 * h + 3] = __uint_as_float(hi & 0xffff0000u);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * h + e] = (float)(int)(int8_t)(p.w[h] >> (8 * e)) * scale;
-      }
-    }
-  }
-}
-
-// Element e of a piece, as stored bits; and put back.
-template <class KT>
-__device__ __forceinline__ uint32_t get_e(const uint32_t* w, int e) {
-  if constexpr (sizeof(KT) == 4) return w[e];
-  if constexpr (sizeof(KT) == 2) return (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
-  return (w[e >> 2] >> (8 * (e & 3))) & 0xffu;
-}
-template <class KT>
-__device__ __forceinline__ void put_e(uint32_t* w, int e, uint32_t v) {
-  if constexpr (sizeof(KT) == 4) w[e] = v;
-  if constexpr (sizeof(KT) == 2) w[e >> 1] |= v << (16 * (e & 1));
-  if constexpr (sizeof(KT) == 1) w[e >> 2] |= v << (8 * (e & 3));
-}
-
-template <class KT>
-__device__ __forceinline__ void ld_words(const char* p, uint32_t* w) {
-  constexpr int W = Piece<KT>::W;
-  if constexpr (W == 2) {
-    const u32x2 v = ld_global<u32x2>(p);
-    w[0] = v[0];
-    w[1] = v[1];
-  } else {
-#pragma unroll
-    for (int q = 0; q < W / 4; ++q) {
-      const u32x4 v = ld_global<u32x4>(p + 16 * q);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[4 * q + i] = v[i];
-    }
-  }
-}
-template <class KT>
-__device__ __forceinline__ void st_words(char* p, const uint32_t* w) {
-  constexpr int W = Piece<KT>::W;
-  if constexpr (W == 2) {
-    *(u32x2*)p = u32x2{w[0], w[1]};
-  } else {
-#pragma unroll
-    for (int q = 0; q < W / 4; ++q) *(u32x4*)(p + 16 * q) = u32x4{w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]};
-  }
-}
-
-// 8 elements of a caller's row (VEC: 16-byte aligned pieces).  Rows of 16 bits are read non-temporally, so
-// that the block lines under assembly stay (14,336 rows x 8 heads x 128 into E4M3: 17.5 us, 18.9 without); in fp32 a
-// lane's two loads share lines, and it costs (8,000 rows x 4 heads x 128, INT8: 7% more).
-template <class IT, bool VEC>
-__device__ __forceinline__ void ld_row8(const void* base, int64_t e, float* x) {
-  if constexpr (VEC) {
-    Piece<IT> p;
-    const char* at = (const char*)base + e * (int64_t)sizeof(IT);
-    if constexpr (Piece<IT>::W == 4) {
-      const u32x4 v = ld_nt16(at);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p.w[i] = v[i];
-    } else {
-      ld_words<IT>(at, p.w);
-    }
-    unpack<IT>(p, 0.f, x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = ldw<IT>(base, (size_t)(e + i));
-  }
-}
-template <class IT, bool VEC>
-__device__ __forceinline__ void st_row8(void* base, int64_t e, const float* x) {
-  const Piece<IT> p = pack<IT>(x, nullptr);
-  if constexpr (VEC) {
-    st_words<IT>((char*)base + e * (int64_t)sizeof(IT), p.w);
-  } else {
-    using E = std::conditional_t<sizeof(IT) == 2, uint16_t, uint32_t>;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ((E*)base)[e + i] = (E)get_e<IT>(p.w, i);
-  }
-}
-
-}  // namespace
 
 // grid (workgroups of all runs, layers, K and V), 256 threads: thread -> (page, kv head, 4 positions, 8 dims), so
 // that a wave writes whole page blocks.
@@ -364,13 +158,47 @@ __global__ __launch_bounds__(256) void k_kv_quant(const Plan* plan, const float*
   if (d8 == 0) ((float*)(pool + scales))[slot * 16 + t] = scale_of(amax);
 }
 
-hipError_t launch_kv_quant(const Plan* plan, int M, const float* rows, void* kpool, void* vpool, size_t scales, const int* bt,
-                           int max_pps, int num_pages, int layer, int hkv, int hd, hipStream_t s) {
+// The same into an MXFP4 cache (whose formulas stand at the kernels of kvput.hip): the 4 lanes of 32 dims find their largest
+// magnitude; of V a lane and the one with the 16 dims above make a byte of each of 16 pairs of dims.
+template <int LD8>
+__global__ __launch_bounds__(256) void k_kv_quant4(const Plan* plan, const float* rows, void* kpool, void* vpool, size_t scales,
+                                                   const int* bt, int max_pps, int num_pages, int layer, int hkv) {
+  constexpr int HD = 8 << LD8, NS = HD / 32;
+  const int m = blockIdx.x, idx = blockIdx.y * 256 + threadIdx.x;
+  const int d8 = idx & ((1 << LD8) - 1), kh = idx >> LD8;
+  if (kh >= 2 * hkv) return;  // (whole rows of lanes leave together)
+  float x[8];
+  ld_row8<float, true>(rows, ((int64_t)m * 2 * hkv + kh) * HD + 8 * d8, x);
+  const RowDesc rd = row_desc(plan, m);
+  const int page = bt[(size_t)rd.seq * max_pps + (rd.pos >> 4)], t = rd.pos & 15;
+  const uint32_t b = mx_scale(umax_lanes<4>(amax8(x)));
+  const float scale = __uint_as_float(b << 23);
+  const bool is_v = kh >= hkv;
+  const size_t slot = ((size_t)layer * num_pages + page) * hkv + (is_v ? kh - hkv : kh);
+  char* pool = (char*)(is_v ? vpool : kpool);
+  char* blk = pool + slot * kv_block_bytes<fp4_t>(HD);
+  const int g = d8 >> 2;
+  float up[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) up[e] = dpp_f<kDppQuad2301>(x[e]);
+  if (!is_v) {
+    *(uint32_t*)(blk + ((16 * (d8 & 3) + t) * NS + g) * 4) = mx_pack8(x, scale);
+  } else if ((d8 & 2) == 0) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      blk[((16 * (t >> 2) + 8 * (d8 & 1) + e) * NS + g) * 4 + (t & 3)] = (char)__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[e], up[e], scale, 0);
+  }
+  if ((d8 & 3) == 0) (pool + scales)[slot * kv_scale_bytes<fp4_t>(HD) + t * NS + g] = (char)b;
+}
+
+hipError_t launch_kv_quant(int kv_type, const Plan* plan, int M, const float* rows, void* kpool, void* vpool, size_t scales,
+                           const int* bt, int max_pps, int num_pages, int layer, int hkv, int hd, hipStream_t s) {
   if (M < 1 || (hd != 64 && hd != 128)) return hipErrorInvalidValue;
   const dim3 grid(M, (2 * hkv * (hd / 8) + 255) / 256), block(256);
-  if (hd == 128)
-    return launch_k(k_kv_quant<4>, grid, block, s, plan, rows, kpool, vpool, scales, bt, max_pps, num_pages, layer, hkv);
-  return launch_k(k_kv_quant<3>, grid, block, s, plan, rows, kpool, vpool, scales, bt, max_pps, num_pages, layer, hkv);
+  auto go = [&](auto k128, auto k64) {
+    return launch_k(hd == 128 ? k128 : k64, grid, block, s, plan, rows, kpool, vpool, scales, bt, max_pps, num_pages, layer, hkv);
+  };
+  return kv_type == 4 ? go(k_kv_quant4<4>, k_kv_quant4<3>) : go(k_kv_quant<4>, k_kv_quant<3>);
 }
 
 template <class KT, class IT, int LD8>
@@ -407,7 +235,8 @@ hipError_t launch_kv_rows(int kv_type, int io, int hd, KvRowsArgs& a, int n_laye
     case 0: return go(float{});
     case 1: return go(bf16_t{});
     case 2: return go(fp8_t{});
-    default: return go(i8_t{});
+    case 3: return go(i8_t{});
+    default: return hipErrorInvalidValue;  // (MXFP4: launch_kv_put, launch_kv_get4)
   }
 }
 

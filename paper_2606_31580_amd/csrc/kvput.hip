@@ -1,0 +1,563 @@
+// Rotary positions (laser_rotate), and rows of K and V on their way into the paged cache with the keys rotated
+// (laser_kv_write_rotated); rows into and out of MXFP4 caches.
+//
+// Pair i of a head at position p turns by p f_i: y1 = a (x1 cos - x2 sin), y2 = a (x2 cos + x1 sin).  Angles are taken in
+// turns: p f_i / (2 pi) in double loses nothing that matters at any position, and what is left of the nearest whole turn goes
+// through sincospi.  The products are in double too (as fast as fp32 here), so that the sum is rounded once, to the element
+// type: in a 4-bit cache an fp32 sum on the wrong side of a border would be off by a third of the value.
+//
+// An MXFP4 cache holds, per 32 dims of a (position, kv head), the smallest e with max |x| <= 7 2^e and the codes of E2M1 nearest
+// to x / 2^e, ties to the even code, at most 6: it stands for code 2^e (kv_pack.hpp; the blocks: device_common.hpp).
+#include <cstddef>
+
+#include "device_common.hpp"
+#include "kernels.hpp"
+#include "kv_pack.hpp"
+
+namespace laser {
+
+namespace {
+
+// d rounded to fp32 such that rounding the result once more, to at most 22 bits, is rounding d: towards zero, with the last
+// bit set if that was not exact.
+__device__ __forceinline__ float to_odd(double d) {
+  const float f = (float)d;
+  const double back = f;
+  uint32_t u = __float_as_uint(f);
+  if (back != d && !(u & 1)) u += fabs(back) < fabs(d) ? 1u : -1u;
+  return __uint_as_float(u);
+}
+
+// Elements e .. e+n-1 of a row, one by one.
+template <class IT>
+__device__ __forceinline__ void ld_part(const void* base, int64_t e, int n, float* x) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = i < n ? ldw<IT>(base, (size_t)(e + i)) : 0.f;
+}
+template <class IT>
+__device__ __forceinline__ void st_part(void* base, int64_t e, int n, const float* x) {
+  using E = std::conditional_t<sizeof(IT) == 2, uint16_t, uint32_t>;
+  const Piece<IT> p = pack<IT>(x, nullptr);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) ((E*)base)[e + i] = (E)get_e<IT>(p.w, i);
+}
+
+// A row's dims in units of two pieces of at most 8: 8 pairs that turn, or 16 dims that do not.
+struct Unit {
+  int a0, n0, a1, n1;  // dims a0 .. a0+n0-1 and a1 .. a1+n1-1
+  bool turns;
+};
+__device__ __forceinline__ int turning_units(const RotArgs& r) { return (r.rot + 15) >> 4; }
+__device__ __forceinline__ int units_of(const RotArgs& r, int hd) { return turning_units(r) + ((hd - r.rot + 15) >> 4); }
+__device__ __forceinline__ Unit unit_of(const RotArgs& r, int hd, int j) {
+  const int nt = turning_units(r);
+  Unit u;
+  u.turns = j < nt;
+  if (!u.turns) {
+    u.a0 = r.rot + 16 * (j - nt);
+    u.a1 = u.a0 + 8;
+    u.n0 = min(8, hd - u.a0);
+    u.n1 = max(0, min(8, hd - u.a1));
+  } else if (r.interleaved) {
+    u.a0 = 16 * j;
+    u.a1 = u.a0 + 8;
+    u.n0 = min(8, r.rot - u.a0);
+    u.n1 = max(0, min(8, r.rot - u.a1));
+  } else {
+    u.a0 = 8 * j;
+    u.a1 = (r.rot >> 1) + u.a0;
+    u.n0 = u.n1 = min(8, (r.rot >> 1) - u.a0);
+  }
+  return u;
+}
+template <class IT, bool VEC>
+__device__ __forceinline__ void ld_unit(const void* base, int64_t e, const Unit& u, float* x) {
+  if constexpr (VEC) {
+    ld_row8<IT, true>(base, e + u.a0, x);
+    ld_row8<IT, true>(base, e + u.a1, x + 8);
+  } else {
+    ld_part<IT>(base, e + u.a0, u.n0, x);
+    ld_part<IT>(base, e + u.a1, u.n1, x + 8);
+  }
+}
+template <class IT, bool VEC>
+__device__ __forceinline__ void st_unit(void* base, int64_t e, const Unit& u, const float* x) {
+  if constexpr (VEC) {
+    st_row8<IT, true>(base, e + u.a0, x);
+    st_row8<IT, true>(base, e + u.a1, x + 8);
+  } else {
+    st_part<IT>(base, e + u.a0, u.n0, x);
+    st_part<IT>(base, e + u.a1, u.n1, x + 8);
+  }
+}
+
+// Cosines and sines of a group of positions in LDS: pair p of a position's P at (p % 8) ceil(P / 8) + p / 8, so that the
+// units of a row read side by side.
+__device__ __forceinline__ int cs_width(int pairs) { return 8 * ((pairs + 7) >> 3); }
+// (The turns are read from the argument segment itself: an index into an argument would have the compiler copy all of it
+// to scratch.)
+__device__ __forceinline__ void fill_cs(double2* cs, size_t turns_at, const RotArgs& r, int rows, int pos, int step) {
+  using Turns = const __attribute__((address_space(4))) double;
+  Turns* turns = (Turns*)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + turns_at);
+  const int pairs = r.rot >> 1, width = cs_width(pairs);
+  for (int i = threadIdx.x; i < rows * pairs; i += 256) {
+    const int t = i / pairs, p = i - t * pairs;
+    const double turn = (double)((int64_t)pos + (int64_t)step * t) * turns[p];
+    double s, c;
+    sincospi(2.0 * (turn - rint(turn)), &s, &c);
+    cs[t * width + (p & 7) * (width >> 3) + (p >> 3)] = make_double2(r.amplitude * c, r.amplitude * s);
+  }
+}
+template <bool ODD>
+__device__ __forceinline__ void turn_unit(const double2* cs, const RotArgs& r, int t, int j, float* x) {
+  const int width = cs_width(r.rot >> 1), w8 = width >> 3;
+  const double2* row = cs + t * width + j;
+  float y[16];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const double2 k = row[i * w8];
+    const double a = r.interleaved ? x[2 * i] : x[i], b = r.interleaved ? x[2 * i + 1] : x[8 + i];
+    const double u = fma(a, k.x, -(b * k.y)), v = fma(b, k.x, a * k.y);
+    y[i] = ODD ? to_odd(u) : (float)u;
+    y[8 + i] = ODD ? to_odd(v) : (float)v;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (r.interleaved) {
+      x[2 * i] = y[i];
+      x[2 * i + 1] = y[8 + i];
+    } else {
+      x[i] = y[i];
+      x[8 + i] = y[8 + i];
+    }
+  }
+}
+
+// A wave's share of dense rows: units first .. first+127 of the rows x heads x units.
+template <class IT, bool VEC>
+__device__ __forceinline__ void turn_rows(const double2* cs, const RotArgs& r, const void* x, void* out, int heads, int hd, int64_t x_row,
+                                          int64_t x_head, int64_t out_row, int64_t out_head, int row0, int rows, int first) {
+  const int nu = units_of(r, hd), all = rows * heads * nu, l = threadIdx.x & 63;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int id = first + 64 * k + l;
+    if (id >= all) break;
+    const int rh = id / nu, j = id - rh * nu, t = rh / heads, h = rh - t * heads;
+    const Unit u = unit_of(r, hd, j);
+    float v[16];
+    ld_unit<IT, VEC>(x, (int64_t)(row0 + t) * x_row + h * x_head, u, v);
+    if (u.turns) turn_unit<false>(cs, r, t, j, v);
+    st_unit<IT, VEC>(out, (int64_t)(row0 + t) * out_row + h * out_head, u, v);
+  }
+}
+
+// Within a wave: what its lanes have stored to LDS is there for the others.  (LDS instructions of a wave run in order.)
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// The run that workgroup blockIdx.x belongs to (runs are listed by their first).
+template <class Run>
+__device__ __forceinline__ int run_of(const Run* runs, int n_runs) {
+  const int lane = threadIdx.x & 63;
+  const unsigned first = lane < n_runs ? runs[lane].first : 0xffffffffu;
+  return __builtin_popcountll(__ballot(first <= blockIdx.x)) - 1;
+}
+
+}  // namespace
+
+// Dense rows: grid (groups of 16 rows of a run, shares of their units), 256 threads.
+template <class IT, bool VEC>
+__global__ __launch_bounds__(256) void k_rotate(RotRowsArgs a) {
+  __shared__ double2 s_cs[16 * kRotPairs];
+  const RotRun run = a.runs[run_of(a.runs, a.n_runs)];
+  const int i0 = 16 * (int)(blockIdx.x - run.first), rows = min(16, run.n - i0);
+  fill_cs(s_cs, offsetof(RotRowsArgs, rot) + offsetof(RotArgs, turns), a.rot, rows, run.pos + run.step * i0, run.step);
+  __syncthreads();
+  const int all = rows * a.heads * units_of(a.rot, a.hd);
+  for (int first = 128 * (blockIdx.y * 4 + (threadIdx.x >> 6)); first < all; first += 512 * gridDim.y)
+    turn_rows<IT, VEC>(s_cs, a.rot, a.x, a.out, a.heads, a.hd, a.x_row, a.x_head, a.out_row, a.out_head, run.row0 + i0, rows, first);
+}
+
+// Rows into the cache: grid (pages of all runs, shares of a page's work, layers), 256 threads.  A wave takes K or V of a kv
+// head at a time: its rows as units (K turned) into a tile of fp32 in LDS, and out of that in the order of the page block, so
+// that a block is stored in whole lines whatever the layout of pairs; or 128 units of the queries.
+template <class KT, class IT, int HD, bool ROT, bool VEC>
+__global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
+  constexpr bool F4 = std::is_same_v<KT, fp4_t>, I8 = std::is_same_v<KT, i8_t>;
+  constexpr bool ODD = F4 || std::is_same_v<KT, fp8_t> || std::is_same_v<KT, bf16_t>;  // (rounded again, to few bits)
+  constexpr int NS = HD / 32, ND = HD / 16, TS = HD + 4;  // TS: 16 rows of the tile fall in different banks
+  __shared__ double2 s_cs[ROT ? 16 * HD / 2 : 1];
+  __shared__ __align__(16) float s_tile[4][16 * TS];
+  __shared__ __align__(16) uint32_t s_scale[4][16];  // of V: fp32 (INT8), or bytes [16][NS]
+  const KvRun run = a.kv.runs[run_of(a.kv.runs, a.kv.n_runs)];
+  const int pg = (run.pos >> 4) + (int)(blockIdx.x - run.first);
+  const int lo = max(run.pos - 16 * pg, 0), hi = min(run.pos + run.n - 16 * pg, 16), rows = hi - lo;
+  const int row0 = run.row0 + 16 * pg + lo - run.pos;  // of position 16 pg + lo
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, lc = l & 15, lg = l >> 4;
+  const int page = a.kv.bt[(size_t)run.seq * a.kv.max_pps + pg], hkv = a.kv.hkv;
+  const int64_t layer = blockIdx.z;
+  if constexpr (ROT) {
+    fill_cs(s_cs, offsetof(KvPutArgs, rot) + offsetof(RotArgs, turns), a.rot, rows, 16 * pg + lo, 1);
+    __syncthreads();
+  }
+  float* tile = s_tile[w];
+  const int q_chunks = ROT && a.q != nullptr ? (rows * a.hq * units_of(a.rot, HD) + 127) / 128 : 0;
+  for (int item = blockIdx.y * 4 + w; item < 2 * hkv + q_chunks; item += 4 * gridDim.y) {
+    if (item >= 2 * hkv) {
+      turn_rows<IT, VEC>(s_cs, a.rot, a.q, a.q_out, a.hq, HD, a.q_row, a.q_head, a.qo_row, a.qo_head, row0, rows, 128 * (item - 2 * hkv));
+      continue;
+    }
+    const bool is_v = item >= hkv;
+    const int kvh = is_v ? item - hkv : item;
+    const void* src = is_v ? a.kv.v : a.kv.k;
+    const int64_t row_stride = is_v ? a.kv.v_row : a.kv.k_row;
+    const int64_t e0 = layer * (is_v ? a.kv.v_layer : a.kv.k_layer) + row0 * row_stride + kvh * (is_v ? a.kv.v_head : a.kv.k_head);
+    // ---- the rows into the tile
+    if (!is_v) {
+      const int nu = ROT && !VEC ? units_of(a.rot, HD) : ND;
+      for (int id = l; id < rows * nu; id += 64) {
+        const int t = id / nu, j = id - t * nu;
+        const Unit u = ROT ? unit_of(a.rot, HD, j) : Unit{16 * j, 8, 16 * j + 8, 8, false};
+        float x[16];
+        ld_unit<IT, VEC>(src, e0 + t * row_stride, u, x);
+        if constexpr (ROT)
+          if (u.turns) turn_unit<ODD>(s_cs, a.rot, t, j, x);
+        float* d = tile + (lo + t) * TS;
+        if constexpr (VEC) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) *(f32x4*)(d + (i < 2 ? u.a0 : u.a1 - 8) + 4 * i) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (i < u.n0) d[u.a0 + i] = x[i];
+            if (i < u.n1) d[u.a1 + i] = x[8 + i];
+          }
+        }
+      }
+    } else {
+      for (int id = l; id < rows * ND; id += 64) {
+        const int t = id / ND, j = id - t * ND;
+        float x[16];
+        ld_unit<IT, VEC>(src, e0 + t * row_stride, Unit{16 * j, 8, 16 * j + 8, 8, false}, x);
+        if constexpr (F4) {
+          const uint32_t b = mx_scale(umax_lanes<2>(max(amax8(x), amax8(x + 8))));
+          if ((j & 1) == 0) ((uint8_t*)s_scale[w])[(lo + t) * NS + (j >> 1)] = (uint8_t)b;
+        }
+        if constexpr (I8) {  // the integers, so that a column of the tile needs no scales
+          const uint32_t amax = umax_lanes<ND>(max(amax8(x), amax8(x + 8)));
+          const RowScale rs(amax);
+          uint32_t n[8];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            rs.quant8(x + 8 * h, n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[8 * h + i] = (float)(int)(int8_t)(n[i] & rs.keep());
+          }
+          if (j == 0) ((float*)s_scale[w])[lo + t] = scale_of(amax);
+        }
+        float* d = tile + (lo + t) * TS + 16 * j;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *(f32x4*)(d + 4 * i) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+      }
+    }
+    wave_sync();
+    // ---- out of it: K, lane (8 dims of 32, position lc); V, lane (4 positions, dim lc of 16)
+    const size_t slot = ((size_t)(a.kv.layer + layer) * a.kv.num_pages + page) * hkv + kvh;
+    char* pool = (char*)(is_v ? a.kv.vpool : a.kv.kpool);
+    char* blk = pool + slot * kv_block_bytes<KT>(HD);
+    char* sc = pool + a.kv.scales + slot * kv_scale_bytes<KT>(HD);
+    if (!is_v) {
+      const bool mine = lc >= lo && lc < hi;
+      float x[NS][8];
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 v = *(const f32x4*)(tile + lc * TS + 32 * s + 8 * lg + 4 * h);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[s][4 * h + i] = mine ? v[i] : 0.f;
+        }
+      if constexpr (F4) {
+        uint32_t wd[NS], b[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          b[s] = mx_scale(umax_rows(amax8(x[s])));
+          wd[s] = mx_pack8(x[s], __uint_as_float(b[s] << 23));
+        }
+        if (mine) {
+          if constexpr (NS == 4) {
+            *(u32x4*)(blk + 16 * l) = u32x4{wd[0], wd[1], wd[2], wd[3]};
+            if (lg == 0) *(uint32_t*)(sc + 4 * lc) = b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24);
+          } else {
+            *(u32x2*)(blk + 8 * l) = u32x2{wd[0], wd[1]};
+            if (lg == 0) *(uint16_t*)(sc + 2 * lc) = (uint16_t)(b[0] | (b[1] << 8));
+          }
+        }
+      } else {
+        uint32_t amax = 0;
+        if constexpr (I8) {
+#pragma unroll
+          for (int s = 0; s < NS; ++s) amax = max(amax, amax8(x[s]));
+          amax = umax_rows(amax);
+          if (mine && lg == 0) ((float*)sc)[lc] = scale_of(amax);
+        }
+        const RowScale rs(amax);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          const Piece<KT> p = pack<KT>(x[s], &rs);
+          if (mine) st_words<KT>(blk + (size_t)(64 * s + l) * 8 * sizeof(KT), p.w);
+        }
+      }
+    } else {
+      const int t0 = 4 * lg;
+      const bool whole = t0 >= lo && t0 + 4 <= hi;
+      if constexpr (F4) {
+        uint32_t s4[NS], wd[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) s4[i] = s_scale[w][lg * NS + i];
+        static_for<NS>([&](auto gc) {
+          constexpr int G = decltype(gc)::value;
+          const float* c = tile + t0 * TS + 32 * G + lc;
+          uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, c[0], c[16], mx_arg_v<NS, 0, G>(s4), 0);
+          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, c[TS], c[TS + 16], mx_arg_v<NS, 1, G>(s4), 1);
+          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, c[2 * TS], c[2 * TS + 16], mx_arg_v<NS, 2, G>(s4), 2);
+          wd[G] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, c[3 * TS], c[3 * TS + 16], mx_arg_v<NS, 3, G>(s4), 3);
+        });
+        if (whole) {
+          if constexpr (NS == 4)
+            *(u32x4*)(blk + 16 * l) = u32x4{wd[0], wd[1], wd[2], wd[3]};
+          else
+            *(u32x2*)(blk + 8 * l) = u32x2{wd[0], wd[1]};
+        } else {
+#pragma unroll
+          for (int g = 0; g < NS; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (t0 + i >= lo && t0 + i < hi) blk[(l * NS + g) * 4 + i] = (char)(wd[g] >> (8 * i));
+        }
+        if (l < 16 && l >= lo && l < hi) {
+          if constexpr (NS == 4)
+            ((uint32_t*)sc)[l] = s_scale[w][l];
+          else
+            ((uint16_t*)sc)[l] = ((const uint16_t*)s_scale[w])[l];
+        }
+      } else {
+        if constexpr (I8)
+          if (l < 16 && l >= lo && l < hi) ((uint32_t*)sc)[l] = s_scale[w][l];
+        using E = std::conditional_t<sizeof(KT) == 1, uint8_t, std::conditional_t<sizeof(KT) == 2, uint16_t, uint32_t>>;
+#pragma unroll
+        for (int d = 0; d < ND; d += 2) {  // two dims' 4 positions at a time
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[i] = tile[(t0 + i) * TS + 16 * d + lc];
+            x[4 + i] = tile[(t0 + i) * TS + 16 * d + 16 + lc];
+          }
+          Piece<KT> p;
+          if constexpr (I8) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t n[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) n[i] = (uint32_t)(int)x[4 * h + i];
+              p.w[h] = low4(n[0], n[1], n[2], n[3]);
+            }
+          } else {
+            p = pack<KT>(x, nullptr);
+          }
+          constexpr int W = Piece<KT>::W / 2;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            char* at = blk + (size_t)(64 * (d + h) + l) * 4 * sizeof(KT);
+            const uint32_t* pw = p.w + W * h;
+            if (whole) {
+              if constexpr (W == 1) *(uint32_t*)at = pw[0];
+              if constexpr (W == 2) *(u32x2*)at = u32x2{pw[0], pw[1]};
+              if constexpr (W == 4) *(u32x4*)at = u32x4{pw[0], pw[1], pw[2], pw[3]};
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (t0 + i >= lo && t0 + i < hi) ((E*)at)[i] = (E)get_e<KT>(pw, i);
+            }
+          }
+        }
+      }
+    }
+    wave_sync();  // (the next item's rows overwrite the tile)
+  }
+}
+
+// Out of an MXFP4 cache: grid (pages of all runs, shares of a page's heads, layers); a wave takes K or V of a kv head at a
+// time, decodes the block into the tile and stores its rows.
+template <class IT, int HD, bool VEC>
+__global__ __launch_bounds__(256) void k_kv_get4(KvRowsArgs a) {
+  constexpr int NS = HD / 32, ND = HD / 16, TS = HD + 4;
+  using Words = std::conditional_t<NS == 4, u32x4, u32x2>;
+  __shared__ __align__(16) float s_tile[4][16 * TS];
+  const KvRun run = a.runs[run_of(a.runs, a.n_runs)];
+  const int pg = (run.pos >> 4) + (int)(blockIdx.x - run.first);
+  const int lo = max(run.pos - 16 * pg, 0), hi = min(run.pos + run.n - 16 * pg, 16), rows = hi - lo;
+  const int row0 = run.row0 + 16 * pg + lo - run.pos;
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, lc = l & 15, lg = l >> 4;
+  const int page = a.bt[(size_t)run.seq * a.max_pps + pg];
+  const int64_t layer = blockIdx.z;
+  float* tile = s_tile[w];
+  for (int item = blockIdx.y * 4 + w; item < 2 * a.hkv; item += 4 * gridDim.y) {
+    const bool is_v = item >= a.hkv;
+    const int kvh = is_v ? item - a.hkv : item;
+    const size_t slot = ((size_t)(a.layer + layer) * a.num_pages + page) * a.hkv + kvh;
+    const char* pool = (const char*)(is_v ? a.vpool : a.kpool);
+    const Words wd = ld_global<Words>(pool + slot * kv_block_bytes<fp4_t>(HD) + 4 * NS * l);
+    const char* sc = pool + a.scales + slot * kv_scale_bytes<fp4_t>(HD);
+    if (!is_v) {
+      const uint32_t s = NS == 4 ? ld_global<uint32_t>(sc + 4 * lc) : (uint32_t)ld_global<uint16_t>(sc + 2 * lc);
+      static_for<NS>([&](auto gc) {
+        constexpr int G = decltype(gc)::value;
+        const u32x4 v = fp4x8_to_bf16(wd[G], mx_arg<G>(s));
+        float* d = tile + lc * TS + 32 * G + 8 * lg;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *(u32x4*)(d + 4 * h) = u32x4{v[2 * h] << 16, v[2 * h] & 0xffff0000u, v[2 * h + 1] << 16, v[2 * h + 1] & 0xffff0000u};
+      });
+    } else {
+      const Words sw = ld_global<Words>(sc + 4 * NS * lg);
+      uint32_t s4[NS];
+#pragma unroll
+      for (int i = 0; i < NS; ++i) s4[i] = sw[i];
+      static_for<NS>([&](auto gc) {
+        constexpr int G = decltype(gc)::value;
+        u32x2 x, y;
+        fp4v_to_bf16<NS, G>(wd[G], s4, x, y);
+        uint32_t* d = (uint32_t*)tile + 4 * lg * TS + 32 * G + lc;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          d[i * TS] = (i & 1) ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16;
+          d[i * TS + 16] = (i & 1) ? y[i >> 1] & 0xffff0000u : y[i >> 1] << 16;
+        }
+      });
+    }
+    wave_sync();
+    void* dense = is_v ? a.v : a.k;
+    const int64_t row_stride = is_v ? a.v_row : a.k_row;
+    const int64_t e0 = layer * (is_v ? a.v_layer : a.k_layer) + row0 * row_stride + kvh * (is_v ? a.v_head : a.k_head);
+    for (int id = l; id < rows * ND; id += 64) {
+      const int t = id / ND, j = id - t * ND;
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 v = *(const f32x4*)(tile + (lo + t) * TS + 16 * j + 4 * i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[4 * i + k] = v[k];
+      }
+      st_unit<IT, VEC>(dense, e0 + t * row_stride, Unit{16 * j, 8, 16 * j + 8, 8, false}, x);
+    }
+    wave_sync();
+  }
+}
+
+// Workgroups over the work of a page or a group of rows: all of a group's waves have something to do, and groups in all are
+// about 4 to a CU.
+static unsigned shares_of(uint64_t groups, int items, int cus) {
+  const uint64_t most = (uint64_t)(items + 3) / 4, want = std::max<uint64_t>(1, (4 * (uint64_t)cus + groups - 1) / groups);
+  return (unsigned)std::max<uint64_t>(1, std::min(most, want));
+}
+
+static unsigned list_pages(KvRowsArgs& a) {
+  unsigned groups = 0;
+  for (int i = 0; i < a.n_runs; ++i) {
+    KvRun& r = a.runs[i];
+    r.first = groups;
+    groups += (unsigned)((r.pos + r.n - 1) / kPage - r.pos / kPage + 1);
+  }
+  return groups;
+}
+static bool rows_on16(const KvRowsArgs& a, int es) {
+  auto on16 = [&](int64_t e) { return e * es % 16 == 0; };
+  return (((uintptr_t)a.k | (uintptr_t)a.v) & 15) == 0 && on16(a.k_row) && on16(a.k_head) && on16(a.k_layer) && on16(a.v_row) &&
+         on16(a.v_head) && on16(a.v_layer);
+}
+static bool runs_fit(const KvRowsArgs& a, int n_layers) {
+  if (a.n_runs < 1 || a.n_runs > kKvRuns || n_layers < 1 || n_layers > 65535) return false;
+  for (int i = 0; i < a.n_runs; ++i)
+    if (a.runs[i].n < 1) return false;
+  return (((uintptr_t)a.kpool | (uintptr_t)a.vpool) & 15) == 0;
+}
+
+hipError_t launch_kv_put(int kv_type, int io, int hd, KvPutArgs& a, bool rotate, int n_layers, int cus, hipStream_t s) {
+  if (!runs_fit(a.kv, n_layers) || (hd != 64 && hd != 128) || (!rotate && kv_type != 4)) return hipErrorInvalidValue;
+  if (rotate && (a.rot.rot < 2 || a.rot.rot > hd || (a.rot.rot & 1))) return hipErrorInvalidValue;
+  const int es = io == 1 ? 2 : 4;
+  auto on16 = [&](int64_t e) { return e * es % 16 == 0; };
+  bool vec = rows_on16(a.kv, es) && (!rotate || a.rot.rot % 16 == 0);
+  if (rotate && a.q != nullptr)
+    vec = vec && (((uintptr_t)a.q | (uintptr_t)a.q_out) & 15) == 0 && on16(a.q_row) && on16(a.q_head) && on16(a.qo_row) && on16(a.qo_head);
+  const unsigned groups = list_pages(a.kv);
+  int longest = 0;
+  for (int i = 0; i < a.kv.n_runs; ++i) longest = std::max(longest, std::min(a.kv.runs[i].n, kPage));
+  const int items = 2 * a.kv.hkv + (rotate && a.q != nullptr ? (longest * a.hq * (hd / 16 + 1) + 127) / 128 : 0);
+  const dim3 grid(groups, shares_of((uint64_t)groups * n_layers, items, cus), n_layers), block(256);
+  auto go = [&](auto kt, auto it, auto hdc, auto rc) {
+    using KT = decltype(kt);
+    using IT = decltype(it);
+    constexpr int HD = decltype(hdc)::value;
+    constexpr bool ROT = decltype(rc)::value;
+    return vec ? launch_k(k_kv_put<KT, IT, HD, ROT, true>, grid, block, s, a) : launch_k(k_kv_put<KT, IT, HD, ROT, false>, grid, block, s, a);
+  };
+  auto of_io = [&](auto kt, auto rc) {
+    using H = std::integral_constant<int, 128>;
+    using G = std::integral_constant<int, 64>;
+    if (io == 1) return hd == 128 ? go(kt, bf16_t{}, H{}, rc) : go(kt, bf16_t{}, G{}, rc);
+    return hd == 128 ? go(kt, float{}, H{}, rc) : go(kt, float{}, G{}, rc);
+  };
+  if (!rotate) return of_io(fp4_t{}, std::false_type{});
+  switch (kv_type) {
+    case 0: return of_io(float{}, std::true_type{});
+    case 1: return of_io(bf16_t{}, std::true_type{});
+    case 2: return of_io(fp8_t{}, std::true_type{});
+    case 3: return of_io(i8_t{}, std::true_type{});
+    default: return of_io(fp4_t{}, std::true_type{});
+  }
+}
+
+hipError_t launch_kv_get4(int io, int hd, KvRowsArgs& a, int n_layers, hipStream_t s) {
+  if (!runs_fit(a, n_layers) || (hd != 64 && hd != 128)) return hipErrorInvalidValue;
+  const bool vec = rows_on16(a, io == 1 ? 2 : 4);
+  const dim3 grid(list_pages(a), (2 * a.hkv + 3) / 4, n_layers), block(256);
+  auto go = [&](auto it, auto hdc) {
+    using IT = decltype(it);
+    constexpr int HD = decltype(hdc)::value;
+    return vec ? launch_k(k_kv_get4<IT, HD, true>, grid, block, s, a) : launch_k(k_kv_get4<IT, HD, false>, grid, block, s, a);
+  };
+  using H = std::integral_constant<int, 128>;
+  using G = std::integral_constant<int, 64>;
+  if (io == 1) return hd == 128 ? go(bf16_t{}, H{}) : go(bf16_t{}, G{});
+  return hd == 128 ? go(float{}, H{}) : go(float{}, G{});
+}
+
+hipError_t launch_rotate(int io, RotRowsArgs& a, int cus, hipStream_t s) {
+  if (a.n_runs < 1 || a.n_runs > kKvRuns || a.heads < 1 || a.hd < 2 || a.hd > 2 * kRotPairs || a.rot.rot < 2 || a.rot.rot > a.hd || (a.rot.rot & 1))
+    return hipErrorInvalidValue;
+  unsigned groups = 0;
+  int longest = 0;
+  for (int i = 0; i < a.n_runs; ++i) {
+    RotRun& r = a.runs[i];
+    if (r.n < 1) return hipErrorInvalidValue;
+    r.first = groups;
+    groups += ((unsigned)r.n + 15) / 16;
+    longest = std::max(longest, std::min(r.n, 16));
+  }
+  const int es = io == 1 ? 2 : 4;
+  auto on16 = [&](int64_t e) { return e * es % 16 == 0; };
+  const bool vec = (((uintptr_t)a.x | (uintptr_t)a.out) & 15) == 0 && on16(a.x_row) && on16(a.x_head) && on16(a.out_row) &&
+                   on16(a.out_head) && a.rot.rot % 16 == 0 && a.hd % 16 == 0;
+  const int64_t units = (int64_t)longest * a.heads * (a.hd / 16 + 2);
+  const dim3 grid(groups, shares_of(groups, (int)std::min<int64_t>((units + 127) / 128, 1 << 17), cus)), block(256);
+  if (io == 1) return vec ? launch_k(k_rotate<bf16_t, true>, grid, block, s, a) : launch_k(k_rotate<bf16_t, false>, grid, block, s, a);
+  return vec ? launch_k(k_rotate<float, true>, grid, block, s, a) : launch_k(k_rotate<float, false>, grid, block, s, a);
+}
+
+}  // namespace laser

@@ -258,7 +258,7 @@ __global__ void k_atp_match(const int* tokens, int n, const unsigned* bitmap, in
 // Copy of one page (every layer and kv head, K and V) from page src to page dst: grid
 // (n_layers * hkv), 16-byte chunks of the 16 x hd block.
 __global__ __launch_bounds__(256) void k_page_copy(void* kpool, void* vpool, int num_pages, int hkv, size_t blk_bytes,
-                                                   size_t scales, int src, int dst) {
+                                                   size_t scales, int scale_bytes, int src, int dst) {
   const int layer = blockIdx.x / hkv, h = blockIdx.x - layer * hkv;
   const size_t s_off = (((size_t)layer * num_pages + src) * hkv + h) * blk_bytes;
   const size_t d_off = (((size_t)layer * num_pages + dst) * hkv + h) * blk_bytes;
@@ -266,19 +266,17 @@ __global__ __launch_bounds__(256) void k_page_copy(void* kpool, void* vpool, int
     *(u32x4*)((char*)kpool + d_off + 16 * c) = *(const u32x4*)((const char*)kpool + s_off + 16 * c);
     *(u32x4*)((char*)vpool + d_off + 16 * c) = *(const u32x4*)((const char*)vpool + s_off + 16 * c);
   }
-  if (scales != 0 && threadIdx.x < 32) {  // an INT8 page's 16 scales of K, and of V
-    char* pool = (char*)(threadIdx.x < 16 ? kpool : vpool) + scales;
-    const int t = threadIdx.x & 15;
-    ((float*)pool)[(((size_t)layer * num_pages + dst) * hkv + h) * 16 + t] =
-        ((const float*)pool)[(((size_t)layer * num_pages + src) * hkv + h) * 16 + t];
+  if (threadIdx.x < 32 && (threadIdx.x & 15) * 4 < scale_bytes) {  // the page's scales of K, and of V
+    char* pool = (char*)(threadIdx.x < 16 ? kpool : vpool) + scales + (threadIdx.x & 15) * 4;
+    *(uint32_t*)(pool + (((size_t)layer * num_pages + dst) * hkv + h) * scale_bytes) =
+        *(const uint32_t*)(pool + (((size_t)layer * num_pages + src) * hkv + h) * scale_bytes);
   }
 }
 
-hipError_t launch_page_copy(int kv_es, void* kpool, void* vpool, int num_pages, int n_layers, int hkv, int hd, size_t scales,
-                            int src, int dst, hipStream_t s) {
-  const size_t blk_bytes = (size_t)16 * hd * kv_es;
-  return launch_k(k_page_copy, dim3(n_layers * hkv), dim3(256), s, kpool, vpool, num_pages, hkv, blk_bytes, scales, src,
-                  dst);
+hipError_t launch_page_copy(int blk_bytes, int scale_bytes, void* kpool, void* vpool, int num_pages, int n_layers, int hkv,
+                            size_t scales, int src, int dst, hipStream_t s) {
+  return launch_k(k_page_copy, dim3(n_layers * hkv), dim3(256), s, kpool, vpool, num_pages, hkv, (size_t)blk_bytes, scales,
+                  scale_bytes, src, dst);
 }
 
 hipError_t launch_embed(int dtype, const Plan* plan, int M, const void* embed, int d, int vocab, float* h, int* bt,

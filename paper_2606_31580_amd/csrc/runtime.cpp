@@ -98,7 +98,7 @@ constexpr size_t kMergeMinOBytes = (size_t)16 << 20;
 struct Layout {
   size_t xfrag, row_scale;  // the fragment path's gain times h, the rows' 1 / rms
   int frag_rows;  // rows the fragment path's buffers hold (0: it is not used)
-  size_t kv_rows;  // INT8 caches: the rows' K and V before they are quantised
+  size_t kv_rows;  // INT8 and MXFP4 caches: the rows' K and V before they are quantised
   size_t rope, h, q, o, act, kpart, kcnt, mcnt, qpart, sqpart, lm_part, attn_part, attn_ml, attn_cnt, plans, probe_p, tok_buf,
       p_buf, total;
   size_t attn_part_bytes, attn_ml_bytes, attn_cnt_bytes, kcnt_bytes, mcnt_bytes;
@@ -171,6 +171,7 @@ struct laser_model {
   int kv_es = 4;  // bytes per KV-cache element
   int kv_fp8 = 0; // KV cache in E4M3
   int kv_i8 = 0;  // KV cache in 8-bit integers with a scale per position and head
+  int kv_f4 = 0;  // KV cache in MXFP4 (kv_es 1: the least that the planners count)
   const void* embed = nullptr;
   const void* lm_head = nullptr;
   const void* final_norm = nullptr;
@@ -490,7 +491,7 @@ static Layout make_layout(const laser_model_desc& d, int max_rows, bool wide = t
   L.q = take(rows * d.n_q_heads * hd * 4);
   L.o = take(rows * d.n_q_heads * hd * 4);
   L.act = take(rows * d.d_ffn * 4);
-  if (d.kv_dtype == LASER_DTYPE_INT8) L.kv_rows = take(rows * 2 * d.n_kv_heads * hd * 4);
+  if (d.kv_dtype == LASER_DTYPE_INT8 || d.kv_dtype == LASER_DTYPE_MXFP4) L.kv_rows = take(rows * 2 * d.n_kv_heads * hd * 4);
   if (L.frag_rows) {
     L.xfrag = take(rows * d.d_model * 4);
     L.row_scale = take(rows * 4);
@@ -534,10 +535,10 @@ static laser_status check_desc(const laser_model_desc* d) {
   if (d->d_ffn % 8) return laser_fail(LASER_ERR_UNSUPPORTED, "d_ffn must be a multiple of 8");
   if ((d->n_q_heads * d->head_dim) % 64) return laser_fail(LASER_ERR_UNSUPPORTED, "n_q_heads*head_dim % 64 != 0");
   if (d->dtype != LASER_DTYPE_F32 && d->dtype != LASER_DTYPE_BF16) return laser_fail(LASER_ERR_INVALID_ARG, "bad dtype");
-  if (d->kv_dtype != 0 && d->kv_dtype != d->dtype && d->kv_dtype != LASER_DTYPE_FP8_E4M3 && d->kv_dtype != LASER_DTYPE_INT8)
-    return laser_fail(LASER_ERR_INVALID_ARG, "bad kv_dtype");
-  if ((d->kv_dtype == LASER_DTYPE_FP8_E4M3 || d->kv_dtype == LASER_DTYPE_INT8) && d->dtype != LASER_DTYPE_BF16)
-    return laser_fail(LASER_ERR_UNSUPPORTED, "an 8-bit KV cache needs bf16 weights");
+  const bool narrow = d->kv_dtype == LASER_DTYPE_FP8_E4M3 || d->kv_dtype == LASER_DTYPE_INT8 || d->kv_dtype == LASER_DTYPE_MXFP4;
+  if (d->kv_dtype != 0 && d->kv_dtype != d->dtype && !narrow) return laser_fail(LASER_ERR_INVALID_ARG, "bad kv_dtype");
+  if (narrow && d->dtype != LASER_DTYPE_BF16)
+    return laser_fail(LASER_ERR_UNSUPPORTED, "a KV cache of 8 or 4 bits needs bf16 weights");
   if (d->max_positions < 16 || d->max_positions > 65536) return laser_fail(LASER_ERR_UNSUPPORTED, "max_positions out of range");
   if (!(d->rope_theta > 1.0f) || !(d->rms_eps > 0.0f)) return laser_fail(LASER_ERR_INVALID_ARG, "bad rope_theta or rms_eps");
   return LASER_OK;
@@ -584,7 +585,8 @@ extern "C" laser_status laser_model_create(const laser_model_desc* desc, laser_m
   m->es = desc->dtype == LASER_DTYPE_BF16 ? 2 : 4;
   m->kv_fp8 = desc->kv_dtype == LASER_DTYPE_FP8_E4M3;
   m->kv_i8 = desc->kv_dtype == LASER_DTYPE_INT8;
-  m->kv_es = m->kv_fp8 || m->kv_i8 ? 1 : m->es;
+  m->kv_f4 = desc->kv_dtype == LASER_DTYPE_MXFP4;
+  m->kv_es = m->kv_fp8 || m->kv_i8 || m->kv_f4 ? 1 : m->es;
   m->layers.assign(desc->n_layers, LayerW{});
   (void)hipGetDevice(&m->device);
   {
@@ -846,19 +848,24 @@ extern "C" laser_status laser_model_destroy(laser_model* m) {
 // ----------------------------------------------------------------------------- KV cache
 
 // The cache's element type as the kernels name it.
-static int kv_type_of(const laser_model* m) { return m->kv_i8 ? 3 : m->kv_fp8 ? 2 : m->es == 2 ? 1 : 0; }
-// Blocks of a pool, and where an INT8 pool's scales start: behind all blocks.
+static int kv_type_of(const laser_model* m) { return m->kv_f4 ? 4 : m->kv_i8 ? 3 : m->kv_fp8 ? 2 : m->es == 2 ? 1 : 0; }
+// Bytes of a block (K or V of a page and kv head) and of its scales: one fp32 a position, or one byte per 32 dims.
+static int kv_block_bytes_of(const laser_model* m) { return m->kv_f4 ? kPage * m->desc.head_dim / 2 : kPage * m->desc.head_dim * m->kv_es; }
+static int kv_scale_bytes_of(const laser_model* m) {
+  return m->kv_i8 ? kPage * (int)sizeof(float) : m->kv_f4 ? kPage * m->desc.head_dim / 32 : 0;
+}
+// Blocks of a pool, and where its scales start: behind all blocks.
 static size_t kv_slots(const laser_model* m, int num_pages) {
   return (size_t)m->desc.n_layers * num_pages * m->desc.n_kv_heads;
 }
 static size_t kv_scales_offset(const laser_model* m, int num_pages) {
-  return kv_slots(m, num_pages) * kPage * m->desc.head_dim * m->kv_es;
+  return kv_slots(m, num_pages) * kv_block_bytes_of(m);
 }
 
 extern "C" laser_status laser_kv_pool_bytes(const laser_model* m, int num_pages, size_t* bytes_per_pool) {
   if (!handle_live(m)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed model");
   if (!bytes_per_pool || num_pages < 1) return laser_fail(LASER_ERR_INVALID_ARG, "bad argument");
-  *bytes_per_pool = kv_scales_offset(m, num_pages) + (m->kv_i8 ? kv_slots(m, num_pages) * kPage * sizeof(float) : 0);
+  *bytes_per_pool = kv_slots(m, num_pages) * (size_t)(kv_block_bytes_of(m) + kv_scale_bytes_of(m));
   return LASER_OK;
 }
 
@@ -870,8 +877,8 @@ extern "C" laser_status laser_kv_create(const laser_model* m, int num_pages, int
     return laser_fail(LASER_ERR_INVALID_ARG, "sizes must be positive");
   if ((long long)max_pages_per_seq * kPage > m->desc.max_positions + kPage)
     return laser_fail(LASER_ERR_INVALID_ARG, "max_pages_per_seq exceeds max_positions");
-  if (m->kv_i8 && (!aligned16(d_k_pool) || !aligned16(d_v_pool)))
-    return laser_fail(LASER_ERR_UNSUPPORTED, "the pools of an INT8 cache have to be 16-byte aligned");
+  if ((m->kv_i8 || m->kv_f4) && (!aligned16(d_k_pool) || !aligned16(d_v_pool)))
+    return laser_fail(LASER_ERR_UNSUPPORTED, "the pools of an INT8 or MXFP4 cache have to be 16-byte aligned");
   laser_kv* kv = new (std::nothrow) laser_kv(m, num_pages, max_seqs, max_pages_per_seq, d_k_pool, d_v_pool, d_block_table);
   if (!kv) return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
   handle_add(kv);
@@ -1490,7 +1497,7 @@ static laser_status launch_forward(laser_model* m, laser_kv* kv, const FwdKey& k
   base.max_pps = max_pps;
   base.num_pages = kv->pool.num_pages();
   base.kv_fp8 = m->kv_fp8;
-  base.kv_rows = m->kv_i8 ? m->wsp<float>(L.kv_rows) : nullptr;
+  base.kv_rows = m->kv_i8 || m->kv_f4 ? m->wsp<float>(L.kv_rows) : nullptr;
   base.h = h;
   base.act = m->wsp<float>(L.act);
   base.F = d.d_ffn;
@@ -1612,9 +1619,9 @@ static laser_status launch_forward(laser_model* m, laser_kv* kv, const FwdKey& k
     st = key.frag ? frag_gemm(LASER_K_QKV, EPI_QKV, a, sc.xfrag, d.d_model, nqkv, nqkv / 16, T ? T->qkv : nullptr, nullptr)
                   : gemm(LASER_K_QKV, EPI_QKV, a, d.d_model, nqkv, nqkv, key.M, T ? T->qkv : nullptr);
     if (st != LASER_OK) return st;
-    if (m->kv_i8)
+    if (m->kv_i8 || m->kv_f4)
       HIP_TRY(timed(m, LASER_K_OTHER, s, [&] {
-        return launch_kv_quant(dp, key.M, base.kv_rows, kv->kpool, kv->vpool, aa.scales, kv->bt, max_pps, aa.num_pages, li,
+        return launch_kv_quant(kv_type_of(m), dp, key.M, base.kv_rows, kv->kpool, kv->vpool, aa.scales, kv->bt, max_pps, aa.num_pages, li,
                                d.n_kv_heads, hd, s);
       }));
 
@@ -1747,7 +1754,17 @@ static KvRowsArgs kv_rows_args(const laser_kv* kv, int layer) {
   return a;
 }
 
-// All positions of a sequence between an INT8 cache and dense bf16 arrays [n_layers][len][hkv][hd].
+// Runs of rows into or out of a cache of any type.
+static hipError_t launch_rows_of(const laser_model* m, int io, KvRowsArgs& a, int n_layers, bool write, hipStream_t s) {
+  const int hd = m->desc.head_dim;
+  if (!m->kv_f4) return launch_kv_rows(kv_type_of(m), io, hd, a, n_layers, write, s);
+  if (!write) return launch_kv_get4(io, hd, a, n_layers, s);
+  KvPutArgs p{};
+  p.kv = a;
+  return launch_kv_put(kv_type_of(m), io, hd, p, false, n_layers, m->cus, s);
+}
+
+// All positions of a sequence between an INT8 or MXFP4 cache and dense bf16 arrays [n_layers][len][hkv][hd].
 static laser_status kv_dense(laser_kv* kv, int seq, void* d_k, void* d_v, bool write, hipStream_t s) {
   const laser_model* m = kv->m;
   const laser_model_desc& d = m->desc;
@@ -1762,7 +1779,7 @@ static laser_status kv_dense(laser_kv* kv, int seq, void* d_k, void* d_v, bool w
   a.k_layer = a.v_layer = a.k_row * len;
   a.n_runs = 1;
   a.runs[0] = KvRun{seq, 0, len, 0, 0};
-  HIP_TRY(launch_kv_rows(kv_type_of(m), 1, d.head_dim, a, d.n_layers, write, s));
+  HIP_TRY(launch_rows_of(m, 1, a, d.n_layers, write, s));
   return LASER_OK;
 }
 
@@ -1777,7 +1794,7 @@ extern "C" laser_status laser_kv_import(laser_kv* kv, int seq_id, const void* d_
   laser_status st = flush_pending(kv, m, s);
   if (st != LASER_OK) return st;
   const laser_model_desc& d = m->desc;
-  if (m->kv_i8) return kv_dense(kv, seq_id, const_cast<void*>(d_k), const_cast<void*>(d_v), true, s);
+  if (m->kv_i8 || m->kv_f4) return kv_dense(kv, seq_id, const_cast<void*>(d_k), const_cast<void*>(d_v), true, s);
   HIP_TRY(launch_kv_copy(m->kv_es, 1, kv->kpool, kv->vpool, kv->bt, kv->pool.max_pages_per_seq(),
                          kv->pool.num_pages(), d.n_layers, d.n_kv_heads, d.head_dim, seq_id, length,
                          const_cast<void*>(d_k), const_cast<void*>(d_v), s));
@@ -1795,7 +1812,7 @@ extern "C" laser_status laser_kv_export(const laser_kv* kvc, int seq_id, void* d
   laser_status st = flush_pending(kv, m, s);
   if (st != LASER_OK) return st;
   const laser_model_desc& d = m->desc;
-  if (m->kv_i8) return kv_dense(kv, seq_id, d_k, d_v, false, s);
+  if (m->kv_i8 || m->kv_f4) return kv_dense(kv, seq_id, d_k, d_v, false, s);
   HIP_TRY(launch_kv_copy(m->kv_es, 0, kv->kpool, kv->vpool, kv->bt, kv->pool.max_pages_per_seq(),
                          kv->pool.num_pages(), d.n_layers, d.n_kv_heads, d.head_dim, seq_id, kv->pool.len(seq_id), d_k, d_v, s));
   return LASER_OK;
@@ -2117,8 +2134,8 @@ extern "C" laser_status laser_kv_fork(laser_kv* kv, int src_seq, int dst_seq, vo
     const laser_model_desc& d = m->desc;
     TimingScope scope(m);
     const hipError_t e = timed(m, LASER_K_OTHER, s, [&] {
-      return launch_page_copy(m->kv_es, kv->kpool, kv->vpool, kv->pool.num_pages(), d.n_layers,
-                              d.n_kv_heads, d.head_dim, m->kv_i8 ? kv_scales_offset(m, kv->pool.num_pages()) : 0, c.src, c.dst, s);
+      return launch_page_copy(kv_block_bytes_of(m), kv_scale_bytes_of(m), kv->kpool, kv->vpool, kv->pool.num_pages(), d.n_layers,
+                              d.n_kv_heads, kv_scales_offset(m, kv->pool.num_pages()), c.src, c.dst, s);
     });
     if (e != hipSuccess) return laser_fail(LASER_ERR_HIP, "page copy: %s", hipGetErrorString(e));
   }
@@ -2351,7 +2368,7 @@ laser_status kv_rows(laser_kv* kv, int layer, int n_runs, const laser_kv_run* ru
       if (runs[i].n > 0) a.runs[a.n_runs++] = KvRun{runs[i].seq, runs[i].pos, runs[i].n, runs[i].row0, 0};
     if (a.n_runs == 0) break;
     HIP_TRY(timed(m, LASER_K_OTHER, s, [&] {
-      return launch_kv_rows(kv_type_of(m), k->dtype == LASER_DTYPE_BF16, d.head_dim, a, 1, write, s);
+      return launch_rows_of(m, k->dtype == LASER_DTYPE_BF16, a, 1, write, s);
     }));
   }
   return LASER_OK;
