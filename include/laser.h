@@ -14,8 +14,10 @@
  *   laser_step_mixed         decode for a batch plus probe chunks for a subset, one forward
  *   laser_kv_fork, laser_forward, laser_confidence
  *                            the pieces of a probe that rides along with later decode steps
- *   laser_kv_write, laser_kv_read, laser_attend
+ *   laser_kv_write, laser_kv_write_rotated, laser_kv_read, laser_attend
  *                            a caller's own rows of K, V and queries on the paged cache
+ *   laser_rotate, laser_rope_frequencies
+ *                            rotary positions of a caller's own rows, scaled for long contexts
  *   laser_exit_decision      the host-side ATP decision (Eq. 5 threshold, Algorithm 1)
  *   laser_budget             the budget pre-allocation of Eq. 6-8
  *   laser_atp_match          device-side ATP detection (token-set membership)
@@ -393,6 +395,60 @@ laser_status laser_kv_write(laser_kv* kv, int layer, int n_runs, const laser_kv_
  * rows keep what they hold. */
 laser_status laser_kv_read(const laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k,
                            const laser_rows* v, void* stream);
+
+/* Rotary positions.  Pair i of a head at position p turns by the angle p inv_freq[i]:
+ *   y1 = amplitude (x1 cos - x2 sin),  y2 = amplitude (x2 cos + x1 sin),
+ * x1 and x2 the elements i and i + rot_dim / 2 (LASER_ROPE_HALF, as the model's own forward has them) or 2 i and 2 i + 1
+ * (LASER_ROPE_INTERLEAVED) of the head's vector; elements from rot_dim on are left as they are.  The angle and the sums are in
+ * double, and the result is rounded once to the type it is kept in (bf16 rows: over fp32).  rot_dim is even, 2 to head_dim;
+ * inv_freq holds rot_dim / 2 finite host values below 2^20 in magnitude, read during the call. */
+enum { LASER_ROPE_HALF = 0, LASER_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  int32_t head_dim, rot_dim, layout;
+  double amplitude; /* 1, or what the frequencies' scaling asks for */
+  const double* inv_freq;
+} laser_rope;
+
+/* Frequencies for contexts longer than a model was trained for.  With f_i = theta^(-2i/rot_dim):
+ *   PLAIN   f_i
+ *   LINEAR  f_i / factor: positions interpolated
+ *   BASE    theta replaced by theta factor^(rot_dim / (rot_dim - 2)): the slowest pair factor times slower, the fastest as it was
+ *   BANDS   by the turns n_i = old_positions f_i / (2 pi) that a pair makes in the old context: f_i from `high` turns on,
+ *           f_i / factor up to `low`, and f_i (w + (1 - w) / factor), w = (n_i - low) / (high - low), between
+ *   RAMP    f_i (1 - r_i + r_i / factor) with r_i rising linearly along the pairs from 0 to 1 between a = the floor of d(high) and
+ *           b = the ceiling of d(low), d(n) = rot_dim ln(old_positions / (2 pi n)) / (2 ln theta), a and b held in
+ *           [0, rot_dim - 1], b - a at least 0.001; the amplitude is 1 + 0.1 ln factor (otherwise 1).
+ * scaling may be NULL (PLAIN).  Writes rot_dim / 2 values and the amplitude.  Host only.  INVALID_ARG: NULL, an odd or
+ * non-positive rot_dim, theta not above 1, an unknown kind, a factor that is not positive (RAMP: below 1), old_positions or low not positive,
+ * high not above low, or anything that is not finite. */
+enum { LASER_ROPE_PLAIN = 0, LASER_ROPE_LINEAR = 1, LASER_ROPE_BASE = 2, LASER_ROPE_BANDS = 3, LASER_ROPE_RAMP = 4 };
+typedef struct {
+  int32_t kind;
+  double factor, old_positions, low, high;
+} laser_rope_scaling;
+laser_status laser_rope_frequencies(int rot_dim, double theta, const laser_rope_scaling* scaling, double* inv_freq,
+                                    double* amplitude);
+
+/* Row row0 + i is at position pos + step i, i < n: step 1 for rows of consecutive positions, -1 with -pos to turn them back
+ * (amplitude 1), 0 to move rows that are rotated already by pos. */
+typedef struct {
+  int32_t n, pos, row0, step;
+} laser_rotate_run;
+
+/* Rotates the runs' rows of x (`heads` heads of rope->head_dim, 2 to 256, elements) into out, of x's type; out may be x itself (the
+ * same pointer and strides), and overlaps it in no other way.  A row is in one run at most (INVALID_ARG); other rows of out keep
+ * what they hold.  On the current device; may be captured into a graph. */
+laser_status laser_rotate(const laser_rope* rope, int n_runs, const laser_rotate_run* runs, int heads, const laser_rows* x,
+                          const laser_rows* out, void* stream);
+
+/* laser_kv_write with the keys rotated to their positions on the way: key row row0 + i of a run is turned to position pos + i
+ * and then kept in the cache's type, rounded once (INT8: from fp32, the scale that of the turned keys); values are kept as they
+ * are.  With q and q_out (n_q_heads heads, of k's type; both or neither NULL) query rows row0 .. of the runs are turned as well,
+ * into the same rows of q_out; q_out may be q itself, and overlaps q, k and v in no other way; no row of it is written by two runs
+ * (INVALID_ARG).  rope->head_dim is the model's. */
+laser_status laser_kv_write_rotated(laser_kv* kv, int layer, const laser_rope* rope, int n_runs, const laser_kv_run* runs,
+                                    const laser_rows* k, const laser_rows* v, const laser_rows* q, const laser_rows* q_out,
+                                    void* stream);
 
 /* Query rows row0 .. row0+n-1, row i at position pos + i, over the keys kv_begin .. kv_end-1 of sequence
  * seq (kv_end = -1: the sequence's length). */

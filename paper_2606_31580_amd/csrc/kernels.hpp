@@ -340,8 +340,10 @@ hipError_t launch_kv_put(int kv_type, int io, int hd, KvPutArgs& a, bool rotate,
 hipError_t launch_kv_get4(int io, int hd, KvRowsArgs& a, int n_layers, hipStream_t s);
 // Rows of x rotated into out (laser_rotate).
 struct RotRun {
-  int n, pos, row0, step;  // row row0 + i at position pos + step i
-  unsigned first;          // (set by the launch)
+  int n;
+  int64_t pos;  // row row0 + i at position pos + step i
+  int row0, step;
+  unsigned first;  // (set by the launch)
 };
 struct RotRowsArgs {
   const void* x;

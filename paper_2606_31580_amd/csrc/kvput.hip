@@ -97,13 +97,13 @@ __device__ __forceinline__ void st_unit(void* base, int64_t e, const Unit& u, co
 __device__ __forceinline__ int cs_width(int pairs) { return 8 * ((pairs + 7) >> 3); }
 // (The turns are read from the argument segment itself: an index into an argument would have the compiler copy all of it
 // to scratch.)
-__device__ __forceinline__ void fill_cs(double2* cs, size_t turns_at, const RotArgs& r, int rows, int pos, int step) {
+__device__ __forceinline__ void fill_cs(double2* cs, size_t turns_at, const RotArgs& r, int rows, int64_t pos, int step) {
   using Turns = const __attribute__((address_space(4))) double;
   Turns* turns = (Turns*)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + turns_at);
   const int pairs = r.rot >> 1, width = cs_width(pairs);
   for (int i = threadIdx.x; i < rows * pairs; i += 256) {
     const int t = i / pairs, p = i - t * pairs;
-    const double turn = (double)((int64_t)pos + (int64_t)step * t) * turns[p];
+    const double turn = (double)(pos + (int64_t)step * t) * turns[p];
     double s, c;
     sincospi(2.0 * (turn - rint(turn)), &s, &c);
     cs[t * width + (p & 7) * (width >> 3) + (p >> 3)] = make_double2(r.amplitude * c, r.amplitude * s);
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(256) void k_rotate(RotRowsArgs a) {
   __shared__ double2 s_cs[16 * kRotPairs];
   const RotRun run = a.runs[run_of(a.runs, a.n_runs)];
   const int i0 = 16 * (int)(blockIdx.x - run.first), rows = min(16, run.n - i0);
-  fill_cs(s_cs, offsetof(RotRowsArgs, rot) + offsetof(RotArgs, turns), a.rot, rows, run.pos + run.step * i0, run.step);
+  fill_cs(s_cs, offsetof(RotRowsArgs, rot) + offsetof(RotArgs, turns), a.rot, rows, run.pos + (int64_t)run.step * i0, run.step);
   __syncthreads();
   const int all = rows * a.heads * units_of(a.rot, a.hd);
   for (int first = 128 * (blockIdx.y * 4 + (threadIdx.x >> 6)); first < all; first += 512 * gridDim.y)

@@ -2313,12 +2313,46 @@ laser_status flush_for_rows(laser_kv* kv, hipStream_t s) {
   return flush_pending(kv, const_cast<laser_model*>(kv->m), s);
 }
 
+// A rotation as the kernels take it: turns per position of each pair.
+laser_status rot_args(const laser_rope* rope, RotArgs& r) {
+  if (!rope || !rope->inv_freq) return laser_fail(LASER_ERR_INVALID_ARG, "rope: NULL");
+  if (rope->head_dim < 2 || rope->head_dim > 2 * kRotPairs) return laser_fail(LASER_ERR_UNSUPPORTED, "rope: head_dim %d outside [2, %d]", rope->head_dim, 2 * kRotPairs);
+  if (rope->rot_dim < 2 || rope->rot_dim % 2 || rope->rot_dim > rope->head_dim)
+    return laser_fail(LASER_ERR_INVALID_ARG, "rope: rot_dim %d is odd or outside [2, %d]", rope->rot_dim, rope->head_dim);
+  if (rope->layout != LASER_ROPE_HALF && rope->layout != LASER_ROPE_INTERLEAVED) return laser_fail(LASER_ERR_INVALID_ARG, "rope: unknown layout");
+  if (!std::isfinite(rope->amplitude)) return laser_fail(LASER_ERR_INVALID_ARG, "rope: amplitude is not finite");
+  r.rot = rope->rot_dim;
+  r.interleaved = rope->layout == LASER_ROPE_INTERLEAVED;
+  r.amplitude = rope->amplitude;
+  for (int i = 0; i < rope->rot_dim / 2; ++i) {
+    if (!(std::fabs(rope->inv_freq[i]) < 0x1p20)) return laser_fail(LASER_ERR_INVALID_ARG, "rope: inv_freq[%d] is not below 2^20", i);
+    r.turns[i] = rope->inv_freq[i] * 0.15915494309189533577;  // 1 / (2 pi)
+  }
+  return LASER_OK;
+}
+
+// What laser_kv_write_rotated adds to a write.
+struct RotateRows {
+  const laser_rope* rope;
+  const laser_rows* q;
+  const laser_rows* q_out;
+};
+
 laser_status kv_rows(laser_kv* kv, int layer, int n_runs, const laser_kv_run* runs, const laser_rows* k, const laser_rows* v,
-                     bool write, hipStream_t s) {
+                     bool write, hipStream_t s, const RotateRows* turn = nullptr) {
   laser_status st = check_rows_call(kv, layer);
   if (st != LASER_OK) return st;
   laser_model* m = const_cast<laser_model*>(kv->m);
   const laser_model_desc& d = m->desc;
+  KvPutArgs put{};
+  if (turn) {
+    st = rot_args(turn->rope, put.rot);
+    if (st != LASER_OK) return st;
+    if (turn->rope->head_dim != d.head_dim) return laser_fail(LASER_ERR_INVALID_ARG, "rope: head_dim %d, the model's is %d", turn->rope->head_dim, d.head_dim);
+    if (!turn->q != !turn->q_out) return laser_fail(LASER_ERR_INVALID_ARG, "q and q_out go together");
+  }
+  const laser_rows* q = turn ? turn->q : nullptr;
+  const laser_rows* q_out = turn ? turn->q_out : nullptr;
   if (n_runs < 0 || (n_runs > 0 && !runs)) return laser_fail(LASER_ERR_INVALID_ARG, "bad runs");
   if (n_runs > 0) {
     st = check_rows(k, "k", d.n_kv_heads, d.head_dim, !write);
@@ -2326,15 +2360,24 @@ laser_status kv_rows(laser_kv* kv, int layer, int n_runs, const laser_kv_run* ru
     if (st != LASER_OK) return st;
     if (k->dtype != v->dtype) return laser_fail(LASER_ERR_UNSUPPORTED, "k and v are of different types");
     if (!write && k->ptr == v->ptr) return laser_fail(LASER_ERR_INVALID_ARG, "k and v are read into the same place");
+    if (q) {
+      st = check_rows(q, "q", d.n_q_heads, d.head_dim, false);
+      if (st == LASER_OK) st = check_rows(q_out, "q_out", d.n_q_heads, d.head_dim, true);
+      if (st != LASER_OK) return st;
+      if (q->dtype != k->dtype || q_out->dtype != k->dtype) return laser_fail(LASER_ERR_UNSUPPORTED, "q and q_out are not of k's type");
+      if (q->ptr == q_out->ptr && (q->row_stride != q_out->row_stride || q->head_stride != q_out->head_stride))
+        return laser_fail(LASER_ERR_INVALID_ARG, "q_out is q's memory with other strides");
+    }
   }
-  std::vector<Interval> iv;
+  const int n_rows = n_runs == 0 ? 0 : std::min({k->rows, v->rows, q ? std::min(q->rows, q_out->rows) : k->rows});
+  std::vector<Interval> iv, qv;
   for (int i = 0; i < n_runs; ++i) {
     const laser_kv_run& r = runs[i];
     if (!kv->pool.live(r.seq)) return laser_fail(LASER_ERR_INVALID_ARG, "run %d: seq_id %d not present", i, r.seq);
     const int len = kv->pool.len(r.seq);
     if (r.n < 0 || r.pos < 0 || r.n > len - r.pos)
       return laser_fail(LASER_ERR_INVALID_ARG, "run %d: positions outside the sequence's %d", i, len);
-    if (r.row0 < 0 || (int64_t)r.row0 + r.n > std::min(k->rows, v->rows))
+    if (r.row0 < 0 || (int64_t)r.row0 + r.n > n_rows)
       return laser_fail(LASER_ERR_INVALID_ARG, "run %d: rows outside the arrays", i);
     if (r.n == 0) continue;
     if (write) {
@@ -2343,11 +2386,13 @@ laser_status kv_rows(laser_kv* kv, int layer, int n_runs, const laser_kv_run* ru
         if (kv->pool.refs(t[p]) > 1)
           return laser_fail(LASER_ERR_INVALID_ARG, "run %d: position %d is on a page that a fork shares", i, std::max(r.pos, p * kPage));
       iv.push_back(Interval{r.seq, r.pos, (int64_t)r.pos + r.n});
+      if (q) qv.push_back(Interval{0, r.row0, (int64_t)r.row0 + r.n});
     } else {
       iv.push_back(Interval{0, r.row0, (int64_t)r.row0 + r.n});
     }
   }
   if (overlaps(iv)) return laser_fail(LASER_ERR_INVALID_ARG, write ? "two runs write the same position" : "two runs read into the same row");
+  if (overlaps(qv)) return laser_fail(LASER_ERR_INVALID_ARG, "two runs write the same row of q_out");
   if (!m->finalized) return laser_fail(LASER_ERR_STATE, "model not finalized");
   DeviceScope dev(m->device);
   HIP_TRY(dev.err);
@@ -2361,6 +2406,15 @@ laser_status kv_rows(laser_kv* kv, int layer, int n_runs, const laser_kv_run* ru
   a.k_head = k->head_stride;
   a.v_row = v->row_stride;
   a.v_head = v->head_stride;
+  if (q) {
+    put.q = q->ptr;
+    put.q_out = q_out->ptr;
+    put.hq = d.n_q_heads;
+    put.q_row = q->row_stride;
+    put.q_head = q->head_stride;
+    put.qo_row = q_out->row_stride;
+    put.qo_head = q_out->head_stride;
+  }
   TimingScope scope(m);
   for (int i = 0; i < n_runs;) {
     a.n_runs = 0;
@@ -2368,7 +2422,10 @@ laser_status kv_rows(laser_kv* kv, int layer, int n_runs, const laser_kv_run* ru
       if (runs[i].n > 0) a.runs[a.n_runs++] = KvRun{runs[i].seq, runs[i].pos, runs[i].n, runs[i].row0, 0};
     if (a.n_runs == 0) break;
     HIP_TRY(timed(m, LASER_K_OTHER, s, [&] {
-      return launch_rows_of(m, k->dtype == LASER_DTYPE_BF16, a, 1, write, s);
+      const int io = k->dtype == LASER_DTYPE_BF16;
+      if (!turn) return launch_rows_of(m, io, a, 1, write, s);
+      put.kv = a;
+      return launch_kv_put(kv_type_of(m), io, d.head_dim, put, true, 1, m->cus, s);
     }));
   }
   return LASER_OK;
@@ -2444,6 +2501,126 @@ extern "C" laser_status laser_kv_write(laser_kv* kv, int layer, int n_runs, cons
                                        const laser_rows* v, void* stream) {
   try {
     return kv_rows(kv, layer, n_runs, runs, k, v, true, (hipStream_t)stream);
+  } catch (const std::bad_alloc&) {
+    return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
+  }
+}
+
+extern "C" laser_status laser_kv_write_rotated(laser_kv* kv, int layer, const laser_rope* rope, int n_runs, const laser_kv_run* runs,
+                                               const laser_rows* k, const laser_rows* v, const laser_rows* q,
+                                               const laser_rows* q_out, void* stream) {
+  try {
+    const RotateRows turn{rope, q, q_out};
+    return kv_rows(kv, layer, n_runs, runs, k, v, true, (hipStream_t)stream, &turn);
+  } catch (const std::bad_alloc&) {
+    return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
+  }
+}
+
+extern "C" laser_status laser_rope_frequencies(int rot_dim, double theta, const laser_rope_scaling* scaling, double* inv_freq,
+                                               double* amplitude) {
+  if (!inv_freq || !amplitude) return laser_fail(LASER_ERR_INVALID_ARG, "NULL argument");
+  if (rot_dim < 2 || rot_dim % 2) return laser_fail(LASER_ERR_INVALID_ARG, "rot_dim %d", rot_dim);
+  if (!(theta > 1.0) || !std::isfinite(theta)) return laser_fail(LASER_ERR_INVALID_ARG, "theta is not above 1");
+  const laser_rope_scaling none{LASER_ROPE_PLAIN, 1.0, 1.0, 1.0, 2.0};
+  const laser_rope_scaling& s = scaling ? *scaling : none;
+  if (s.kind < LASER_ROPE_PLAIN || s.kind > LASER_ROPE_RAMP) return laser_fail(LASER_ERR_INVALID_ARG, "unknown kind of scaling");
+  if (s.kind != LASER_ROPE_PLAIN && (!(s.factor > 0.0) || !std::isfinite(s.factor) || (s.kind == LASER_ROPE_RAMP && s.factor < 1.0)))
+    return laser_fail(LASER_ERR_INVALID_ARG, "bad factor");
+  if (s.kind == LASER_ROPE_BANDS || s.kind == LASER_ROPE_RAMP)
+    if (!(s.old_positions > 0.0) || !(s.low > 0.0) || !(s.high > s.low) || !std::isfinite(s.old_positions) || !std::isfinite(s.high))
+      return laser_fail(LASER_ERR_INVALID_ARG, "bad old_positions, low or high");
+  const double two_pi = 6.283185307179586477, r = rot_dim;
+  double base = theta, first = 0.0, last = 0.0;
+  if (s.kind == LASER_ROPE_BASE && rot_dim > 2) base = theta * std::pow(s.factor, r / (r - 2.0));
+  if (s.kind == LASER_ROPE_RAMP) {
+    auto pair = [&](double n) { return r * std::log(s.old_positions / (two_pi * n)) / (2.0 * std::log(theta)); };
+    first = std::min(std::max(std::floor(pair(s.high)), 0.0), r - 1.0);
+    last = std::min(std::max(std::ceil(pair(s.low)), 0.0), r - 1.0);
+  }
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / r);
+    if (s.kind == LASER_ROPE_LINEAR) f /= s.factor;
+    if (s.kind == LASER_ROPE_BANDS) {
+      const double w = std::min(std::max((s.old_positions * f / two_pi - s.low) / (s.high - s.low), 0.0), 1.0);
+      f *= w + (1.0 - w) / s.factor;
+    }
+    if (s.kind == LASER_ROPE_RAMP) {
+      const double w = std::min(std::max((i - first) / std::max(last - first, 1e-3), 0.0), 1.0);
+      f *= 1.0 - w + w / s.factor;
+    }
+    inv_freq[i] = f;
+  }
+  *amplitude = s.kind == LASER_ROPE_RAMP ? 1.0 + 0.1 * std::log(s.factor) : 1.0;
+  return LASER_OK;
+}
+
+// Compute units of the current device.
+static int current_cus() {
+  static std::atomic<int> known[kMaxDevices];
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return 256;
+  cus = known[dev].load(std::memory_order_relaxed);
+  if (cus == 0) {
+    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1) cus = 256;
+    known[dev].store(cus, std::memory_order_relaxed);
+  }
+  return cus;
+}
+
+static laser_status rotate_rows(const laser_rope* rope, int n_runs, const laser_rotate_run* runs, int heads, const laser_rows* x,
+                                const laser_rows* out, hipStream_t s) {
+  RotRowsArgs a{};
+  laser_status st = rot_args(rope, a.rot);
+  if (st != LASER_OK) return st;
+  if (heads < 1 || heads > (1 << 16)) return laser_fail(LASER_ERR_INVALID_ARG, "bad number of heads");
+  if (n_runs < 0 || (n_runs > 0 && !runs)) return laser_fail(LASER_ERR_INVALID_ARG, "bad runs");
+  st = check_rows(x, "x", heads, rope->head_dim, false);
+  if (st == LASER_OK) st = check_rows(out, "out", heads, rope->head_dim, true);
+  if (st != LASER_OK) return st;
+  if (x->dtype != out->dtype) return laser_fail(LASER_ERR_UNSUPPORTED, "x and out are of different types");
+  if (x->ptr == out->ptr && (x->row_stride != out->row_stride || x->head_stride != out->head_stride))
+    return laser_fail(LASER_ERR_INVALID_ARG, "out is x's memory with other strides");
+  std::vector<Interval> iv;
+  for (int i = 0; i < n_runs; ++i) {
+    if (runs[i].n < 0 || runs[i].row0 < 0 || (int64_t)runs[i].row0 + runs[i].n > std::min(x->rows, out->rows))
+      return laser_fail(LASER_ERR_INVALID_ARG, "run %d: rows outside the arrays", i);
+    if (runs[i].n > 0) iv.push_back(Interval{0, runs[i].row0, (int64_t)runs[i].row0 + runs[i].n});
+  }
+  if (overlaps(iv)) return laser_fail(LASER_ERR_INVALID_ARG, "two runs hold the same row");
+  if (iv.empty()) return LASER_OK;
+  a.x = x->ptr;
+  a.out = out->ptr;
+  a.heads = heads;
+  a.hd = rope->head_dim;
+  a.x_row = x->row_stride;
+  a.x_head = x->head_stride;
+  a.out_row = out->row_stride;
+  a.out_head = out->head_stride;
+  const int io = x->dtype == LASER_DTYPE_BF16, cus = current_cus();
+  constexpr int kPiece = 1 << 21;  // rows of a run in one launch, so that 64 of them stay below a grid's 2^32 threads
+  for (int i = 0, at = 0; i < n_runs;) {
+    a.n_runs = 0;
+    while (i < n_runs && a.n_runs < kKvRuns) {
+      const laser_rotate_run& r = runs[i];
+      const int n = std::min(r.n - at, kPiece);
+      // (positions of later pieces pass 32 bits where pos + step i does: each piece starts from its own)
+      if (n > 0) a.runs[a.n_runs++] = RotRun{n, r.pos + (int64_t)r.step * at, r.row0 + at, r.step, 0};
+      at += n;
+      if (at >= r.n) {
+        ++i;
+        at = 0;
+      }
+    }
+    if (a.n_runs > 0) HIP_TRY(launch_rotate(io, a, cus, s));
+  }
+  return LASER_OK;
+}
+
+extern "C" laser_status laser_rotate(const laser_rope* rope, int n_runs, const laser_rotate_run* runs, int heads,
+                                     const laser_rows* x, const laser_rows* out, void* stream) {
+  try {
+    return rotate_rows(rope, n_runs, runs, heads, x, out, (hipStream_t)stream);
   } catch (const std::bad_alloc&) {
     return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
   }

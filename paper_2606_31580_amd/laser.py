@@ -108,6 +108,9 @@ _SIGS = {
     "laser_kv_truncate": (_I, [_P, _I, _I]),
     "laser_kv_write": (_I, [_P, _I, _I, _P, _P, _P, _P]),
     "laser_kv_read": (_I, [_P, _I, _I, _P, _P, _P, _P]),
+    "laser_kv_write_rotated": (_I, [_P, _I, _P, _I, _P, _P, _P, _P, _P, _P]),
+    "laser_rope_frequencies": (_I, [_I, C.c_double, _P, _P, _P]),
+    "laser_rotate": (_I, [_P, _I, _P, _I, _P, _P, _P]),
     "laser_attend_workspace": (_I, [_P, _I, _P, _I, _I, _I, C.POINTER(C.c_size_t)]),
     "laser_attend": (_I, [_P, _I, _I, _P, C.c_float, _I, _I, _P, _P, _P, _P, C.c_size_t, _P]),
     "laser_prefill": (_I, [_P, _P, _I, _P, _I, _P, _P]),
@@ -505,17 +508,21 @@ _row_dtypes: Dict["object", int] = {}
 
 def _rows(t, what: str, kv: KVCache, heads: int) -> laser_rows:
     """A [rows, heads, head_dim] tensor (fp32 or bf16, contiguous in its last dimension) as the library takes it."""
+    return _rows_on(t, what, kv.k_pool.device, heads, kv.model.shape.head_dim)
+
+
+def _rows_on(t, what: str, device, heads: int, hd: int) -> laser_rows:
     if not _row_dtypes:
         import torch
         _row_dtypes.update({torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16})
     dtype = _row_dtypes.get(t.dtype)
     if dtype is None:
         raise TypeError(f"{what}: rows are float32 or bfloat16, not {t.dtype}")
-    shape, hd = t.shape, kv.model.shape.head_dim
+    shape = t.shape
     if len(shape) != 3 or shape[1] != heads or shape[2] != hd:
         raise ValueError(f"{what}: expected [rows, {heads}, {hd}], got {tuple(shape)}")
-    if t.device != kv.k_pool.device:
-        raise ValueError(f"{what}: on {t.device}, the cache on {kv.k_pool.device}")
+    if t.device != device:
+        raise ValueError(f"{what}: on {t.device}, the others on {device}")
     row, head, one = t.stride()
     if one != 1:
         raise ValueError(f"{what}: the last dimension is not contiguous")
@@ -549,6 +556,92 @@ def laser_kv_write(kv: KVCache, layer: int, runs: Sequence[laser_kv_run], k=None
 def laser_kv_read(kv: KVCache, layer: int, runs: Sequence[laser_kv_run], k, v, stream=None) -> None:
     """The runs' positions as the values the cache stands for, into rows of k and v."""
     _kv_rows("laser_kv_read", kv, layer, runs, k, v, stream)
+
+
+# Rotary positions.
+
+class laser_rope(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_double),
+                ("inv_freq", C.c_void_p)]
+
+
+class laser_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32)] + [(n, C.c_double) for n in ("factor", "old_positions", "low", "high")]
+
+
+class laser_rotate_run(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n", "pos", "row0", "step")]
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+def laser_rope_frequencies(rot_dim: int, theta: float, scaling: Optional[laser_rope_scaling] = None):
+    """(radians per position of each of the rot_dim / 2 pairs, amplitude)."""
+    f, a = (C.c_double * max(rot_dim // 2, 1))(), C.c_double()
+    _call("laser_rope_frequencies", rot_dim, theta, None if scaling is None else C.byref(scaling), f, C.byref(a))
+    return list(f), a.value
+
+
+def rope(head_dim: int, theta: float = 1.0e4, rot_dim: Optional[int] = None, layout: str = "half", scaling: str = "plain",
+         factor: float = 1.0, old_positions: float = 1.0, low: float = 1.0, high: float = 2.0,
+         inv_freq: Optional[Sequence[float]] = None, amplitude: Optional[float] = None) -> laser_rope:
+    """A laser_rope for heads of head_dim, of which the first rot_dim (all of them unless given) are rotated, in pairs
+    (i, i + rot_dim / 2) ("half") or (2i, 2i + 1) ("interleaved"); frequencies of theta and a scaling ("linear", "base", "bands",
+    "ramp": see laser_rope_frequencies), or inv_freq, radians per position of each pair."""
+    rot_dim = head_dim if rot_dim is None else rot_dim
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        raise ValueError(f"layout {layout!r}: one of {list(ROPE_LAYOUTS)}; scaling {scaling!r}: one of {list(ROPE_SCALINGS)}")
+    if inv_freq is None:
+        inv_freq, own = laser_rope_frequencies(rot_dim, theta, laser_rope_scaling(ROPE_SCALINGS[scaling], factor, old_positions, low, high))
+        amplitude = own if amplitude is None else amplitude
+    if len(inv_freq) != rot_dim // 2:
+        raise ValueError(f"inv_freq: {len(inv_freq)} values for {rot_dim // 2} pairs")
+    held = (C.c_double * len(inv_freq))(*inv_freq)
+    r = laser_rope(head_dim, rot_dim, ROPE_LAYOUTS[layout], 1.0 if amplitude is None else amplitude, C.addressof(held))
+    r.held = held  # the structure points into it
+    return r
+
+
+def rotate_run(n: int, pos: int, row0: int = 0, step: int = 1) -> laser_rotate_run:
+    """Row row0 + i is at position pos + step i, i < n."""
+    return laser_rotate_run(n, pos, row0, step)
+
+
+def laser_rotate(rope: laser_rope, runs: Sequence[laser_rotate_run], x, out, stream=None) -> None:
+    """The runs' rows of x ([rows, heads, head_dim]) rotated into out (of x's type; x itself, to rotate in place)."""
+    import torch
+
+    if x.dim() != 3:
+        raise ValueError(f"x: expected [rows, heads, {rope.head_dim}], got {tuple(x.shape)}")
+    heads, dev = x.shape[1], x.device
+    rx, ro = _rows_on(x, "x", dev, heads, rope.head_dim), _rows_on(out, "out", dev, heads, rope.head_dim)
+    if dev.type != "cuda":
+        raise ValueError(f"x: on {dev}")
+    args = (C.byref(rope), len(runs), _joined(laser_rotate_run, runs), heads, C.byref(rx), C.byref(ro),
+            torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream)
+    if torch._C._cuda_getDevice() == dev.index:
+        _call("laser_rotate", *args)
+    else:
+        with torch.cuda.device(dev):
+            _call("laser_rotate", *args)
+
+
+def laser_kv_write_rotated(kv: KVCache, layer: int, rope: laser_rope, runs: Sequence[laser_kv_run], k=None, v=None, q=None, q_out=None,
+                           stream=None) -> None:
+    """laser_kv_write with the key rows rotated to the runs' positions on the way; with q and q_out ([rows, query heads,
+    head_dim], of k's type; q_out may be q) the same rows of q are rotated into q_out."""
+    n, shape = len(runs), kv.model.shape
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    arr = rk = rv = rq = ro = None
+    if n:
+        arr = _joined(laser_kv_run, runs)
+        rk, rv = C.byref(_rows(k, "k", kv, shape.n_kv_heads)), C.byref(_rows(v, "v", kv, shape.n_kv_heads))
+        if q is not None:
+            rq, ro = C.byref(_rows(q, "q", kv, shape.n_q_heads)), C.byref(_rows(q_out, "q_out", kv, shape.n_q_heads))
+    _call("laser_kv_write_rotated", kv.h, layer, C.byref(rope), n, arr, rk, rv, rq, ro, _stream_of(kv, stream))
 
 
 def laser_attend_workspace(kv: KVCache, spans: Sequence[laser_attend_span], dtype: int = DTYPE_BF16, causal: bool = True,
