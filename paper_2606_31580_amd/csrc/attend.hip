@@ -492,7 +492,7 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
 #pragma unroll
         for (int d = 0; d < (F4 ? NS : ND); ++d) {
           if constexpr (F4) {
-            odd |= mx_has_nan(b.vs[x][d]);
+            odd |= mx_odd(b.vs[x][d]);
           } else if constexpr (ES == 1) {
             uint32_t lo, hi;
             fp8x4_to_bf16x4(b.v[x][d], lo, hi);
@@ -825,7 +825,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
       bool odd = I8 && raw_s != 0.f && !(raw_s >= 0x1p-36f && raw_s <= 0x1p36f);
       if constexpr (F4)
 #pragma unroll
-        for (int i = 0; i < NS; ++i) odd |= mx_has_nan(raw_4[i]);
+        for (int i = 0; i < NS; ++i) odd |= mx_odd(raw_4[i]);
       if constexpr (!I8 && !F4)
 #pragma unroll
         for (int i = 0; i < NL; ++i)

@@ -118,8 +118,9 @@ __device__ __forceinline__ void fp4v_to_bf16(uint32_t w, const uint32_t* scales,
   lo = u32x2{__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(d, c, 0x05040100u)};
   hi = u32x2{__builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u)};
 }
-// Some byte of a word of scales is 255.
-__device__ __forceinline__ bool mx_has_nan(uint32_t w) { return ((((w & 0x7f7f7f7fu) + 0x01010101u) & w) & 0x80808080u) != 0; }
+// Some byte of a word of scales is above 252: codes times it may be infinite or NaN.  (Of what was written only 255 is; a
+// position that was not may hold anything.)
+__device__ __forceinline__ bool mx_odd(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x03030303u) & w & 0x80808080u) != 0; }
 
 __device__ __forceinline__ float bf2f(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
 

@@ -252,13 +252,18 @@ def test_nan_in_unseen_places(mode, io, hd, n):
         assert np.all(np.abs(f64(o) - ref)[fine] <= tol[fine])
 
 
-def test_poisoned_neighbours():
-    """Slots past the length, pages of other sequences and other layers hold NaN bytes (the cache is created so)."""
+@pytest.mark.parametrize("mode", [1, 2], ids=["rows", "tiles"])
+@pytest.mark.parametrize("byte", [0xFF, 0xFE, 0xFD, 0xFC, 0x77, 0x00])
+def test_poisoned_neighbours(byte, mode):
+    """Slots past the length, pages of other sequences and other layers hold scales that are NaN, that make codes infinite,
+    or are the largest that do not."""
     for hd in (64, 128):
-        kv = cache(4, 2, hd, pages=40, seqs=3, per_seq=20)
-        held = fill(kv, [17, 33, 50], 2, hd, 14)
-        q = queries(np.random.default_rng(15), 12, 4, hd, "bf16")
-        check(kv, "mxfp4", "bf16", held, [L.attend_span(0, 1, 16, 0), L.attend_span(1, 5, 28, 1), L.attend_span(2, 6, 44, 6)], q)
+        kv = cache(4, 2, hd, pages=40, seqs=4, per_seq=20, mode=mode)
+        kv.k_pool.fill_(byte)
+        kv.v_pool.fill_(byte)
+        held = fill(kv, [17, 33, 50, 101], 2, hd, 14)
+        q = queries(np.random.default_rng(15), 62, 4, hd, "bf16")
+        check(kv, "mxfp4", "bf16", held, [L.attend_span(0, 1, 16, 0), L.attend_span(1, 5, 28, 1), L.attend_span(2, 6, 44, 6), L.attend_span(3, 50, 51, 12)], q)
 
 
 def test_captured():
