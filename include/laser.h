@@ -400,7 +400,7 @@ laser_status laser_kv_read(const laser_kv* kv, int layer, int n_runs, const lase
  *   y1 = amplitude (x1 cos - x2 sin),  y2 = amplitude (x2 cos + x1 sin),
  * x1 and x2 the elements i and i + rot_dim / 2 (LASER_ROPE_HALF, as the model's own forward has them) or 2 i and 2 i + 1
  * (LASER_ROPE_INTERLEAVED) of the head's vector; elements from rot_dim on are left as they are.  The angle and the sums are in
- * double, and the result is rounded once to the type it is kept in (bf16 rows: over fp32).  rot_dim is even, 2 to head_dim;
+ * double, and the result is rounded once to the type it is kept in (bf16 rows: over fp32; beyond fp32's range it is infinite).  rot_dim is even, 2 to head_dim;
  * inv_freq holds rot_dim / 2 finite host values below 2^20 in magnitude, read during the call. */
 enum { LASER_ROPE_HALF = 0, LASER_ROPE_INTERLEAVED = 1 };
 typedef struct {
@@ -435,7 +435,7 @@ typedef struct {
   int32_t n, pos, row0, step;
 } laser_rotate_run;
 
-/* Rotates the runs' rows of x (`heads` heads of rope->head_dim, 2 to 256, elements) into out, of x's type; out may be x itself (the
+/* Rotates the runs' rows of x (`heads` heads, 8192 at most, of rope->head_dim, 2 to 256, elements) into out, of x's type; out may be x itself (the
  * same pointer and strides), and overlaps it in no other way.  A row is in one run at most (INVALID_ARG); other rows of out keep
  * what they hold.  On the current device; may be captured into a graph. */
 laser_status laser_rotate(const laser_rope* rope, int n_runs, const laser_rotate_run* runs, int heads, const laser_rows* x,

@@ -405,8 +405,22 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
       }
     return acc;
   };
+  [[maybe_unused]] bool left = false;  // (4-bit pages) pairs put off
   auto compute = [&](const Pair& b, int pg, auto careful) {
     const bool whole = 16 * pg >= flo && 16 * pg + 32 <= fhi && pg + 1 < p1;  // (uniform)
+    if constexpr (F4) {  // a scale of V that makes codes infinite or NaN, next to positions that some column does not see?
+      bool odd = false;
+      if (!whole)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int g = 0; g < NS; ++g) odd |= mx_odd(b.vs[x][g]);
+      const bool any = __ballot(odd) != 0;
+      if (any != decltype(careful)::value) {  // such pairs come after all others
+        left |= any;
+        return;
+      }
+    }
     f32x4 s[NT][2];
 #pragma unroll
     for (int u = 0; u < NT; ++u) s[u][0] = s[u][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -436,7 +450,7 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
           if constexpr (I8) f *= b.ks[x][i];
           sv[4 * x + i] = s[u][x][i] * f;
         }
-      if (!whole) {
+      if (F4 ? __builtin_expect(!whole, 0) : !whole) {
         seen[u] = 0;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
@@ -485,14 +499,13 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
 #pragma unroll
       for (int k = 0; k < WP; ++k) p[u][k] = __builtin_bit_cast(bf16x8, pw[k]);
     }
-    bool odd = false;
-    if (!I8 && (decltype(careful)::value || !whole)) {  // an infinite or NaN V anywhere in the pair?
+    bool odd = F4 && decltype(careful)::value;
+    if (!I8 && !F4 && (decltype(careful)::value || !whole)) {  // an infinite or NaN V anywhere in the pair?
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int d = 0; d < (F4 ? NS : ND); ++d) {
+        for (int d = 0; d < ND; ++d) {
           if constexpr (F4) {
-            odd |= mx_odd(b.vs[x][d]);
           } else if constexpr (ES == 1) {
             uint32_t lo, hi;
             fp8x4_to_bf16x4(b.v[x][d], lo, hi);
@@ -505,7 +518,7 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
           }
         }
     }
-    if (!__ballot(odd)) {
+    if (F4 ? !odd : !__ballot(odd)) {
       if constexpr (F4) {
         static_for<NS>([&](auto gc) {
           constexpr int G = decltype(gc)::value;
@@ -603,6 +616,15 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
       if (pg + 2 >= p1) break;
       load(buf[0], pg + 4);
       compute(buf[1], pg + 2, std::false_type{});
+    }
+    if constexpr (F4) {
+      if (__builtin_expect(left, 0))
+#pragma unroll 1
+        for (int pg = p0; pg < p1; pg += 2) {
+          look(pg);
+          load(buf[0], pg);
+          compute(buf[0], pg, std::true_type{});
+        }
     }
     if constexpr (INF) {  // a sum that is infinite or NaN stays so: the run once more, parts and infinities apart
       float z = 0.f;

@@ -320,6 +320,12 @@ hipError_t launch_kv_rows(int kv_type, int io, int hd, KvRowsArgs& a, int n_laye
 
 // Rotation of pairs of the first rot dims of a head: element i with i + rot / 2, or 2 i with 2 i + 1.
 constexpr int kRotPairs = 128;  // of a head, at most
+constexpr int kRotHeads = 8192;
+// n / d of unsigned n with n d < 2^32, by a multiplication: m = ceil(2^32 / d), 0 for d = 1.
+struct FastDiv {
+  uint32_t m;
+};
+inline FastDiv fast_div(uint32_t d) { return FastDiv{d <= 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d)}; }
 struct RotArgs {
   int rot, interleaved;
   double amplitude;
@@ -332,6 +338,7 @@ struct KvPutArgs {
   const void* q;  // or null
   void* q_out;
   int hq;
+  FastDiv by_hq;  // (set by the launch)
   int64_t q_row, q_head, qo_row, qo_head;
   RotArgs rot;
 };
@@ -349,6 +356,7 @@ struct RotRowsArgs {
   const void* x;
   void* out;
   int heads, hd;
+  FastDiv by_heads, by_units;  // (set by the launch)
   int64_t x_row, x_head, out_row, out_head;
   RotArgs rot;
   int n_runs;

@@ -110,7 +110,12 @@ __device__ __forceinline__ uint32_t pk_fp8x4(const float* x) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false), true);
 }
 
-__device__ __forceinline__ uint16_t f2bf_any(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
+// Two values as bf16 (to nearest even), the first in the low half.
+__device__ __forceinline__ uint32_t f2bf2(float a, float b) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
+}
 
 // 8 elements of one position in the cache's type.
 template <class KT>
@@ -126,7 +131,7 @@ __device__ __forceinline__ Piece<KT> pack(const float* x, const RowScale* rs) {
     for (int e = 0; e < 8; ++e) p.w[e] = __float_as_uint(x[e]);
   } else if constexpr (std::is_same_v<KT, bf16_t>) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) p.w[e] = (uint32_t)f2bf_any(x[2 * e]) | ((uint32_t)f2bf_any(x[2 * e + 1]) << 16);
+    for (int e = 0; e < 4; ++e) p.w[e] = f2bf2(x[2 * e], x[2 * e + 1]);
   } else {
     if constexpr (std::is_same_v<KT, fp8_t>) {
       p.w[0] = pk_fp8x4(x);

@@ -18,15 +18,15 @@ namespace laser {
 
 namespace {
 
-// d rounded to fp32 such that rounding the result once more, to at most 22 bits, is rounding d: towards zero, with the last
-// bit set if that was not exact.
+// d to fp32 such that rounding the result once more, to at most 19 bits, is rounding d: its upper 21 significant bits, the
+// last one set if anything lies below.
 __device__ __forceinline__ float to_odd(double d) {
-  const float f = (float)d;
-  const double back = f;
-  uint32_t u = __float_as_uint(f);
-  if (back != d && !(u & 1)) u += fabs(back) < fabs(d) ? 1u : -1u;
-  return __uint_as_float(u);
+  return (float)__hiloint2double(__double2hiint(d) | (int)min((uint32_t)__double2loint(d), 1u), 0);
 }
+__device__ __forceinline__ int div_by(int n, FastDiv d) { return d.m == 0 ? n : (int)__umulhi((uint32_t)n, d.m); }
+// How the pairs of a launch's rows lie, and how its rows are read: by 16-byte pieces, whole units only; or element by
+// element, whatever the layout.
+enum { kAny = 0, kHalf = 1, kInterleaved = 2 };
 
 // Elements e .. e+n-1 of a row, one by one.
 template <class IT>
@@ -50,8 +50,14 @@ struct Unit {
 };
 __device__ __forceinline__ int turning_units(const RotArgs& r) { return (r.rot + 15) >> 4; }
 __device__ __forceinline__ int units_of(const RotArgs& r, int hd) { return turning_units(r) + ((hd - r.rot + 15) >> 4); }
+template <int MODE>
 __device__ __forceinline__ Unit unit_of(const RotArgs& r, int hd, int j) {
   const int nt = turning_units(r);
+  if constexpr (MODE != kAny) {
+    const bool turns = j < nt;
+    const int a0 = MODE == kHalf && turns ? 8 * j : 16 * j;
+    return Unit{a0, 8, MODE == kHalf && turns ? (r.rot >> 1) + a0 : a0 + 8, 8, turns};
+  }
   Unit u;
   u.turns = j < nt;
   if (!u.turns) {
@@ -71,19 +77,45 @@ __device__ __forceinline__ Unit unit_of(const RotArgs& r, int hd, int j) {
   }
   return u;
 }
-template <class IT, bool VEC>
+template <class IT>
 __device__ __forceinline__ void ld_unit(const void* base, int64_t e, const Unit& u, float* x) {
-  if constexpr (VEC) {
-    ld_row8<IT, true>(base, e + u.a0, x);
-    ld_row8<IT, true>(base, e + u.a1, x + 8);
+  ld_part<IT>(base, e + u.a0, u.n0, x);
+  ld_part<IT>(base, e + u.a1, u.n1, x + 8);
+}
+// A unit as it was loaded (16-byte pieces), to be converted when it is there.
+template <class IT>
+struct RawUnit {
+  u32x4 w[sizeof(IT)];
+};
+template <class IT>
+__device__ __forceinline__ RawUnit<IT> ld_raw(const void* base, int64_t e, const Unit& u) {
+  RawUnit<IT> r;
+  const char* a = (const char*)base + (e + u.a0) * (int64_t)sizeof(IT);
+  const char* b = (const char*)base + (e + u.a1) * (int64_t)sizeof(IT);
+  if constexpr (sizeof(IT) == 2) {
+    r.w[0] = ld_nt16(a);
+    r.w[1] = ld_nt16(b);
   } else {
-    ld_part<IT>(base, e + u.a0, u.n0, x);
-    ld_part<IT>(base, e + u.a1, u.n1, x + 8);
+    r.w[0] = ld_global<u32x4>(a);
+    r.w[1] = ld_global<u32x4>(a + 16);
+    r.w[2] = ld_global<u32x4>(b);
+    r.w[3] = ld_global<u32x4>(b + 16);
+  }
+  return r;
+}
+template <class IT>
+__device__ __forceinline__ void of_raw(const RawUnit<IT>& r, float* x) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    Piece<IT> p;
+#pragma unroll
+    for (int i = 0; i < Piece<IT>::W; ++i) p.w[i] = r.w[(h * Piece<IT>::W + i) / 4][i % 4];
+    unpack<IT>(p, 0.f, x + 8 * h);
   }
 }
-template <class IT, bool VEC>
+template <class IT, int MODE>
 __device__ __forceinline__ void st_unit(void* base, int64_t e, const Unit& u, const float* x) {
-  if constexpr (VEC) {
+  if constexpr (MODE != kAny) {
     st_row8<IT, true>(base, e + u.a0, x);
     st_row8<IT, true>(base, e + u.a1, x + 8);
   } else {
@@ -109,22 +141,23 @@ __device__ __forceinline__ void fill_cs(double2* cs, size_t turns_at, const RotA
     cs[t * width + (p & 7) * (width >> 3) + (p >> 3)] = make_double2(r.amplitude * c, r.amplitude * s);
   }
 }
-template <bool ODD>
+template <bool ODD, int MODE>
 __device__ __forceinline__ void turn_unit(const double2* cs, const RotArgs& r, int t, int j, float* x) {
+  const bool side = MODE == kAny ? r.interleaved != 0 : MODE == kInterleaved;
   const int width = cs_width(r.rot >> 1), w8 = width >> 3;
   const double2* row = cs + t * width + j;
   float y[16];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const double2 k = row[i * w8];
-    const double a = r.interleaved ? x[2 * i] : x[i], b = r.interleaved ? x[2 * i + 1] : x[8 + i];
+    const double a = side ? x[2 * i] : x[i], b = side ? x[2 * i + 1] : x[8 + i];
     const double u = fma(a, k.x, -(b * k.y)), v = fma(b, k.x, a * k.y);
     y[i] = ODD ? to_odd(u) : (float)u;
     y[8 + i] = ODD ? to_odd(v) : (float)v;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (r.interleaved) {
+    if (side) {
       x[2 * i] = y[i];
       x[2 * i + 1] = y[8 + i];
     } else {
@@ -134,22 +167,40 @@ __device__ __forceinline__ void turn_unit(const double2* cs, const RotArgs& r, i
   }
 }
 
-// A wave's share of dense rows: units first .. first+127 of the rows x heads x units.
-template <class IT, bool VEC>
-__device__ __forceinline__ void turn_rows(const double2* cs, const RotArgs& r, const void* x, void* out, int heads, int hd, int64_t x_row,
-                                          int64_t x_head, int64_t out_row, int64_t out_head, int row0, int rows, int first) {
-  const int nu = units_of(r, hd), all = rows * heads * nu, l = threadIdx.x & 63;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int id = first + 64 * k + l;
-    if (id >= all) break;
-    const int rh = id / nu, j = id - rh * nu, t = rh / heads, h = rh - t * heads;
-    const Unit u = unit_of(r, hd, j);
-    float v[16];
-    ld_unit<IT, VEC>(x, (int64_t)(row0 + t) * x_row + h * x_head, u, v);
-    if (u.turns) turn_unit<false>(cs, r, t, j, v);
-    st_unit<IT, VEC>(out, (int64_t)(row0 + t) * out_row + h * out_head, u, v);
-  }
+// Dense rows: rows row0 .. of x, as rows x heads x units.
+struct Dense {
+  const void* x;
+  void* out;
+  int heads, hd, units, all, row0;  // units of a head, of all rows
+  FastDiv by_heads, by_units;
+  int64_t x_row, x_head, out_row, out_head;
+};
+struct DensePlace {
+  Unit u;
+  int t, j, h;
+};
+template <int MODE>
+__device__ __forceinline__ DensePlace dense_place(const RotArgs& r, const Dense& d, int id) {
+  const int rh = div_by(id, d.by_units), j = id - rh * d.units, t = div_by(rh, d.by_heads);
+  return DensePlace{unit_of<MODE>(r, d.hd, j), t, j, rh - t * d.heads};
+}
+template <class IT, int MODE>
+__device__ __forceinline__ RawUnit<IT> ld_dense(const RotArgs& r, const Dense& d, int id) {
+  const DensePlace p = dense_place<MODE>(r, d, min(id, d.all - 1));
+  return ld_raw<IT>(d.x, (int64_t)(d.row0 + p.t) * d.x_row + p.h * d.x_head, p.u);
+}
+// Unit id turned and stored (raw: as it was loaded).
+template <class IT, int MODE>
+__device__ __forceinline__ void put_dense(const double2* cs, const RotArgs& r, const Dense& d, int id, const RawUnit<IT>* raw) {
+  if (id >= d.all) return;
+  const DensePlace p = dense_place<MODE>(r, d, id);
+  float v[16];
+  if constexpr (MODE != kAny)
+    of_raw<IT>(*raw, v);
+  else
+    ld_unit<IT>(d.x, (int64_t)(d.row0 + p.t) * d.x_row + p.h * d.x_head, p.u, v);
+  if (p.u.turns) turn_unit<false, MODE>(cs, r, p.t, p.j, v);
+  st_unit<IT, MODE>(d.out, (int64_t)(d.row0 + p.t) * d.out_row + p.h * d.out_head, p.u, v);
 }
 
 // Within a wave: what its lanes have stored to LDS is there for the others.  (LDS instructions of a wave run in order.)
@@ -169,24 +220,40 @@ __device__ __forceinline__ int run_of(const Run* runs, int n_runs) {
 
 }  // namespace
 
-// Dense rows: grid (groups of 16 rows of a run, shares of their units), 256 threads.
-template <class IT, bool VEC>
+// Dense rows: grid (groups of 16 rows of a run, shares of their units), 256 threads.  A wave takes 128 units at a time, two a
+// lane, the next 128 on their way while these are turned, the first ones while the cosines are computed.
+template <class IT, int PAIRS, int MODE>
 __global__ __launch_bounds__(256) void k_rotate(RotRowsArgs a) {
-  __shared__ double2 s_cs[16 * kRotPairs];
+  constexpr bool VEC = MODE != kAny;
+  __shared__ double2 s_cs[16 * PAIRS];
   const RotRun run = a.runs[run_of(a.runs, a.n_runs)];
   const int i0 = 16 * (int)(blockIdx.x - run.first), rows = min(16, run.n - i0);
+  const int units = units_of(a.rot, a.hd), all = rows * a.heads * units, l = threadIdx.x & 63;
+  const Dense d{a.x, a.out, a.heads, a.hd, units, all, run.row0 + i0, a.by_heads, a.by_units, a.x_row, a.x_head, a.out_row, a.out_head};
+  int first = 128 * (blockIdx.y * 4 + (threadIdx.x >> 6));
+  RawUnit<IT> raw[2], next[2];
+  if constexpr (VEC)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) raw[k] = ld_dense<IT, MODE>(a.rot, d, first + 64 * k + l);
   fill_cs(s_cs, offsetof(RotRowsArgs, rot) + offsetof(RotArgs, turns), a.rot, rows, run.pos + (int64_t)run.step * i0, run.step);
   __syncthreads();
-  const int all = rows * a.heads * units_of(a.rot, a.hd);
-  for (int first = 128 * (blockIdx.y * 4 + (threadIdx.x >> 6)); first < all; first += 512 * gridDim.y)
-    turn_rows<IT, VEC>(s_cs, a.rot, a.x, a.out, a.heads, a.hd, a.x_row, a.x_head, a.out_row, a.out_head, run.row0 + i0, rows, first);
+  for (; first < all; first += 512 * gridDim.y) {
+    if constexpr (VEC)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) next[k] = ld_dense<IT, MODE>(a.rot, d, first + 512 * (int)gridDim.y + 64 * k + l);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) put_dense<IT, MODE>(s_cs, a.rot, d, first + 64 * k + l, &raw[k]);
+    if constexpr (VEC) raw[0] = next[0], raw[1] = next[1];
+  }
 }
 
 // Rows into the cache: grid (pages of all runs, shares of a page's work, layers), 256 threads.  A wave takes K or V of a kv
 // head at a time: its rows as units (K turned) into a tile of fp32 in LDS, and out of that in the order of the page block, so
-// that a block is stored in whole lines whatever the layout of pairs; or 128 units of the queries.
-template <class KT, class IT, int HD, bool ROT, bool VEC>
+// that a block is stored in whole lines whatever the layout of pairs; or hd units of the queries.  The rows of a wave's next
+// item are on their way meanwhile, those of its first while the cosines are computed.
+template <class KT, class IT, int HD, bool ROT, int MODE>
 __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
+  constexpr bool VEC = MODE != kAny;
   constexpr bool F4 = std::is_same_v<KT, fp4_t>, I8 = std::is_same_v<KT, i8_t>;
   constexpr bool ODD = F4 || std::is_same_v<KT, fp8_t> || std::is_same_v<KT, bf16_t>;  // (rounded again, to few bits)
   constexpr int NS = HD / 32, ND = HD / 16, TS = HD + 4;  // TS: 16 rows of the tile fall in different banks
@@ -200,32 +267,70 @@ __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63, lc = l & 15, lg = l >> 4;
   const int page = a.kv.bt[(size_t)run.seq * a.kv.max_pps + pg], hkv = a.kv.hkv;
   const int64_t layer = blockIdx.z;
+  constexpr int U = (ND + 3) / 4;  // units a lane
+  const int q_units = VEC ? ND : units_of(a.rot, HD);
+  const Dense q{a.q, a.q_out, a.hq, HD, q_units, rows * a.hq * q_units, row0, a.by_hq,
+                FastDiv{VEC ? 0xffffffffu / ND + 1 : q_units == ND ? 0xffffffffu / ND + 1 : 0xffffffffu / (ND + 1) + 1}, a.q_row, a.q_head, a.qo_row, a.qo_head};
+  const int q_chunks = ROT && a.q != nullptr ? (q.all + 64 * U - 1) / (64 * U) : 0;
+  const int items = 2 * hkv + q_chunks;
+  auto unit_at = [&](bool is_v, int j) { return ROT && !is_v ? unit_of<MODE>(a.rot, HD, j) : Unit{16 * j, 8, 16 * j + 8, 8, false}; };
+  auto row_at = [&](int item, const void*& src, int64_t& stride) {  // first element of the item's rows
+    const bool is_v = item >= hkv;
+    src = is_v ? a.kv.v : a.kv.k;
+    stride = is_v ? a.kv.v_row : a.kv.k_row;
+    return layer * (is_v ? a.kv.v_layer : a.kv.k_layer) + row0 * stride + (is_v ? (item - hkv) * a.kv.v_head : item * a.kv.k_head);
+  };
+  auto load = [&](int item, RawUnit<IT>* raw) {
+    if (item >= items) return;
+    if (ROT && item >= 2 * hkv) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) raw[k] = ld_dense<IT, MODE>(a.rot, q, 64 * U * (item - 2 * hkv) + 64 * k + l);
+      return;
+    }
+    const void* src;
+    int64_t stride;
+    const int64_t e0 = row_at(item, src, stride);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int id = min(64 * k + l, rows * ND - 1);
+      raw[k] = ld_raw<IT>(src, e0 + id / ND * stride, unit_at(item >= hkv, id % ND));
+    }
+  };
+  int item = blockIdx.y * 4 + w;
+  RawUnit<IT> raw[U], next[U];
+  if constexpr (VEC) load(item, raw);
   if constexpr (ROT) {
     fill_cs(s_cs, offsetof(KvPutArgs, rot) + offsetof(RotArgs, turns), a.rot, rows, 16 * pg + lo, 1);
     __syncthreads();
   }
   float* tile = s_tile[w];
-  const int q_chunks = ROT && a.q != nullptr ? (rows * a.hq * units_of(a.rot, HD) + 127) / 128 : 0;
-  for (int item = blockIdx.y * 4 + w; item < 2 * hkv + q_chunks; item += 4 * gridDim.y) {
-    if (item >= 2 * hkv) {
-      turn_rows<IT, VEC>(s_cs, a.rot, a.q, a.q_out, a.hq, HD, a.q_row, a.q_head, a.qo_row, a.qo_head, row0, rows, 128 * (item - 2 * hkv));
-      continue;
+  auto work = [&](int item, const RawUnit<IT>* raw) {
+    if (ROT && item >= 2 * hkv) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) put_dense<IT, MODE>(s_cs, a.rot, q, 64 * U * (item - 2 * hkv) + 64 * k + l, raw + k);
+      return;
     }
     const bool is_v = item >= hkv;
     const int kvh = is_v ? item - hkv : item;
-    const void* src = is_v ? a.kv.v : a.kv.k;
-    const int64_t row_stride = is_v ? a.kv.v_row : a.kv.k_row;
-    const int64_t e0 = layer * (is_v ? a.kv.v_layer : a.kv.k_layer) + row0 * row_stride + kvh * (is_v ? a.kv.v_head : a.kv.k_head);
+    const void* src;
+    int64_t stride;
+    const int64_t e0 = row_at(item, src, stride);
     // ---- the rows into the tile
     if (!is_v) {
       const int nu = ROT && !VEC ? units_of(a.rot, HD) : ND;
-      for (int id = l; id < rows * nu; id += 64) {
+#pragma unroll
+      for (int k = 0; k < (VEC ? U : U + 1); ++k) {  // (at most 16 (ND + 1) units)
+        const int id = 64 * k + l;
+        if (id >= rows * nu) break;
         const int t = id / nu, j = id - t * nu;
-        const Unit u = ROT ? unit_of(a.rot, HD, j) : Unit{16 * j, 8, 16 * j + 8, 8, false};
+        const Unit u = unit_at(false, j);
         float x[16];
-        ld_unit<IT, VEC>(src, e0 + t * row_stride, u, x);
+        if constexpr (VEC)
+          of_raw<IT>(raw[k], x);
+        else
+          ld_unit<IT>(src, e0 + t * stride, u, x);
         if constexpr (ROT)
-          if (u.turns) turn_unit<ODD>(s_cs, a.rot, t, j, x);
+          if (u.turns) turn_unit<ODD, MODE>(s_cs, a.rot, t, j, x);
         float* d = tile + (lo + t) * TS;
         if constexpr (VEC) {
 #pragma unroll
@@ -239,10 +344,16 @@ __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
         }
       }
     } else {
-      for (int id = l; id < rows * ND; id += 64) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int id = 64 * k + l;
+        if (id >= rows * ND) break;
         const int t = id / ND, j = id - t * ND;
         float x[16];
-        ld_unit<IT, VEC>(src, e0 + t * row_stride, Unit{16 * j, 8, 16 * j + 8, 8, false}, x);
+        if constexpr (VEC)
+          of_raw<IT>(raw[k], x);
+        else
+          ld_unit<IT>(src, e0 + t * stride, unit_at(true, j), x);
         if constexpr (F4) {
           const uint32_t b = mx_scale(umax_lanes<2>(max(amax8(x), amax8(x + 8))));
           if ((j & 1) == 0) ((uint8_t*)s_scale[w])[(lo + t) * NS + (j >> 1)] = (uint8_t)b;
@@ -388,6 +499,13 @@ __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
       }
     }
     wave_sync();  // (the next item's rows overwrite the tile)
+  };
+  for (; item < items; item += 4 * gridDim.y) {
+    if constexpr (VEC) load(item + 4 * gridDim.y, next);
+    work(item, raw);
+    if constexpr (VEC)
+#pragma unroll
+      for (int k = 0; k < U; ++k) raw[k] = next[k];
   }
 }
 
@@ -453,7 +571,7 @@ __global__ __launch_bounds__(256) void k_kv_get4(KvRowsArgs a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[4 * i + k] = v[k];
       }
-      st_unit<IT, VEC>(dense, e0 + t * row_stride, Unit{16 * j, 8, 16 * j + 8, 8, false}, x);
+      st_unit<IT, VEC ? kHalf : kAny>(dense, e0 + t * row_stride, Unit{16 * j, 8, 16 * j + 8, 8, false}, x);
     }
     wave_sync();
   }
@@ -495,17 +613,21 @@ hipError_t launch_kv_put(int kv_type, int io, int hd, KvPutArgs& a, bool rotate,
   bool vec = rows_on16(a.kv, es) && (!rotate || a.rot.rot % 16 == 0);
   if (rotate && a.q != nullptr)
     vec = vec && (((uintptr_t)a.q | (uintptr_t)a.q_out) & 15) == 0 && on16(a.q_row) && on16(a.q_head) && on16(a.qo_row) && on16(a.qo_head);
+  a.by_hq = fast_div((uint32_t)std::max(a.hq, 1));
   const unsigned groups = list_pages(a.kv);
   int longest = 0;
   for (int i = 0; i < a.kv.n_runs; ++i) longest = std::max(longest, std::min(a.kv.runs[i].n, kPage));
-  const int items = 2 * a.kv.hkv + (rotate && a.q != nullptr ? (longest * a.hq * (hd / 16 + 1) + 127) / 128 : 0);
+  const int items = 2 * a.kv.hkv + (rotate && a.q != nullptr ? (longest * a.hq * (hd / 16 + 1) + hd - 1) / hd : 0);
   const dim3 grid(groups, shares_of((uint64_t)groups * n_layers, items, cus), n_layers), block(256);
   auto go = [&](auto kt, auto it, auto hdc, auto rc) {
     using KT = decltype(kt);
     using IT = decltype(it);
     constexpr int HD = decltype(hdc)::value;
     constexpr bool ROT = decltype(rc)::value;
-    return vec ? launch_k(k_kv_put<KT, IT, HD, ROT, true>, grid, block, s, a) : launch_k(k_kv_put<KT, IT, HD, ROT, false>, grid, block, s, a);
+    if (!vec) return launch_k(k_kv_put<KT, IT, HD, ROT, kAny>, grid, block, s, a);
+    if constexpr (ROT)
+      if (a.rot.interleaved) return launch_k(k_kv_put<KT, IT, HD, ROT, kInterleaved>, grid, block, s, a);
+    return launch_k(k_kv_put<KT, IT, HD, ROT, kHalf>, grid, block, s, a);
   };
   auto of_io = [&](auto kt, auto rc) {
     using H = std::integral_constant<int, 128>;
@@ -539,7 +661,7 @@ hipError_t launch_kv_get4(int io, int hd, KvRowsArgs& a, int n_layers, hipStream
 }
 
 hipError_t launch_rotate(int io, RotRowsArgs& a, int cus, hipStream_t s) {
-  if (a.n_runs < 1 || a.n_runs > kKvRuns || a.heads < 1 || a.hd < 2 || a.hd > 2 * kRotPairs || a.rot.rot < 2 || a.rot.rot > a.hd || (a.rot.rot & 1))
+  if (a.n_runs < 1 || a.n_runs > kKvRuns || a.heads < 1 || a.heads > kRotHeads || a.hd < 2 || a.hd > 2 * kRotPairs || a.rot.rot < 2 || a.rot.rot > a.hd || (a.rot.rot & 1))
     return hipErrorInvalidValue;
   unsigned groups = 0;
   int longest = 0;
@@ -554,10 +676,20 @@ hipError_t launch_rotate(int io, RotRowsArgs& a, int cus, hipStream_t s) {
   auto on16 = [&](int64_t e) { return e * es % 16 == 0; };
   const bool vec = (((uintptr_t)a.x | (uintptr_t)a.out) & 15) == 0 && on16(a.x_row) && on16(a.x_head) && on16(a.out_row) &&
                    on16(a.out_head) && a.rot.rot % 16 == 0 && a.hd % 16 == 0;
-  const int64_t units = (int64_t)longest * a.heads * (a.hd / 16 + 2);
-  const dim3 grid(groups, shares_of(groups, (int)std::min<int64_t>((units + 127) / 128, 1 << 17), cus)), block(256);
-  if (io == 1) return vec ? launch_k(k_rotate<bf16_t, true>, grid, block, s, a) : launch_k(k_rotate<bf16_t, false>, grid, block, s, a);
-  return vec ? launch_k(k_rotate<float, true>, grid, block, s, a) : launch_k(k_rotate<float, false>, grid, block, s, a);
+  const int units = (a.rot.rot + 15) / 16 + (a.hd - a.rot.rot + 15) / 16;  // of a head
+  a.by_heads = fast_div((uint32_t)a.heads);
+  a.by_units = fast_div((uint32_t)units);
+  const dim3 grid(groups, shares_of(groups, (longest * a.heads * units + 127) / 128, cus)), block(256);
+  auto go = [&](auto it, auto pairs) {
+    using IT = decltype(it);
+    constexpr int P = decltype(pairs)::value;
+    if (!vec) return launch_k(k_rotate<IT, P, kAny>, grid, block, s, a);
+    return a.rot.interleaved ? launch_k(k_rotate<IT, P, kInterleaved>, grid, block, s, a) : launch_k(k_rotate<IT, P, kHalf>, grid, block, s, a);
+  };
+  using Half = std::integral_constant<int, kRotPairs / 2>;  // (half the LDS)
+  using All = std::integral_constant<int, kRotPairs>;
+  if (io == 1) return a.rot.rot <= kRotPairs ? go(bf16_t{}, Half{}) : go(bf16_t{}, All{});
+  return a.rot.rot <= kRotPairs ? go(float{}, Half{}) : go(float{}, All{});
 }
 
 }  // namespace laser

@@ -2573,7 +2573,8 @@ static laser_status rotate_rows(const laser_rope* rope, int n_runs, const laser_
   RotRowsArgs a{};
   laser_status st = rot_args(rope, a.rot);
   if (st != LASER_OK) return st;
-  if (heads < 1 || heads > (1 << 16)) return laser_fail(LASER_ERR_INVALID_ARG, "bad number of heads");
+  if (heads < 1) return laser_fail(LASER_ERR_INVALID_ARG, "bad number of heads");
+  if (heads > kRotHeads) return laser_fail(LASER_ERR_UNSUPPORTED, "more than %d heads", kRotHeads);
   if (n_runs < 0 || (n_runs > 0 && !runs)) return laser_fail(LASER_ERR_INVALID_ARG, "bad runs");
   st = check_rows(x, "x", heads, rope->head_dim, false);
   if (st == LASER_OK) st = check_rows(out, "out", heads, rope->head_dim, true);
