@@ -57,6 +57,10 @@ inline int64_t span_part_bytes(const AttendSize& s, int splits, int heads, int h
 // heads, 8 sequences, 17 pages 50.5 and 60.8; INT8, 16 sequences of 100-2,000, 2 pages 13.4 and 11.5; 6 of
 // 3,000-9,000, 9 pages 20.5 and 26.6).  Runs end at 32 pages: more rounds even out ragged lengths (64 sequences of
 // 3,000-14,000: 219 us with runs of 133 pages, 192 with 33).
+// 4-bit pools (f4): a wave takes pages two at a time, and an odd one costs as much as two.  The kernel with 16 columns and bf16
+// rows has three workgroups on a CU, and half the bytes in flight per wave: shorter runs (us, `two` and half of it: 8B heads,
+// 16 sequences of 1,000-9,000 27.5 and 25.8; 8 of 3,000-14,000 26.7 and 24.5; 128 of 1,000-6,000 in runs of 32 and 20
+// 126.7 and 120; 4 sequences, 8 rows, which have 32 columns and two workgroups, 27.0 and 33.2).
 // A span of up to 32 pages stays whole, since joining splits is a launch of its own, up to 64 where there
 // are spans enough to fill the CUs (64 sequences of 50-600 positions: 18.2 us split, 14.4 whole) or rows enough to
 // make the join long.
@@ -65,9 +69,11 @@ inline int64_t span_part_bytes(const AttendSize& s, int splits, int heads, int h
 // number of splits at which all partials (8 or 17 KB per workgroup) fit kAttendPartBytes.
 // Tile kernel: see tile_run.
 // mode: 0 the kernels as above, 1 only row kernels, 2 the tile kernel wherever it can be (laser_model_set_attend_kernel).
-inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool i8, bool io16, int mode) {
+inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd, int cus, int es, bool i8, bool io16, int mode,
+                        bool f4 = false) {
   int64_t work = 0, wide = 0, wgs = 0;
-  const int half_parts = io16 ? (i8 ? 12 : 8) : i8 ? 15 : es == 1 ? 12 : 10;
+  bool narrow = true;  // (row kernels: 16 columns at most)
+  const int half_parts = io16 ? (i8 || f4 ? 12 : 8) : i8 || f4 ? 15 : es == 1 ? 12 : 10;
   auto fills = [&](int64_t cols) {  // tiles filled far enough
     return cols > kAttendFewCols && (mode == 2 || 2 * (int64_t)attend_ceil(cols, 32) >= half_parts * (int64_t)attend_ceil(cols, 256));
   };
@@ -81,11 +87,16 @@ inline void plan_attend(AttendSize* s, int n, int q_heads, int kv_heads, int hd,
     s[i].kind = tiles && fills(cols) ? 2 : es == 4 || cols <= 16 || !io16 ? 0 : 1;
     s[i].tiles = attend_ceil(cols, attend_cols(s[i].kind));
     if (s[i].kind == 2) continue;
+    narrow &= s[i].kind == 0;
     work += (int64_t)s[i].pages * s[i].tiles * kv_heads;
     wgs += (int64_t)s[i].tiles * kv_heads;
   }
   const int two = attend_ceil(work, (int64_t)cus * 8);  // pages per wave, two workgroups per CU
-  const int run = two <= (es == 1 ? 4 : 8) ? std::max(2, attend_ceil(work, (int64_t)cus * 4)) : std::min(two, 32);
+  int run = two <= (es == 1 ? 4 : 8) ? std::max(2, attend_ceil(work, (int64_t)cus * 4)) : std::min(two, 32);
+  if (f4) {
+    if (two > 8) run = narrow && io16 ? std::min(attend_ceil(two, 2), 20) : std::min(two, 24);
+    run += run & 1;
+  }
   const int most = std::max(1, attend_ceil(64 * (int64_t)cus, std::max<int64_t>(wgs, 1)));
   int widest = 1;
   for (int i = 0; i < n; ++i) {

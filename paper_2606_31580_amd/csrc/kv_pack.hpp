@@ -102,6 +102,28 @@ __device__ __forceinline__ uint32_t mx_pack8(const float* x, float scale) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
 }
 
+// The same from values of 16 bits, packed two to a word: bf16 that holds the value, or its first 8 significant bits with the
+// last one set if anything lies below (which rounds to a code as the value itself does).
+__device__ __forceinline__ uint32_t amax8_16(u32x4 w) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  auto mag = [](uint32_t x) { return __builtin_bit_cast(u16x2, x & 0x7fff7fffu); };
+  const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(mag(w[0]), mag(w[1])), __builtin_elementwise_max(mag(w[2]), mag(w[3])));
+  return max((uint32_t)m[0], (uint32_t)m[1]) << 16;  // (as the bits of an fp32 number)
+}
+template <int SEL>
+__device__ __forceinline__ uint32_t mx_pack2_16(uint32_t old, uint32_t pair, float scale) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(b2, pair), scale, SEL);
+}
+__device__ __forceinline__ uint32_t mx_pack8_16(u32x4 w, float scale) {
+  return mx_pack2_16<3>(mx_pack2_16<2>(mx_pack2_16<1>(mx_pack2_16<0>(0u, w[0], scale), w[1], scale), w[2], scale), w[3], scale);
+}
+// Two fp32 values so.
+__device__ __forceinline__ uint32_t odd16x2(float a, float b) {
+  auto odd = [](float f) { return __float_as_uint(f) | (min(__float_as_uint(f) & 0xffffu, 1u) << 16); };
+  return __builtin_amdgcn_perm(odd(b), odd(a), 0x07060302u);
+}
+
 // Four values as E4M3 (to nearest even, saturated at +-448; NaN stays NaN).
 __device__ __forceinline__ uint32_t pk_fp8x4(const float* x) {
   float c[4];

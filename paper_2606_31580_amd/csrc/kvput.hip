@@ -23,6 +23,14 @@ namespace {
 __device__ __forceinline__ float to_odd(double d) {
   return (float)__hiloint2double(__double2hiint(d) | (int)min((uint32_t)__double2loint(d), 1u), 0);
 }
+// Two doubles as 16-bit values that round to a few bits as they do (see amax8_16).
+__device__ __forceinline__ uint32_t odd16x2(double a, double b) {
+  auto odd = [](double d) {
+    const uint32_t hi = (uint32_t)__double2hiint(d);
+    return __float_as_uint((float)__hiloint2double((int)(hi | (min((hi & 0x1fffu) | (uint32_t)__double2loint(d), 1u) << 13)), 0));
+  };
+  return __builtin_amdgcn_perm(odd(b), odd(a), 0x07060302u);
+}
 __device__ __forceinline__ int div_by(int n, FastDiv d) { return d.m == 0 ? n : (int)__umulhi((uint32_t)n, d.m); }
 // How the pairs of a launch's rows lie, and how its rows are read: by 16-byte pieces, whole units only; or element by
 // element, whatever the layout.
@@ -115,9 +123,15 @@ __device__ __forceinline__ void of_raw(const RawUnit<IT>& r, float* x) {
 }
 template <class IT, int MODE>
 __device__ __forceinline__ void st_unit(void* base, int64_t e, const Unit& u, const float* x) {
-  if constexpr (MODE != kAny) {
-    st_row8<IT, true>(base, e + u.a0, x);
-    st_row8<IT, true>(base, e + u.a1, x + 8);
+  if constexpr (MODE != kAny) {  // (non-temporal: 16,384 rows of 32 heads turned in 54.7 us, 57.8 without)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const Piece<IT> p = pack<IT>(x + 8 * h, nullptr);
+      char* at = (char*)base + (e + (h == 0 ? u.a0 : u.a1)) * (int64_t)sizeof(IT);
+#pragma unroll
+      for (int i = 0; i < Piece<IT>::W; i += 4)
+        __builtin_nontemporal_store(u32x4{p.w[i], p.w[i + 1], p.w[i + 2], p.w[i + 3]}, (u32x4*)(at + 4 * i));
+    }
   } else {
     st_part<IT>(base, e + u.a0, u.n0, x);
     st_part<IT>(base, e + u.a1, u.n1, x + 8);
@@ -141,17 +155,22 @@ __device__ __forceinline__ void fill_cs(double2* cs, size_t turns_at, const RotA
     cs[t * width + (p & 7) * (width >> 3) + (p >> 3)] = make_double2(r.amplitude * c, r.amplitude * s);
   }
 }
+template <int MODE>
+__device__ __forceinline__ void turn_pair(const double2* row, int w8, int i, bool side, const float* x, double& u, double& v) {
+  const double2 k = row[i * w8];
+  const double a = side ? x[2 * i] : x[i], b = side ? x[2 * i + 1] : x[8 + i];
+  u = fma(a, k.x, -(b * k.y));
+  v = fma(b, k.x, a * k.y);
+}
 template <bool ODD, int MODE>
 __device__ __forceinline__ void turn_unit(const double2* cs, const RotArgs& r, int t, int j, float* x) {
   const bool side = MODE == kAny ? r.interleaved != 0 : MODE == kInterleaved;
-  const int width = cs_width(r.rot >> 1), w8 = width >> 3;
-  const double2* row = cs + t * width + j;
+  const int width = cs_width(r.rot >> 1);
   float y[16];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const double2 k = row[i * w8];
-    const double a = side ? x[2 * i] : x[i], b = side ? x[2 * i + 1] : x[8 + i];
-    const double u = fma(a, k.x, -(b * k.y)), v = fma(b, k.x, a * k.y);
+    double u, v;
+    turn_pair<MODE>(cs + t * width + j, width >> 3, i, side, x, u, v);
     y[i] = ODD ? to_odd(u) : (float)u;
     y[8 + i] = ODD ? to_odd(v) : (float)v;
   }
@@ -165,6 +184,28 @@ __device__ __forceinline__ void turn_unit(const double2* cs, const RotArgs& r, i
       x[8 + i] = y[8 + i];
     }
   }
+}
+// The same into 16-bit values, the unit's first and second eight in order.
+template <int MODE>
+__device__ __forceinline__ void turn_unit16(const double2* cs, const RotArgs& r, int t, int j, const float* x, u32x4* w) {
+  const bool side = MODE == kAny ? r.interleaved != 0 : MODE == kInterleaved;
+  const int width = cs_width(r.rot >> 1);
+  uint32_t pairs[8], halves[8];  // (u, v) of pair i; (pairs i, i + 1) of u, then of v
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    double u0, v0, u1, v1;
+    turn_pair<MODE>(cs + t * width + j, width >> 3, i, side, x, u0, v0);
+    turn_pair<MODE>(cs + t * width + j, width >> 3, i + 1, side, x, u1, v1);
+    if (side) {
+      pairs[i] = odd16x2(u0, v0);
+      pairs[i + 1] = odd16x2(u1, v1);
+    } else {
+      halves[i / 2] = odd16x2(u0, u1);
+      halves[4 + i / 2] = odd16x2(v0, v1);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i >> 2][i & 3] = side ? pairs[i] : halves[i];
 }
 
 // Dense rows: rows row0 .. of x, as rows x heads x units.
@@ -256,7 +297,11 @@ __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
   constexpr bool VEC = MODE != kAny;
   constexpr bool F4 = std::is_same_v<KT, fp4_t>, I8 = std::is_same_v<KT, i8_t>;
   constexpr bool ODD = F4 || std::is_same_v<KT, fp8_t> || std::is_same_v<KT, bf16_t>;  // (rounded again, to few bits)
-  constexpr int NS = HD / 32, ND = HD / 16, TS = HD + 4;  // TS: 16 rows of the tile fall in different banks
+  constexpr int NS = HD / 32, ND = HD / 16;
+  // Words of a row of the tile (16 rows fall in different banks): fp32, or, on the way to 4 bits, 16-bit values, which take half
+  // the LDS and fewer instructions (14,336 rows of 8 heads x 128, 32 heads of queries turned: 71.5 us, 75.7 with fp32; without a
+  // rotation 19.0 and 20.6).
+  constexpr int TS = (F4 ? HD / 2 : HD) + 4;
   __shared__ double2 s_cs[ROT ? 16 * HD / 2 : 1];
   __shared__ __align__(16) float s_tile[4][16 * TS];
   __shared__ __align__(16) uint32_t s_scale[4][16];  // of V: fp32 (INT8), or bytes [16][NS]
@@ -273,7 +318,10 @@ __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
                 FastDiv{VEC ? 0xffffffffu / ND + 1 : q_units == ND ? 0xffffffffu / ND + 1 : 0xffffffffu / (ND + 1) + 1}, a.q_row, a.q_head, a.qo_row, a.qo_head};
   const int q_chunks = ROT && a.q != nullptr ? (q.all + 64 * U - 1) / (64 * U) : 0;
   const int items = 2 * hkv + q_chunks;
-  auto unit_at = [&](bool is_v, int j) { return ROT && !is_v ? unit_of<MODE>(a.rot, HD, j) : Unit{16 * j, 8, 16 * j + 8, 8, false}; };
+  auto unit_at = [&](bool is_v, int j) {
+    if (F4 && is_v) return Unit{32 * (j >> 1) + 8 * (j & 1), 8, 32 * (j >> 1) + 8 * (j & 1) + 16, 8, false};  // (dims that share bytes)
+    return ROT && !is_v ? unit_of<MODE>(a.rot, HD, j) : Unit{16 * j, 8, 16 * j + 8, 8, false};
+  };
   auto row_at = [&](int item, const void*& src, int64_t& stride) {  // first element of the item's rows
     const bool is_v = item >= hkv;
     src = is_v ? a.kv.v : a.kv.k;
@@ -329,6 +377,30 @@ __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
           of_raw<IT>(raw[k], x);
         else
           ld_unit<IT>(src, e0 + t * stride, u, x);
+        if constexpr (F4) {
+          u32x4 w16[2];
+          bool done = false;
+          if constexpr (ROT)
+            if (u.turns) {
+              turn_unit16<MODE>(s_cs, a.rot, t, j, x, w16);
+              done = true;
+            }
+          if (!done)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w16[i >> 2][i & 3] = odd16x2(x[2 * i], x[2 * i + 1]);
+          uint32_t* d = (uint32_t*)tile + (lo + t) * TS;
+          if constexpr (VEC) {
+            *(u32x4*)(d + u.a0 / 2) = w16[0];
+            *(u32x4*)(d + u.a1 / 2) = w16[1];
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              if (i < u.n0) ((uint16_t*)d)[u.a0 + i] = (uint16_t)(w16[0][i >> 1] >> (16 * (i & 1)));
+              if (i < u.n1) ((uint16_t*)d)[u.a1 + i] = (uint16_t)(w16[1][i >> 1] >> (16 * (i & 1)));
+            }
+          }
+          continue;
+        }
         if constexpr (ROT)
           if (u.turns) turn_unit<ODD, MODE>(s_cs, a.rot, t, j, x);
         float* d = tile + (lo + t) * TS;
@@ -354,9 +426,21 @@ __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
           of_raw<IT>(raw[k], x);
         else
           ld_unit<IT>(src, e0 + t * stride, unit_at(true, j), x);
-        if constexpr (F4) {
-          const uint32_t b = mx_scale(umax_lanes<2>(max(amax8(x), amax8(x + 8))));
+        if constexpr (F4) {  // dims d and d + 16 side by side, as they share a byte
+          u32x4 w16[2], out[2];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w16[i >> 2][i & 3] = odd16x2(x[2 * i], x[2 * i + 1]);
+          const uint32_t b = mx_scale(umax_lanes<2>(max(amax8_16(w16[0]), amax8_16(w16[1]))));
           if ((j & 1) == 0) ((uint8_t*)s_scale[w])[(lo + t) * NS + (j >> 1)] = (uint8_t)b;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            out[i >> 1][2 * (i & 1)] = __builtin_amdgcn_perm(w16[1][i], w16[0][i], 0x05040100u);
+            out[i >> 1][2 * (i & 1) + 1] = __builtin_amdgcn_perm(w16[1][i], w16[0][i], 0x07060302u);
+          }
+          uint32_t* d = (uint32_t*)tile + (lo + t) * TS + 8 * j;
+          *(u32x4*)d = out[0];
+          *(u32x4*)(d + 4) = out[1];
+          continue;
         }
         if constexpr (I8) {  // the integers, so that a column of the tile needs no scales
           const uint32_t amax = umax_lanes<ND>(max(amax8(x), amax8(x + 8)));
@@ -383,21 +467,23 @@ __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
     char* sc = pool + a.kv.scales + slot * kv_scale_bytes<KT>(HD);
     if (!is_v) {
       const bool mine = lc >= lo && lc < hi;
-      float x[NS][8];
+      [[maybe_unused]] float x[NS][8];
+      if constexpr (!F4)
 #pragma unroll
-      for (int s = 0; s < NS; ++s)
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f32x4 v = *(const f32x4*)(tile + lc * TS + 32 * s + 8 * lg + 4 * h);
+          for (int h = 0; h < 2; ++h) {
+            const f32x4 v = *(const f32x4*)(tile + lc * TS + 32 * s + 8 * lg + 4 * h);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[s][4 * h + i] = mine ? v[i] : 0.f;
-        }
+            for (int i = 0; i < 4; ++i) x[s][4 * h + i] = v[i];  // (not mine: whatever is there)
+          }
       if constexpr (F4) {
         uint32_t wd[NS], b[NS];
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          b[s] = mx_scale(umax_rows(amax8(x[s])));
-          wd[s] = mx_pack8(x[s], __uint_as_float(b[s] << 23));
+          const u32x4 v = *(const u32x4*)(tile + lc * TS + 16 * s + 4 * lg);
+          b[s] = mx_scale(umax_rows(amax8_16(v)));
+          wd[s] = mx_pack8_16(v, __uint_as_float(b[s] << 23));
         }
         if (mine) {
           if constexpr (NS == 4) {
@@ -432,11 +518,11 @@ __global__ __launch_bounds__(256) void k_kv_put(KvPutArgs a) {
         for (int i = 0; i < NS; ++i) s4[i] = s_scale[w][lg * NS + i];
         static_for<NS>([&](auto gc) {
           constexpr int G = decltype(gc)::value;
-          const float* c = tile + t0 * TS + 32 * G + lc;
-          uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, c[0], c[16], mx_arg_v<NS, 0, G>(s4), 0);
-          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, c[TS], c[TS + 16], mx_arg_v<NS, 1, G>(s4), 1);
-          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, c[2 * TS], c[2 * TS + 16], mx_arg_v<NS, 2, G>(s4), 2);
-          wd[G] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, c[3 * TS], c[3 * TS + 16], mx_arg_v<NS, 3, G>(s4), 3);
+          const uint32_t* c = (const uint32_t*)tile + t0 * TS + 16 * G + lc;
+          uint32_t v = mx_pack2_16<0>(0u, c[0], mx_arg_v<NS, 0, G>(s4));
+          v = mx_pack2_16<1>(v, c[TS], mx_arg_v<NS, 1, G>(s4));
+          v = mx_pack2_16<2>(v, c[2 * TS], mx_arg_v<NS, 2, G>(s4));
+          wd[G] = mx_pack2_16<3>(v, c[3 * TS], mx_arg_v<NS, 3, G>(s4));
         });
         if (whole) {
           if constexpr (NS == 4)
@@ -577,11 +663,14 @@ __global__ __launch_bounds__(256) void k_kv_get4(KvRowsArgs a) {
   }
 }
 
-// Workgroups over the work of a page or a group of rows: all of a group's waves have something to do, and groups in all are
-// about 4 to a CU.
-static unsigned shares_of(uint64_t groups, int items, int cus) {
-  const uint64_t most = (uint64_t)(items + 3) / 4, want = std::max<uint64_t>(1, (4 * (uint64_t)cus + groups - 1) / groups);
-  return (unsigned)std::max<uint64_t>(1, std::min(most, want));
+// Workgroups over the work of a page or a group of rows: all of a group's waves have something to do, and all groups together
+// come to `per_cu` workgroups a CU.  Where cosines are computed each workgroup computes them again: 3 a CU, but two a page
+// where queries come along (us, 1 / 2 / 3 / 4 / 8 shares: 4,000 rows of the 8B heads with queries 34.9 / 25.7 / 23.5 / 23.5 /
+// 25.4; 30,000 140 / 132 / 135 / 132 / 151; 14,336 without queries 27.4 / 28.2 / 30.4 / 33.1 / 33.4).  Otherwise 16 (14,336
+// rows: 19.3 / 18.9 / 18.2 / 17.8 / 17.9).
+static unsigned shares_of(uint64_t groups, int items, int cus, int per_cu, int least = 1) {
+  const uint64_t most = (uint64_t)(items + 3) / 4, want = (per_cu * (uint64_t)cus + groups - 1) / groups;
+  return (unsigned)std::max<uint64_t>(1, std::min(most, std::max<uint64_t>(least, want)));
 }
 
 static unsigned list_pages(KvRowsArgs& a) {
@@ -618,7 +707,7 @@ hipError_t launch_kv_put(int kv_type, int io, int hd, KvPutArgs& a, bool rotate,
   int longest = 0;
   for (int i = 0; i < a.kv.n_runs; ++i) longest = std::max(longest, std::min(a.kv.runs[i].n, kPage));
   const int items = 2 * a.kv.hkv + (rotate && a.q != nullptr ? (longest * a.hq * (hd / 16 + 1) + hd - 1) / hd : 0);
-  const dim3 grid(groups, shares_of((uint64_t)groups * n_layers, items, cus), n_layers), block(256);
+  const dim3 grid(groups, shares_of((uint64_t)groups * n_layers, items, cus, rotate ? 3 : 16, items > 2 * a.kv.hkv ? 2 : 1), n_layers), block(256);
   auto go = [&](auto kt, auto it, auto hdc, auto rc) {
     using KT = decltype(kt);
     using IT = decltype(it);
@@ -679,7 +768,7 @@ hipError_t launch_rotate(int io, RotRowsArgs& a, int cus, hipStream_t s) {
   const int units = (a.rot.rot + 15) / 16 + (a.hd - a.rot.rot + 15) / 16;  // of a head
   a.by_heads = fast_div((uint32_t)a.heads);
   a.by_units = fast_div((uint32_t)units);
-  const dim3 grid(groups, shares_of(groups, (longest * a.heads * units + 127) / 128, cus)), block(256);
+  const dim3 grid(groups, shares_of(groups, (longest * a.heads * units + 127) / 128, cus, 3)), block(256);
   auto go = [&](auto it, auto pairs) {
     using IT = decltype(it);
     constexpr int P = decltype(pairs)::value;

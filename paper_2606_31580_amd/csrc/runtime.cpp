@@ -2476,7 +2476,7 @@ laser_status plan_attend_call(const laser_kv* kv, int n_spans, const laser_atten
     job.size.push_back(z);
   }
   plan_attend(job.size.data(), (int)job.size.size(), d.n_q_heads, d.n_kv_heads, d.head_dim, m->cus, m->kv_es, m->kv_i8 != 0,
-              io == LASER_DTYPE_BF16, m->attend_kernel);
+              io == LASER_DTYPE_BF16, m->attend_kernel, m->kv_f4 != 0);
   for (size_t i = 0; i < job.sp.size(); ++i) {
     job.sp[i].nsplit = job.size[i].nsplit;
     const uint64_t rows = (uint64_t)job.sp[i].n * d.n_q_heads, wgs = (uint64_t)job.size[i].tiles * job.size[i].nsplit * d.n_kv_heads;

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional, Sequence
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "liblaser.so")
@@ -504,14 +505,15 @@ def _joined(T, items) -> bytes:
 
 
 _row_dtypes: Dict["object", int] = {}
+_pack_rows = struct.Struct("@Piiqq").pack  # a laser_rows, as C reads it (a structure object takes 0.5 us longer)
 
 
-def _rows(t, what: str, kv: KVCache, heads: int) -> laser_rows:
+def _rows(t, what: str, kv: KVCache, heads: int) -> bytes:
     """A [rows, heads, head_dim] tensor (fp32 or bf16, contiguous in its last dimension) as the library takes it."""
     return _rows_on(t, what, kv.k_pool.device, heads, kv.model.shape.head_dim)
 
 
-def _rows_on(t, what: str, device, heads: int, hd: int) -> laser_rows:
+def _rows_on(t, what: str, device, heads: int, hd: int) -> bytes:
     if not _row_dtypes:
         import torch
         _row_dtypes.update({torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16})
@@ -526,7 +528,7 @@ def _rows_on(t, what: str, device, heads: int, hd: int) -> laser_rows:
     row, head, one = t.stride()
     if one != 1:
         raise ValueError(f"{what}: the last dimension is not contiguous")
-    return laser_rows(t.data_ptr(), dtype, shape[0], row, head)
+    return _pack_rows(t.data_ptr(), dtype, shape[0], row, head)
 
 
 def _stream_of(kv: KVCache, stream) -> int:
@@ -544,7 +546,7 @@ def _kv_rows(fn, kv, layer, runs, k, v, stream):
     if n:
         heads = kv.model.shape.n_kv_heads
         arr = _joined(laser_kv_run, runs)
-        rk, rv = C.byref(_rows(k, "k", kv, heads)), C.byref(_rows(v, "v", kv, heads))
+        rk, rv = _rows(k, "k", kv, heads), _rows(v, "v", kv, heads)
     _call(fn, kv.h, layer, n, arr, rk, rv, _stream_of(kv, stream))
 
 
@@ -619,7 +621,7 @@ def laser_rotate(rope: laser_rope, runs: Sequence[laser_rotate_run], x, out, str
     rx, ro = _rows_on(x, "x", dev, heads, rope.head_dim), _rows_on(out, "out", dev, heads, rope.head_dim)
     if dev.type != "cuda":
         raise ValueError(f"x: on {dev}")
-    args = (C.byref(rope), len(runs), _joined(laser_rotate_run, runs), heads, C.byref(rx), C.byref(ro),
+    args = (C.byref(rope), len(runs), _joined(laser_rotate_run, runs), heads, rx, ro,
             torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream)
     if torch._C._cuda_getDevice() == dev.index:
         _call("laser_rotate", *args)
@@ -638,9 +640,9 @@ def laser_kv_write_rotated(kv: KVCache, layer: int, rope: laser_rope, runs: Sequ
     arr = rk = rv = rq = ro = None
     if n:
         arr = _joined(laser_kv_run, runs)
-        rk, rv = C.byref(_rows(k, "k", kv, shape.n_kv_heads)), C.byref(_rows(v, "v", kv, shape.n_kv_heads))
+        rk, rv = _rows(k, "k", kv, shape.n_kv_heads), _rows(v, "v", kv, shape.n_kv_heads)
         if q is not None:
-            rq, ro = C.byref(_rows(q, "q", kv, shape.n_q_heads)), C.byref(_rows(q_out, "q_out", kv, shape.n_q_heads))
+            rq, ro = _rows(q, "q", kv, shape.n_q_heads), _rows(q_out, "q_out", kv, shape.n_q_heads)
     _call("laser_kv_write_rotated", kv.h, layer, C.byref(rope), n, arr, rk, rv, rq, ro, _stream_of(kv, stream))
 
 
@@ -672,7 +674,7 @@ def laser_attend(kv: KVCache, layer: int, spans: Sequence[laser_attend_span], q,
     arr = _joined(laser_attend_span, spans)
     if workspace is None:
         nb = C.c_size_t()
-        _call("laser_attend_workspace", kv.h, n, arr, rq.dtype, int(causal), window, C.byref(nb))
+        _call("laser_attend_workspace", kv.h, n, arr, _row_dtypes[q.dtype], int(causal), window, C.byref(nb))
         if nb.value:
             if stream is None:
                 workspace = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
@@ -682,7 +684,7 @@ def laser_attend(kv: KVCache, layer: int, spans: Sequence[laser_attend_span], q,
     elif workspace.device != q.device or not workspace.is_contiguous():
         raise ValueError("workspace: not contiguous, or on another device")
     _call("laser_attend", kv.h, layer, n, arr, shape.head_dim ** -0.5 if scale is None else scale, int(causal), window,
-          C.byref(rq), C.byref(ro), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+          rq, ro, _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
           _stream_of(kv, stream))
 
 
