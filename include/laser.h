@@ -429,6 +429,11 @@ typedef struct {
 laser_status laser_rope_frequencies(int rot_dim, double theta, const laser_rope_scaling* scaling, double* inv_freq,
                                     double* amplitude);
 
+/* Frequencies and amplitude of the model's own forwards, in place of rope_theta's, before laser_model_finalize (STATE after): so a
+ * model runs with scaled positions, and keys of its forwards and of laser_kv_write_rotated mix in one cache.  Half layout,
+ * rot_dim = head_dim (UNSUPPORTED); the model copies the values. */
+laser_status laser_model_set_rope(laser_model* m, const laser_rope* rope);
+
 /* Row row0 + i is at position pos + step i, i < n: step 1 for rows of consecutive positions, -1 with -pos to turn them back
  * (amplitude 1), 0 to move rows that are rotated already by pos. */
 typedef struct {

@@ -177,6 +177,8 @@ struct laser_model {
   const void* final_norm = nullptr;
   std::vector<LayerW> layers;
   bool finalized = false;
+  std::vector<double> rope_freq;  // laser_model_set_rope: radians per position of each pair (empty: rope_theta's)
+  double rope_amplitude = 1.0;
   int max_rows = 0;
   char* ws = nullptr;
   Layout lay{};
@@ -692,8 +694,8 @@ extern "C" laser_status laser_model_finalize(laser_model* m, int max_rows, void*
   std::vector<float2> rope((size_t)d.max_positions * half);
   for (int p = 0; p < d.max_positions; ++p)
     for (int i = 0; i < half; ++i) {
-      const double ang = (double)p * std::pow((double)d.rope_theta, -2.0 * i / d.head_dim);
-      rope[(size_t)p * half + i] = make_float2((float)std::cos(ang), (float)std::sin(ang));
+      const double ang = (double)p * (m->rope_freq.empty() ? std::pow((double)d.rope_theta, -2.0 * i / d.head_dim) : m->rope_freq[i]);
+      rope[(size_t)p * half + i] = make_float2((float)(m->rope_amplitude * std::cos(ang)), (float)(m->rope_amplitude * std::sin(ang)));
     }
   Plan* hp = nullptr;
   // fine-grained: the forward's first kernel reads the staged plan over the bus, uncached
@@ -2330,6 +2332,28 @@ laser_status rot_args(const laser_rope* rope, RotArgs& r) {
   }
   return LASER_OK;
 }
+
+}  // namespace
+
+extern "C" laser_status laser_model_set_rope(laser_model* m, const laser_rope* rope) {
+  if (!model_of(m)) return laser_fail(LASER_ERR_STATE, "invalid or destroyed model");
+  if (m->finalized) return laser_fail(LASER_ERR_STATE, "model already finalized");
+  RotArgs r{};
+  const laser_status st = rot_args(rope, r);
+  if (st != LASER_OK) return st;
+  if (rope->head_dim != m->desc.head_dim) return laser_fail(LASER_ERR_INVALID_ARG, "rope: head_dim %d, the model's is %d", rope->head_dim, m->desc.head_dim);
+  if (rope->layout != LASER_ROPE_HALF || rope->rot_dim != rope->head_dim)
+    return laser_fail(LASER_ERR_UNSUPPORTED, "rope: the forward rotates whole heads in the half layout");
+  try {
+    m->rope_freq.assign(rope->inv_freq, rope->inv_freq + rope->rot_dim / 2);
+  } catch (const std::bad_alloc&) {
+    return laser_fail(LASER_ERR_INVALID_ARG, "allocation failed");
+  }
+  m->rope_amplitude = rope->amplitude;
+  return LASER_OK;
+}
+
+namespace {
 
 // What laser_kv_write_rotated adds to a write.
 struct RotateRows {

@@ -111,6 +111,7 @@ _SIGS = {
     "laser_kv_read": (_I, [_P, _I, _I, _P, _P, _P, _P]),
     "laser_kv_write_rotated": (_I, [_P, _I, _P, _I, _P, _P, _P, _P, _P, _P]),
     "laser_rope_frequencies": (_I, [_I, C.c_double, _P, _P, _P]),
+    "laser_model_set_rope": (_I, [_P, _P]),
     "laser_rotate": (_I, [_P, _I, _P, _I, _P, _P, _P]),
     "laser_attend_workspace": (_I, [_P, _I, _P, _I, _I, _I, C.POINTER(C.c_size_t)]),
     "laser_attend": (_I, [_P, _I, _I, _P, C.c_float, _I, _I, _P, _P, _P, _P, C.c_size_t, _P]),
@@ -278,7 +279,8 @@ class Model:
     """A finalized model over device weights (dict name -> torch tensor on the GPU)."""
 
     def __init__(self, shape, weights: Dict[str, "object"], max_rows: int = 16, max_positions: int = 16640, stream=None,
-                 poison: bool = False, tiles: bool = True):
+                 poison: bool = False, tiles: bool = True, rope: Optional["laser_rope"] = None):
+        """rope: frequencies and amplitude of the forwards (whole heads, half layout), instead of the shape's rope_theta."""
         import torch
         self.shape = shape
         self.weights = weights  # kept alive: the library borrows them
@@ -289,6 +291,8 @@ class Model:
         for name, t in weights.items():
             assert t.is_cuda and t.is_contiguous()
             _call("laser_model_set_tensor", self.h, name.encode(), t.data_ptr(), t.numel() * t.element_size())
+        if rope is not None:
+            _call("laser_model_set_rope", self.h, C.byref(rope))
         nbytes = C.c_size_t()
         _call("laser_workspace_size", self.h, max_rows, C.byref(nbytes))
         self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=next(iter(weights.values())).device)

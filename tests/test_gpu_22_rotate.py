@@ -5,12 +5,14 @@ import numpy as np
 import pytest
 import torch
 
-from gpu_helpers import require_gpu
+from gpu_helpers import compare_logits, require_gpu
 from mxfp4_ref import IO, cache, f64, kept, rows
 from oracle import transformer as OT
 from oracle.numerics import round_bf16
 from paged_ref import attend
 from paper_2606_31580_amd import laser as L
+from paper_2606_31580_amd import synth
+from paper_2606_31580_amd.configs import ModelShape
 from test_gpu_16_kv_rows import stored_tol
 from test_gpu_17_attend import queries, tolerance
 
@@ -355,3 +357,52 @@ def test_on_another_stream():
         L.laser_rotate(rope, [L.rotate_run(1, 0)], x[:, :4], here)
     with pytest.raises(TypeError):
         L.laser_rotate(rope, [L.kv_run(0, 0, 1)][:1] + [1], x, here)
+
+
+@pytest.mark.parametrize("name,more", SCALED[1:], ids=[s[0] for s in SCALED[1:]])
+def test_model_with_scaled_positions(monkeypatch, name, more):
+    """A prompt and decode steps of a model with scaled frequencies against the oracle that turns by the same angles, then a
+    position of the caller's own among the forward's keys: laser_kv_write_rotated keeps the bytes that a forward would."""
+    require_gpu()
+    shape = ModelShape("rope-scaled", 2, 256, 4, 2, 64, 688, 2048, False, False, "f32", 1.0e4, 1.0e-5)
+    rope = L.rope(64, 1.0e4, scaling=name, **more)
+    f = np.array(list(rope.held))
+    w = synth.make_weights(shape)
+    model = L.Model(shape, {k: v.cuda() for k, v in w.items()}, max_rows=8, max_positions=512, rope=rope)
+    plain_rope = OT.rope
+
+    def scaled(x, pos, theta):
+        a = pos * f
+        lo, hi = x[..., :32], x[..., 32:]
+        return rope.amplitude * np.concatenate([lo * np.cos(a) - hi * np.sin(a), hi * np.cos(a) + lo * np.sin(a)], axis=-1)
+
+    assert np.allclose(scaled(np.ones(64), 0, 0), rope.amplitude * plain_rope(np.ones(64), 0, 1.0e4))
+    monkeypatch.setattr(OT, "rope", scaled)
+    orc = OT.DecoderOracle(shape, {k: synth.to_numpy(v) for k, v in w.items()})
+    kv = L.KVCache(model, 20, 1, 20, poison=True)
+    kv.add_seq(0, 0)
+    st = OT.SeqState(shape, 512)
+    toks = synth.make_tokens(41, shape.vocab, 5)
+    logits = torch.zeros(1, shape.vocab, device="cuda")
+    L.laser_prefill(model, kv, 0, toks[:40].cuda(), logits[0])
+    torch.cuda.synchronize()
+    for t in toks[:40]:
+        ref = orc.decode_token(st, int(t))
+    compare_logits(logits[0].cpu().numpy(), ref, "prompt")
+    nxt, p = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(1, device="cuda")
+    L.laser_decode_step(model, kv, [0], toks[40:].cuda(), nxt, p, logits)
+    torch.cuda.synchronize()
+    compare_logits(logits[0].cpu().numpy(), orc.decode_token(st, int(toks[40])), "decode")
+    # the forward's keys turned back, and written again by laser_kv_write_rotated
+    for layer in range(2):
+        k, v = (torch.empty(41, 2, 64, device="cuda") for _ in range(2))
+        L.laser_kv_read(kv, layer, [L.kv_run(0, 0, 41)], k, v)
+        raw, again = torch.empty_like(k), [torch.empty_like(k) for _ in range(2)]
+        back = L.rope(64, inv_freq=list(f), amplitude=1.0 / rope.amplitude)
+        L.laser_rotate(back, [L.rotate_run(41, 0, 0, -1)], k, raw)
+        L.laser_kv_write_rotated(kv, layer, rope, [L.kv_run(0, 0, 41)], raw, v)
+        L.laser_kv_read(kv, layer, [L.kv_run(0, 0, 41)], *again)
+        torch.cuda.synchronize()
+        # (three fp32 roundings of values that the pair's size bounds)
+        size = k.abs() + torch.roll(k.abs(), 32, -1)
+        assert bool(((again[0] - k).abs() <= 4 * 2.0 ** -24 * size).all()) and torch.equal(again[1], v)

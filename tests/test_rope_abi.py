@@ -136,3 +136,12 @@ def test_write_rotated_refused(kind):
     assert call([L.kv_run(0, 30, 11)]) == inv and call([L.kv_run(2, 0, 1)]) == inv and call([L.kv_run(0, 0, 2), L.kv_run(0, 1, 1)]) == inv
     assert call(ok, layer=2) == inv and call(ok, handle=None) == state
     assert call(ok, k=_rows(50, 2, L.DTYPE_F32)) == uns and call(ok, k=None) == inv
+
+
+def test_set_rope_refused():
+    m, _ = _kv("bf16")
+    call = lambda h, r: L.lib().laser_model_set_rope(h, None if r is None else C.byref(r))  # noqa: E731
+    assert call(m, L.rope(64, 5.0e5, scaling="linear", factor=2.0)) == L.OK and call(m, L.rope(64)) == L.OK
+    assert call(None, L.rope(64)) == L.ERR_STATE
+    assert call(m, None) == L.ERR_INVALID_ARG and call(m, L.rope(128)) == L.ERR_INVALID_ARG
+    assert call(m, L.rope(64, rot_dim=32)) == L.ERR_UNSUPPORTED and call(m, L.rope(64, layout="interleaved")) == L.ERR_UNSUPPORTED
