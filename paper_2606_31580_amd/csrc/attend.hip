@@ -15,7 +15,7 @@
 // the second takes P^T as the first leaves it in its accumulators: which position stands in which slot
 // of the contraction is free, as long as V is read in the same order.
 // Types: K and V as bf16 (bf16, E4M3 and 8-bit integers are exact in it; an integer row's scale goes
-// onto the scores, and onto the weights).  bf16 queries are exact.  Their weights are two bf16 parts in workgroups of
+// onto the scores, and onto the weights; 4-bit codes times their power of two are exact as well).  bf16 queries are exact.  Their weights are two bf16 parts in workgroups of
 // 16 columns (one or two new tokens, and all rows of an fp32 pool; off by at most 2^-16 of themselves), where the second
 // costs about 1% (64 sequences of 3,000-14,000, 8B heads, INT8: 191.7 and 193.2 us; a chunk of 200 rows of an fp32 pool
 // 22.7 and 23.8).  In wider ones they are rounded to bf16, each off by at most 2^-8 of itself, as the bf16 output is
@@ -27,6 +27,14 @@
 // (whatever the scale), and where the stored V itself can be infinite or NaN, pages that not every
 // column sees whole are looked through and, if one has such a value, taken row by row with the
 // unseen positions' V zeroed.
+//
+// 4-bit pages: a lane's 8 dims of K are a word, which four conversions (two codes and a scale byte each) turn into an operand's
+// 16 bytes; its 4 positions of two dims of V are a word too, whose positions have scales of their own.  So a page of 128 dims is
+// one load of 16 bytes a lane for K, one for V and a word of scales for each, and the conversions are what a row kernel is busy
+// with: 274 vector instructions for a pair of pages, 60% of the cycles; 64 sequences of 3,000-14,000 (8B heads) 106 us, 5.6 TB/s
+// of the 590 MB that it has to read, and 7 us to join them (INT8 194 for 1,147 MB).  A scale of V can make codes infinite or NaN;
+// a pair of pages with such a scale next to unseen positions is put off to a second loop behind the first, which has the row by
+// row path.  With that in the same loop the kernel took 242 registers and two workgroups a CU, without it 148 and three.
 #include <cstddef>
 
 #include "device_common.hpp"
@@ -319,7 +327,7 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
     look(pg + 2);
   };
   auto key = [&](const KRaw* raw, bf16x8* k, auto careful) {
-    if constexpr (F4) {
+    if constexpr (F4) {  // (fp4x8_to_bf16)
     } else if constexpr (ES == 1) {
       uint32_t w4[4];
       if constexpr (I8) {
@@ -349,7 +357,7 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
   };
   // dims 16 d + lc of positions 4 lg .. of both pages
   auto value = [&](const VRaw& va, const VRaw& vb, bf16x8* v, auto careful) {
-    if constexpr (F4) {
+    if constexpr (F4) {  // (value4)
     } else if constexpr (ES == 1) {
       uint32_t w4[4];
       if constexpr (I8) {
@@ -499,7 +507,7 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
 #pragma unroll
       for (int k = 0; k < WP; ++k) p[u][k] = __builtin_bit_cast(bf16x8, pw[k]);
     }
-    bool odd = F4 && decltype(careful)::value;
+    bool odd = F4 && decltype(careful)::value;  // (4-bit pages: known)
     if (!I8 && !F4 && (decltype(careful)::value || !whole)) {  // an infinite or NaN V anywhere in the pair?
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -573,35 +581,34 @@ __global__ __launch_bounds__(256, NT == 1 && sizeof(KT) == 2 && sizeof(IT) == 2 
                 if (crow[u] == r) o[u][2 * G + y] = t;
               }
           });
-          continue;
-        }
-        if constexpr (!F4)
+        } else {
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          VRaw va = b.v[0][d], vb = b.v[1][d];
-          if constexpr (ES == 1) {
-            uint32_t ma = 0, mb = 0;
+          for (int d = 0; d < ND; ++d) {
+            VRaw va = b.v[0][d], vb = b.v[1][d];
+            if constexpr (ES == 1) {
+              uint32_t ma = 0, mb = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              ma |= (vis >> i) & 1 ? 0xffu << (8 * i) : 0u;
-              mb |= (vis >> (4 + i)) & 1 ? 0xffu << (8 * i) : 0u;
+              for (int i = 0; i < 4; ++i) {
+                ma |= (vis >> i) & 1 ? 0xffu << (8 * i) : 0u;
+                mb |= (vis >> (4 + i)) & 1 ? 0xffu << (8 * i) : 0u;
+              }
+              va &= ma;
+              vb &= mb;
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t keep = ES == 2 ? 0xffffu << (16 * (i & 1)) : 0xffffffffu;
+                if (!((vis >> i) & 1)) va[ES == 2 ? i >> 1 : i] &= ~keep;
+                if (!((vis >> (4 + i)) & 1)) vb[ES == 2 ? i >> 1 : i] &= ~keep;
+              }
             }
-            va &= ma;
-            vb &= mb;
-          } else {
+            bf16x8 v[KP];
+            value(va, vb, v, careful);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t keep = ES == 2 ? 0xffffu << (16 * (i & 1)) : 0xffffffffu;
-              if (!((vis >> i) & 1)) va[ES == 2 ? i >> 1 : i] &= ~keep;
-              if (!((vis >> (4 + i)) & 1)) vb[ES == 2 ? i >> 1 : i] &= ~keep;
+            for (int u = 0; u < NT; ++u) {
+              const f32x4 t = mma(v, p[u], o[u][d], careful);
+              if (crow[u] == r) o[u][d] = t;
             }
-          }
-          bf16x8 v[KP];
-          value(va, vb, v, careful);
-#pragma unroll
-          for (int u = 0; u < NT; ++u) {
-            const f32x4 t = mma(v, p[u], o[u][d], careful);
-            if (crow[u] == r) o[u][d] = t;
           }
         }
       }
@@ -804,30 +811,32 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
   auto stage = [&](int buf, int pg, bool as_is) {
     if (!st_v) {  // as in the page: chunk (8 dims, position) at 16 bytes each
       char* d = s_k[buf] + st_p * KB;
-      if constexpr (F4)
+      if constexpr (F4) {
         static_for<NS>([&](auto gc) {
           constexpr int G = decltype(gc)::value;
           *(u32x4*)(d + (64 * G + l) * 16) = fp4x8_to_bf16(raw[0][G], mx_arg<G>(raw_4[0]));
         });
+      } else {
 #pragma unroll
-      for (int i = 0; i < (F4 ? 0 : NL); ++i) {
-        if constexpr (F4) {
-        } else if constexpr (ES == 2) {
-          *(u32x4*)(d + (64 * i + l) * 16) = raw[i];
-        } else {
-          uint32_t t[8];
+        for (int i = 0; i < NL; ++i) {
+          if constexpr (ES == 2) {
+            *(u32x4*)(d + (64 * i + l) * 16) = raw[i];
+          } else {
+            uint32_t t[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) convert(raw[i][e], t[2 * e], t[2 * e + 1]);
-          *(u32x4*)(d + (64 * i + l) * 32) = u32x4{t[0], t[1], t[2], t[3]};
-          *(u32x4*)(d + (64 * i + l) * 32 + 16) = u32x4{t[4], t[5], t[6], t[7]};
+            for (int e = 0; e < 4; ++e) convert(raw[i][e], t[2 * e], t[2 * e + 1]);
+            *(u32x4*)(d + (64 * i + l) * 32) = u32x4{t[0], t[1], t[2], t[3]};
+            *(u32x4*)(d + (64 * i + l) * 32 + 16) = u32x4{t[4], t[5], t[6], t[7]};
+          }
         }
       }
       if (I8 && l < 16) s_ks[buf][16 * st_p + l] = raw_s * sc;
     } else {  // positions 4 x .. 4 x + 3 of a dim go to half x / 2 of its 16 bytes in plane x % 2
       char* d = s_v[buf] + st_p * PB;
       const int left = sp.ke - 16 * (pg + st_p);  // keys of the page
-      if (__builtin_expect(left < 16, 0)) {
-        if constexpr (F4) {
+      bool odd = false;
+      if constexpr (F4) {  // (codes and scales of no key: zeros)
+        if (__builtin_expect(left < 16, 0)) {
           const int n = min(max(left - 4 * (l >> 4), 0), 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -836,30 +845,32 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
               if (i >= n) raw[0][g] &= ~(0xffu << (8 * i)), raw_4[(i * NS + g) / 4] &= ~(0xffu << (8 * ((i * NS + g) % 4)));
         }
 #pragma unroll
-        for (int i = 0; i < (F4 ? 0 : NL); ++i) if constexpr (!F4) {
-          const int n = min(max(left - 4 * ((64 * i + l) / (ES == 2 ? 8 : 4) % 4), 0), 4);  // keys of the 4
-          const uint64_t keep = n == 4 ? ~0ull : (1ull << (8 * ES * n)) - 1;
-          raw[i] &= ES == 2 ? u32x4{(uint32_t)keep, (uint32_t)(keep >> 32), (uint32_t)keep, (uint32_t)(keep >> 32)}
-                            : u32x4{(uint32_t)keep, (uint32_t)keep, (uint32_t)keep, (uint32_t)keep};
-        }
-        if ((l & 15) >= left) raw_s = 0.f;
-      }
-      bool odd = I8 && raw_s != 0.f && !(raw_s >= 0x1p-36f && raw_s <= 0x1p36f);
-      if constexpr (F4)
-#pragma unroll
         for (int i = 0; i < NS; ++i) odd |= mx_odd(raw_4[i]);
-      if constexpr (!I8 && !F4)
+      } else {
+        if (__builtin_expect(left < 16, 0)) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (ES == 2) {
-              odd |= odd_bf16(raw[i][e]);
-            } else {  // E4M3: a NaN is all ones below the sign
-              const uint32_t x = raw[i][e] & 0x7f7f7f7fu;
-              odd |= ((x + 0x01010101u) & 0x80808080u) != 0;
-            }
+          for (int i = 0; i < NL; ++i) {
+            const int n = min(max(left - 4 * ((64 * i + l) / (ES == 2 ? 8 : 4) % 4), 0), 4);  // keys of the 4
+            const uint64_t keep = n == 4 ? ~0ull : (1ull << (8 * ES * n)) - 1;
+            raw[i] &= ES == 2 ? u32x4{(uint32_t)keep, (uint32_t)(keep >> 32), (uint32_t)keep, (uint32_t)(keep >> 32)}
+                              : u32x4{(uint32_t)keep, (uint32_t)keep, (uint32_t)keep, (uint32_t)keep};
           }
+          if ((l & 15) >= left) raw_s = 0.f;
+        }
+        odd = I8 && raw_s != 0.f && !(raw_s >= 0x1p-36f && raw_s <= 0x1p36f);
+        if constexpr (!I8)
+#pragma unroll
+          for (int i = 0; i < NL; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if constexpr (ES == 2) {
+                odd |= odd_bf16(raw[i][e]);
+              } else {  // E4M3: a NaN is all ones below the sign
+                const uint32_t x = raw[i][e] & 0x7f7f7f7fu;
+                odd |= ((x + 0x01010101u) & 0x80808080u) != 0;
+              }
+            }
+      }
       const bool any = __ballot(odd) != 0;
       if (l == 0) s_odd[buf][st_p] = any;
       if (__builtin_expect(any && !as_is, 0)) {
@@ -881,24 +892,24 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttendArgs a) {
           *(u32x2*)(b + 512 * G) = lo;
           *(u32x2*)(b + 512 * G + 256) = hi;
         });
-      }
+      } else {
 #pragma unroll
-      for (int i = 0; i < (F4 ? 0 : NL); ++i) {
-        const int k = 64 * i + l;
-        if constexpr (F4) {
-        } else if constexpr (ES == 2) {
-          const int d0 = k / 32 * 16 + 2 * (k % 8), x = k / 8 % 4;
-          char* b = d + ((x & 1) * HD + d0) * 16 + (x >> 1) * 8;
-          *(u32x2*)b = u32x2{raw[i][0], raw[i][1]};
-          *(u32x2*)(b + 16) = u32x2{raw[i][2], raw[i][3]};
-        } else {
-          const int d0 = k / 16 * 16 + 4 * (k % 4), x = k / 4 % 4;
-          char* b = d + ((x & 1) * HD + d0) * 16 + (x >> 1) * 8;
+        for (int i = 0; i < NL; ++i) {
+          const int k = 64 * i + l;
+          if constexpr (ES == 2) {
+            const int d0 = k / 32 * 16 + 2 * (k % 8), x = k / 8 % 4;
+            char* b = d + ((x & 1) * HD + d0) * 16 + (x >> 1) * 8;
+            *(u32x2*)b = u32x2{raw[i][0], raw[i][1]};
+            *(u32x2*)(b + 16) = u32x2{raw[i][2], raw[i][3]};
+          } else {
+            const int d0 = k / 16 * 16 + 4 * (k % 4), x = k / 4 % 4;
+            char* b = d + ((x & 1) * HD + d0) * 16 + (x >> 1) * 8;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint32_t lo, hi;
-            convert(raw[i][e], lo, hi);
-            *(u32x2*)(b + 16 * e) = u32x2{lo, hi};
+            for (int e = 0; e < 4; ++e) {
+              uint32_t lo, hi;
+              convert(raw[i][e], lo, hi);
+              *(u32x2*)(b + 16 * e) = u32x2{lo, hi};
+            }
           }
         }
       }

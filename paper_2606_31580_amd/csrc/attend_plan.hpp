@@ -48,7 +48,8 @@ inline int64_t span_part_bytes(const AttendSize& s, int splits, int heads, int h
 // or bf16 pools; fp32 rows: 7.5, 6 with E4M3, 5 with bf16 (us, tiles and rows, 8B heads, 16 sequences of 1,000-9,000:
 // INT8, 120 columns, 4 parts, 122 and 100, 192, 6, 121 and 142; E4M3, 96, 3, 111 and 114, 160, 5, 104 and 153;
 // bf16, 3, 125 and 120, 4, 123 and 131; fp32 rows: INT8, 7, 308 and 252, 8, 308 and 307, a chunk of 1,000 rows 253 and
-// 298; E4M3, 5, 205 and 183, 8, 218 and 278; bf16, 5, 234 and 248).
+// 298; E4M3, 5, 205 and 183, 8, 218 and 278; bf16, 5, 234 and 248; 4-bit as INT8: bf16 rows, 5 parts, 108 and 94, 6, 104 and
+// 110; fp32, 6, 207 and 199, 8, 212 and 248; a prompt of 1,024 rows 39 and 26, of 2,048 63 and 62).
 //
 // Row kernels: pages per wave.  Every CU runs one workgroup of 4 waves, or two on 8-bit pools (fewer
 // registers).  Long runs stream best when two workgroups per CU share the pages; where that leaves a wave only
