@@ -433,7 +433,8 @@ def main():
         "higher_is_better": True,
         "scaling": "weak",
         "vs_baseline": None,
-        "dtype": "bf16 weights+KV, fp32 activations" if shape.dtype == "bf16" else "f32",
+        "dtype": ("bf16 weights+KV, fp32 activations" if shape.kv_storage == "bf16" else f"bf16 weights, {shape.kv_storage} KV, fp32 activations")
+        if shape.dtype == "bf16" else "f32",
         "data": "synthetic: random-init weights, seeded pre-filled KV",
         "config": {"workload": wl.name, "model_shape": shape.name, "batch": B, "kv_lens": lens,
                    "probe_every": wl.probe_every, "suffix": S, "trials": T, "attn_merge": args.attn_merge,

@@ -420,7 +420,7 @@ typedef struct {
  *           [0, rot_dim - 1], b - a at least 0.001; the amplitude is 1 + 0.1 ln factor (otherwise 1).
  * scaling may be NULL (PLAIN).  Writes rot_dim / 2 values and the amplitude.  Host only.  INVALID_ARG: NULL, an odd or
  * non-positive rot_dim, theta not above 1, an unknown kind, a factor that is not positive (RAMP: below 1), old_positions or low not positive,
- * high not above low, or anything that is not finite. */
+ * high not above low, or anything that is not finite, theta factor^(..) and the frequencies among it. */
 enum { LASER_ROPE_PLAIN = 0, LASER_ROPE_LINEAR = 1, LASER_ROPE_BASE = 2, LASER_ROPE_BANDS = 3, LASER_ROPE_RAMP = 4 };
 typedef struct {
   int32_t kind;

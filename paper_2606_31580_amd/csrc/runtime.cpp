@@ -2562,7 +2562,7 @@ extern "C" laser_status laser_rope_frequencies(int rot_dim, double theta, const 
     first = std::min(std::max(std::floor(pair(s.high)), 0.0), r - 1.0);
     last = std::min(std::max(std::ceil(pair(s.low)), 0.0), r - 1.0);
   }
-  for (int i = 0; i < rot_dim / 2; ++i) {
+  auto freq = [&](int i) {
     double f = std::pow(base, -2.0 * i / r);
     if (s.kind == LASER_ROPE_LINEAR) f /= s.factor;
     if (s.kind == LASER_ROPE_BANDS) {
@@ -2573,8 +2573,12 @@ extern "C" laser_status laser_rope_frequencies(int rot_dim, double theta, const 
       const double w = std::min(std::max((i - first) / std::max(last - first, 1e-3), 0.0), 1.0);
       f *= 1.0 - w + w / s.factor;
     }
-    inv_freq[i] = f;
-  }
+    return f;
+  };
+  if (!std::isfinite(base) || !(base > 0.0)) return laser_fail(LASER_ERR_INVALID_ARG, "the factor takes theta out of double's range");
+  for (int i = 0; i < rot_dim / 2; ++i)
+    if (!std::isfinite(freq(i))) return laser_fail(LASER_ERR_INVALID_ARG, "frequency %d is not finite", i);
+  for (int i = 0; i < rot_dim / 2; ++i) inv_freq[i] = freq(i);
   *amplitude = s.kind == LASER_ROPE_RAMP ? 1.0 + 0.1 * std::log(s.factor) : 1.0;
   return LASER_OK;
 }

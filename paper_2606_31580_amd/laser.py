@@ -599,6 +599,8 @@ def rope(head_dim: int, theta: float = 1.0e4, rot_dim: Optional[int] = None, lay
     rot_dim = head_dim if rot_dim is None else rot_dim
     if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
         raise ValueError(f"layout {layout!r}: one of {list(ROPE_LAYOUTS)}; scaling {scaling!r}: one of {list(ROPE_SCALINGS)}")
+    if inv_freq is not None and scaling != "plain":
+        raise ValueError("inv_freq holds the frequencies as they are to be: no scaling with it")
     if inv_freq is None:
         inv_freq, own = laser_rope_frequencies(rot_dim, theta, laser_rope_scaling(ROPE_SCALINGS[scaling], factor, old_positions, low, high))
         amplitude = own if amplitude is None else amplitude

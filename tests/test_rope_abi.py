@@ -62,6 +62,18 @@ def test_frequencies_refused():
         L.rope(64, inv_freq=[1.0] * 31)
 
 
+def test_frequencies_beyond_double():
+    """A factor that leaves the doubles' range is refused, and nothing is written."""
+    for rot, theta, s in ((4, 1e4, (2, 1e200, 0.0, 0.0, 0.0)), (4, 1e4, (2, 1e-200, 0.0, 0.0, 0.0)), (64, 1e4, (1, 5e-324, 0.0, 0.0, 0.0)),
+                          (64, 1e4, (3, 5e-324, 1.0, 1.0, 4.0))):
+        f, a = (C.c_double * (rot // 2))(*[-1.0] * (rot // 2)), C.c_double(-1.0)
+        sc = L.laser_rope_scaling(*s)
+        assert L.lib().laser_rope_frequencies(rot, theta, C.byref(sc), f, C.byref(a)) == L.ERR_INVALID_ARG
+        assert list(f) == [-1.0] * (rot // 2) and a.value == -1.0
+    with pytest.raises(ValueError):
+        L.rope(64, scaling="linear", factor=2.0, inv_freq=[1.0] * 32)
+
+
 def _rows(n, heads, dtype=L.DTYPE_BF16, ptr=PTR, row=None, head=64):
     return L.laser_rows(ptr, dtype, n, heads * 64 if row is None else row, head)
 
