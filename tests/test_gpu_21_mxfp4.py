@@ -266,6 +266,35 @@ def test_poisoned_neighbours(byte, mode):
         check(kv, "mxfp4", "bf16", held, [L.attend_span(0, 1, 16, 0), L.attend_span(1, 5, 28, 1), L.attend_span(2, 6, 44, 6), L.attend_span(3, 50, 51, 12)], q)
 
 
+@pytest.mark.parametrize("kind", ["mxfp4", "int8"])
+def test_far_into_a_pool(kind):
+    """Pages that lie past 2^32 bytes of their pool: what a small cache gives, from rotated write to attention, and of a fork."""
+    rng = np.random.default_rng(14)
+    hq, hkv, hd, n = 8, 8, 128, 90
+    pages, layer = {"mxfp4": 140000, "int8": 75000}[kind], 4
+    small, far = (cache(hq, hkv, hd, pages=p, layers=5, kind=kind) for p in (30, pages))
+    k, v, q = (rows(rng, n, h, hd, "bf16") for h in (hkv, hkv, hq))
+    rope = L.rope(hd, 1.0e4)
+    got = []
+    for kv in (small, far):
+        assert kv is small or layer * pages * hkv * hd * 16 // (2 if kind == "mxfp4" else 1) > 2 ** 32
+        kv.add_seq(0, n)
+        out = [torch.zeros_like(x) for x in (q, k, v, q, q, k, v)]
+        L.laser_kv_write_rotated(kv, layer, rope, [L.kv_run(0, 0, n)], k, v, q, out[0])
+        L.laser_kv_read(kv, layer, [L.kv_run(0, 0, n)], *out[1:3])
+        for mode, o in zip((1, 2), out[3:5]):
+            kv.model.set_attend_kernel(mode)
+            L.laser_attend(kv, layer, [L.attend_span(0, n, 0)], out[0], o)
+        kv.model.set_attend_kernel(0)
+        kv.fork(0, 1)
+        L.laser_kv_read(kv, layer, [L.kv_run(1, 0, n)], *out[5:])
+        torch.cuda.synchronize()
+        got.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert torch.equal(got[0][1], got[0][5]) and torch.equal(got[0][2], got[0][6])
+    assert np.array_equal(f64(got[0][2]), kept(kind, f64(v))) if kind == "mxfp4" else True
+
+
 def test_captured():
     """Write, attention and read in one graph, replayed with other rows between eager calls on the same cache."""
     rng = np.random.default_rng(21)

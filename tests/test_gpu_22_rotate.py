@@ -136,6 +136,36 @@ def test_back_and_shifted():
     assert float(((s - direct).abs() / size).max()) <= 4 * 2.0 ** -24
 
 
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,hd,rot", [(8192, 256, 256), (8191, 250, 130)])
+def test_most_heads(heads, hd, rot, io):
+    """The most heads of a call; against 64 bits in 3 of its 19 rows."""
+    require_gpu()
+    rng = np.random.default_rng(1)
+    rope = L.rope(hd, 1.0e4, rot)
+    x = rows(rng, 1, heads, hd, io).expand(19, heads, hd).contiguous()
+    out = torch.full_like(x, 7.0)
+    L.laser_rotate(rope, [L.rotate_run(18, 5000, 1)], x, out)
+    torch.cuda.synchronize()
+    assert bool((out[0] == 7.0).all())
+    for i in (1, 16, 18):
+        ref, size, far = turned(rope, f64(x[i:i + 1]), [5000 + i - 1])
+        assert np.all(np.abs(f64(out[i:i + 1]) - ref) <= rotated_tol(io, ref, size, far))
+
+
+def test_most_rows():
+    """More rows than a launch takes of a run: each is turned by its own position."""
+    require_gpu()
+    n = 2 ** 21 + 37
+    rope = L.rope(2, inv_freq=[2.0 ** -12])
+    x = rows(np.random.default_rng(2), 1, 1, 2, "f32").expand(n, 1, 2).contiguous()
+    L.laser_rotate(rope, [L.rotate_run(n, -3, 0, 2)], x, x)
+    torch.cuda.synchronize()
+    idx = np.concatenate([np.arange(0, n, 9973), np.arange(2 ** 21 - 20, n)])
+    ref, size, far = turned(rope, np.broadcast_to(f64(rows(np.random.default_rng(2), 1, 1, 2, "f32")), (len(idx), 1, 2)), [int(2 * i - 3) for i in idx])
+    assert np.all(np.abs(f64(x[torch.from_numpy(idx).cuda()]) - ref) <= rotated_tol("f32", ref, size, far))
+
+
 def test_odd_values():
     """Infinities and NaN stay within their pair; other dims, heads and rows are as without them."""
     require_gpu()
@@ -357,6 +387,29 @@ def test_on_another_stream():
         L.laser_rotate(rope, [L.rotate_run(1, 0)], x[:, :4], here)
     with pytest.raises(TypeError):
         L.laser_rotate(rope, [L.kv_run(0, 0, 1)][:1] + [1], x, here)
+
+
+@pytest.mark.parametrize("kind", ["mxfp4", "int8", "fp8"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_two_calls_at_once(kind, hd):
+    """Every other position of the same pages from two streams at once, bytes of whose blocks lie side by side: as one call."""
+    rng = np.random.default_rng(8)
+    hkv, n = 2, 120
+    rope = L.rope(hd, 1.0e4)
+    k, v = (rows(rng, n, hkv, hd, "bf16") for _ in range(2))
+    one, two = (cache(4, hkv, hd, kind=kind) for _ in range(2))
+    for c in (one, two):
+        c.add_seq(0, n)
+        L.laser_kv_write(c, 1, [])
+    L.laser_kv_write_rotated(one, 1, rope, [L.kv_run(0, 0, n)], k, v)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for at in range(0, n, 40):
+        for i, s in enumerate(streams):
+            L.laser_kv_write_rotated(two, 1, rope, [L.kv_run(0, p, 1, p) for p in range(at + i, at + 40, 2)], k, v, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(one.k_pool, two.k_pool) and torch.equal(one.v_pool, two.v_pool)
 
 
 @pytest.mark.parametrize("name,more", SCALED[1:], ids=[s[0] for s in SCALED[1:]])
