@@ -2391,6 +2391,7 @@ laser_status kv_rows(laser_kv* kv, int layer, int n_runs, const laser_kv_run* ru
       if (q->dtype != k->dtype || q_out->dtype != k->dtype) return laser_fail(LASER_ERR_UNSUPPORTED, "q and q_out are not of k's type");
       if (q->ptr == q_out->ptr && (q->row_stride != q_out->row_stride || q->head_stride != q_out->head_stride))
         return laser_fail(LASER_ERR_INVALID_ARG, "q_out is q's memory with other strides");
+      if (q_out->ptr == k->ptr || q_out->ptr == v->ptr) return laser_fail(LASER_ERR_INVALID_ARG, "q_out is k's or v's memory");
     }
   }
   const int n_rows = n_runs == 0 ? 0 : std::min({k->rows, v->rows, q ? std::min(q->rows, q_out->rows) : k->rows});

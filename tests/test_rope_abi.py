@@ -157,3 +157,13 @@ def test_set_rope_refused():
     assert call(None, L.rope(64)) == L.ERR_STATE
     assert call(m, None) == L.ERR_INVALID_ARG and call(m, L.rope(128)) == L.ERR_INVALID_ARG
     assert call(m, L.rope(64, rot_dim=32)) == L.ERR_UNSUPPORTED and call(m, L.rope(64, layout="interleaved")) == L.ERR_UNSUPPORTED
+
+
+def test_q_out_is_not_k_or_v():
+    _, kv = _kv("mxfp4")
+    L._call("laser_kv_add_seq", kv, 0, 40)
+    rope, q = L.rope(64), _rows(50, 4, ptr=5 * PTR)
+    runs = L._joined(L.laser_kv_run, [L.kv_run(0, 3, 20)])
+    for at, code in ((PTR, L.ERR_INVALID_ARG), (3 * PTR, L.ERR_INVALID_ARG), (6 * PTR, L.ERR_STATE)):
+        k, v, out = _rows(50, 2), _rows(50, 2, ptr=3 * PTR), _rows(50, 4, ptr=at)
+        assert L.lib().laser_kv_write_rotated(kv, 0, C.byref(rope), 1, runs, C.byref(k), C.byref(v), C.byref(q), C.byref(out), None) == code
